@@ -386,6 +386,124 @@ int plora_probe_stream(uint64_t w_bytes, uint64_t y_bytes, uint32_t w_tile, uint
 int plora_probe_h2d(uint64_t bytes, int32_t iters, plora_stream stream, double* ms_per_copy);
 
 /* ---------------------------------------------------------------------------------------------
+ * Between the q, k, v and the o projections of a layer: rotary positions, a paged KV cache held in 4 bits, and
+ * attention over it.  None of these calls needs a pool; none allocates or synchronises, all enqueue kernels only
+ * on `stream` (so they may be recorded into a HIP graph), and every buffer is the caller's.  Arrays named "device"
+ * are read by the kernels when these run: what they hold cannot be refused by the call, so values out of range are
+ * defined below for each and never touch memory outside the buffers.
+ *
+ * Tensors of heads.  plora_rows describes n_tokens x heads rows of head_dim contiguous elements: row (t, h) starts at
+ * data + t * token_stride + h * head_stride, strides in elements.  data is 16-byte aligned and the strides are
+ * multiples of 16 bytes.  In an output no two rows may overlap. */
+typedef struct {
+  void* data; /* device; read only where the call takes a const plora_rows that it does not write */
+  int64_t token_stride, head_stride;
+} plora_rows;
+
+/* Rotary positions: the first rot_dim channels of a head are rotated in pairs by an angle that grows with the token's
+ * position p:  (a, b) -> (a cos - b sin, b cos + a sin),  angle(p, j) = p * f_j,  j < rot_dim / 2.  The pair is
+ * (j, j + rot_dim / 2), or (2j, 2j + 1) if `interleaved`; channels from rot_dim on stay as they are.  table: device, max_pos x
+ * rot_dim/2 pairs (cos, sin) of floats, 16-byte aligned, made once by plora_rotary_table (or by the caller).
+ * A token whose position is not in [0, max_pos) has no rotation: its rotated channels become NaN. */
+typedef struct {
+  const float* table;
+  int32_t max_pos;     /* >= 1 */
+  int32_t rot_dim;     /* even, 2 .. head_dim */
+  int32_t interleaved; /* 0 or 1 */
+} plora_rotary;
+
+/* Frequencies: f_j = base^(-2j / rot_dim), stretched for contexts longer than the model was trained on:
+ *   NONE    f_j;       LINEAR  f_j / factor;       NTK  f_j with base * factor^(rot_dim / (rot_dim - 2))  (rot_dim > 2)
+ *   TURNS   by how often the pair turns within original_len positions, r = original_len * f_j / (2 pi):
+ *           f_j / factor up to `low` turns, f_j from `high` turns on, (1 - u) * f_j / factor + u * f_j with
+ *           u = (r - low) / (high - low) between.
+ * cos and sin are multiplied by `magnitude` (1: a rotation).  factor >= 1; original_len, low and high count for TURNS
+ * only (original_len >= 1, 0 <= low < high). */
+typedef enum { PLORA_ROTARY_NONE = 0, PLORA_ROTARY_LINEAR = 1, PLORA_ROTARY_NTK = 2, PLORA_ROTARY_TURNS = 3 } plora_rotary_scaling;
+typedef struct {
+  double base, factor, low, high, magnitude;
+  int32_t scaling; /* plora_rotary_scaling */
+  int32_t original_len;
+} plora_rotary_config;
+
+/* Fills table (device, max_pos * rot_dim floats): angles, cos and sin in 64 bits, rounded once.  rot_dim <= 512. */
+int plora_rotary_table(const plora_rotary_config* config, int32_t rot_dim, int32_t max_pos, float* table, plora_stream stream);
+
+/* y = x rotated by the tokens' positions (device, n_tokens entries), in 32 bits, rounded once to dtype.  head_dim: a multiple of
+ * 8, up to 1024.  y may be x (same data, same strides); otherwise the two must not overlap.  inverse != 0: by the negative
+ * angle, which is also the gradient: dL/dx is dL/dy with inverse = 1. */
+int plora_rotate(const plora_rotary* rotary, int32_t dtype, int32_t n_tokens, int32_t n_heads, int32_t head_dim,
+                 const int32_t* positions, const plora_rows* x, const plora_rows* y, int32_t inverse, plora_stream stream);
+
+/* The cache of one layer: n_pages pages (device, 16-byte aligned, plora_kv_page_bytes each) of page_tokens tokens for all
+ * n_kv_heads heads.  A row (token, head) of D = head_dim keys or values is held as D codes of 4 bits, a scale and a min: with
+ * lo, hi = the row's smallest and largest value,
+ *   scale = bf16((hi - lo) / 15), 0 if below 2^-100;  min = bf16(lo);  code = clamp(rint((x - min) / scale), 0, 15), 0 if scale = 0;
+ * in 32 bits, and a code stands for  min + scale * code.  A row with a value that is not finite, or whose scale or min
+ * would not be, has scale = min = NaN: every value of it reads NaN.
+ * A page holds, head after head, page_tokens * (D + 8) bytes:
+ *   keys' codes    page_tokens x D/2 bytes: channel d of token t is nibble d % 2 (low first) of byte t * D/2 + d/2
+ *   values' codes  page_tokens x D/2 bytes: for every 32 tokens D/64 x 4 x 16 x 4 words [j][g][r][i] of 8 codes; nibble n of a
+ *                  word belongs to token 16 * (n/4) + 4 * g + n % 4 of the 32 and to channel (r/4) * (D/4) + (4j + i) * 4 + r % 4
+ *   keys' then values' (scale, min): page_tokens x two bf16 each
+ * (the values lie as the matrix instructions of the attention take them, so they go from memory to registers as they are). */
+typedef struct {
+  int32_t dtype;       /* plora_dtype of q, k, v and the outputs */
+  int32_t n_kv_heads;  /* 1 .. 1024 */
+  int32_t head_dim;    /* 64, 128 or 256 */
+  int32_t page_tokens; /* 32, 64, 128 or 256 */
+  int32_t n_pages;     /* >= 1 */
+  void* pages;         /* device */
+} plora_kv_cache;
+
+/* Bytes of a page: n_kv_heads * page_tokens * (head_dim + 8), or 0 for a cache whose fields are out of range. */
+uint64_t plora_kv_page_bytes(const plora_kv_cache* cache);
+
+/* A batch: n_seqs sequences, sequence i with the tokens tok_start[i] .. tok_start[i+1]-1 of the call's n_tokens rows as its last
+ * ones, and kv_len[i] tokens in the cache, these included: the j-th of its n tokens has place kv_len[i] - n + j.  Token
+ * place s of sequence i lives in page page_table[i * table_stride + s / page_tokens], slot s % page_tokens.
+ * positions: what the rotation goes by (NULL: the places).
+ * Out of range: tok_start is held to [0, n_tokens] and kv_len to [0, min(max_len, table_stride * page_tokens)]; a page outside
+ * [0, n_pages) is a hole: nothing is appended there, it reads as NaN, and attention passes over its tokens; tokens at
+ * negative places are not appended, read as NaN and see no key (unless attention is not causal).  More than max_new tokens
+ * of a sequence: those beyond may be left out.  Rows of no sequence are left alone.  Sequences may share pages that are
+ * only read; two that append to one page race. */
+typedef struct {
+  int32_t n_seqs, n_tokens;
+  int32_t max_new;           /* most tokens of one sequence in this call, >= 1 */
+  int32_t max_len;           /* largest kv_len, >= 1 */
+  int32_t table_stride;      /* >= 1 */
+  const int32_t* tok_start;  /* device, n_seqs + 1 entries, ascending */
+  const int32_t* kv_len;     /* device, n_seqs entries */
+  const int32_t* page_table; /* device, n_seqs x table_stride entries */
+  const int32_t* positions;  /* device, n_tokens entries, or NULL */
+} plora_kv_batch;
+
+/* Writes the batch's tokens into the cache; k and v: n_tokens x n_kv_heads rows.  rotary (or NULL): applied to k on the way,
+ * in 32 bits, without a rounding before the codes are chosen.  Codes of other tokens are kept as they are. */
+int plora_kv_append(const plora_kv_cache* cache, const plora_kv_batch* batch, const plora_rows* k, const plora_rows* v,
+                    const plora_rotary* rotary, plora_stream stream);
+
+/* Reads the batch's tokens back as the values they stand for, rounded once to dtype (a prefix on its way to another cache; tests).
+ * k, v: n_tokens x n_kv_heads rows, written. */
+int plora_kv_read(const plora_kv_cache* cache, const plora_kv_batch* batch, const plora_rows* k, const plora_rows* v, plora_stream stream);
+
+/* Attention of the batch's tokens over their sequences' cache rows:
+ *   out[t, h] = sum_s p_s V[s] ,  p = softmax over the keys s that t sees of  scale * (q[t, h] . K[s]) ,
+ * K, V of kv head h / (n_heads / n_kv_heads), as the values the codes stand for.  Sums are held in 32 bits; codes and q enter exactly
+ * (a q that is rotated on the way, and fp32's, with 22 bits; bf16's rotated one with 11), the weights p with 11 bits for the
+ * 16-bit types and 22 for fp32.  causal != 0: a token at place s sees the
+ * places up to s, with window > 0 the last `window` of them only; causal = 0 (window 0): every place of its sequence, as
+ * for queries that look at an encoder's states.  A token that sees no key gets 0.  NaN in rows that a token does not see
+ * do not reach it.  rotary (or NULL): applied to q on the way.  n_heads: a multiple of n_kv_heads; scale > 0 and finite.
+ * workspace: device, 16-byte aligned, of any size (0 and NULL too): room for partial results.  With few tokens and many
+ * keys the keys are split among workgroups as far as it reaches: n_tokens * n_heads * (head_dim + 2) * 4 bytes per part.
+ * Its contents do not matter and mean nothing afterwards; calls that may overlap need one each. */
+int plora_kv_attend(const plora_kv_cache* cache, const plora_kv_batch* batch, int32_t n_heads, const plora_rows* q,
+                    const plora_rows* out, float scale, int32_t causal, int32_t window, const plora_rotary* rotary, void* workspace,
+                    uint64_t workspace_bytes, plora_stream stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Traffic predictor (Sec. III-A), host only: every pointer below is a host pointer and no call
  * touches the GPU.  A stack of `layers` LSTM layers of `hidden` units over a sliding window of
  * `window` prediction intervals, followed by a fully connected layer that gives one access

@@ -23,12 +23,16 @@ __all__ = ["PLORA_OK", "PLORA_ERR_INVAL", "PLORA_ERR_NOMEM", "PLORA_ERR_EXISTS",
            "plora_manager_create", "plora_manager_destroy", "plora_manager_set_adapter", "plora_manager_set_prediction",
            "plora_manager_request", "plora_manager_prefetch", "plora_manager_scores", "plora_manager_residents",
            "plora_manager_state", "plora_manager_get_stats", "plora_manager_log", "ResidencyManager",
-           "plora_suggest_page_bytes"]
+           "plora_suggest_page_bytes",
+           "PLORA_ROTARY_NONE", "PLORA_ROTARY_LINEAR", "PLORA_ROTARY_NTK", "PLORA_ROTARY_TURNS",
+           "plora_rotary_table", "plora_rotate", "plora_kv_page_bytes", "plora_kv_append", "plora_kv_read", "plora_kv_attend",
+           "RotaryConfig", "RotaryStruct", "RowsStruct", "KvCacheStruct", "KvBatchStruct", "Rotary", "KvBatch", "PagedKvCache"]
 
 PLORA_OK, PLORA_ERR_INVAL, PLORA_ERR_NOMEM, PLORA_ERR_EXISTS = 0, -1, -2, -3
 PLORA_ERR_NOTFOUND, PLORA_ERR_BUSY, PLORA_ERR_HIP, PLORA_ERR_LIMIT = -4, -5, -6, -7
 PLORA_F16, PLORA_BF16, PLORA_F32 = 0, 1, 2
 PLORA_POOL_PLACEMENT_ONLY = 1
+PLORA_ROTARY_NONE, PLORA_ROTARY_LINEAR, PLORA_ROTARY_NTK, PLORA_ROTARY_TURNS = 0, 1, 2, 3
 _STATUS = {0: "OK", -1: "INVAL", -2: "NOMEM", -3: "EXISTS", -4: "NOTFOUND", -5: "BUSY", -6: "HIP", -7: "LIMIT"}
 
 LIB_PATH = os.environ.get("PLORA_LIB") or os.path.join(os.path.dirname(os.path.abspath(__file__)), "libplora.so")
@@ -644,3 +648,169 @@ def plora_suggest_page_bytes(d_in, d_out, dtype, ranks, weights, max_internal_fr
     rc = lib.plora_suggest_page_bytes(C.byref(lay), r.ctypes.data, w.ctypes.data, len(r), max_internal_frag, min_page, max_page,
                                       C.byref(page), C.byref(frag))
     return rc, page.value, frag.value
+
+
+# ---------------------------------------------------------------------------------------------
+# rotary positions, the paged 4-bit KV cache, attention
+# ---------------------------------------------------------------------------------------------
+class RowsStruct(C.Structure):
+    """plora_rows; strides in elements."""
+    _fields_ = [("data", _vp), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class RotaryStruct(C.Structure):
+    _fields_ = [("table", _vp), ("max_pos", _i32), ("rot_dim", _i32), ("interleaved", _i32)]
+
+
+class RotaryConfig(C.Structure):
+    """plora_rotary_config."""
+    _fields_ = [(k, C.c_double) for k in ("base", "factor", "low", "high", "magnitude")] + [("scaling", _i32), ("original_len", _i32)]
+
+    def __init__(self, base=10000.0, factor=1.0, low=0.0, high=0.0, magnitude=1.0, scaling=PLORA_ROTARY_NONE, original_len=0):
+        super().__init__(base, factor, low, high, magnitude, scaling, original_len)
+
+
+class KvCacheStruct(C.Structure):
+    _fields_ = [(k, _i32) for k in ("dtype", "n_kv_heads", "head_dim", "page_tokens", "n_pages")] + [("pages", _vp)]
+
+
+class KvBatchStruct(C.Structure):
+    _fields_ = [(k, _i32) for k in ("n_seqs", "n_tokens", "max_new", "max_len", "table_stride")] + [
+        (k, _vp) for k in ("tok_start", "kv_len", "page_table", "positions")]
+
+
+_rows_p, _rotary_p, _cache_p, _batch_p = C.POINTER(RowsStruct), C.POINTER(RotaryStruct), C.POINTER(KvCacheStruct), C.POINTER(KvBatchStruct)
+lib.plora_rotary_table.argtypes = [C.POINTER(RotaryConfig), _i32, _i32, _vp, _vp]
+lib.plora_rotate.argtypes = [_rotary_p, _i32, _i32, _i32, _i32, _vp, _rows_p, _rows_p, _i32, _vp]
+lib.plora_kv_page_bytes.argtypes = [_cache_p]
+lib.plora_kv_page_bytes.restype = _u64
+lib.plora_kv_append.argtypes = [_cache_p, _batch_p, _rows_p, _rows_p, _rotary_p, _vp]
+lib.plora_kv_read.argtypes = [_cache_p, _batch_p, _rows_p, _rows_p, _vp]
+lib.plora_kv_attend.argtypes = [_cache_p, _batch_p, _i32, _rows_p, _rows_p, _f32, _i32, _i32, _rotary_p, _vp, _u64, _vp]
+
+
+def plora_rotary_table(config, rot_dim, max_pos, table_ptr, stream=None):
+    return lib.plora_rotary_table(C.byref(config), rot_dim, max_pos, table_ptr, stream)
+
+
+def plora_rotate(rotary, dtype, n_tokens, n_heads, head_dim, positions_ptr, x, y, inverse=0, stream=None):
+    """rotary: RotaryStruct; x, y: RowsStruct."""
+    return lib.plora_rotate(rotary, dtype, n_tokens, n_heads, head_dim, positions_ptr, x, y, int(inverse), stream)
+
+
+def plora_kv_page_bytes(cache):
+    return lib.plora_kv_page_bytes(cache)
+
+
+def plora_kv_append(cache, batch, k, v, rotary=None, stream=None):
+    """cache: KvCacheStruct, batch: KvBatchStruct, k, v: RowsStruct, rotary: RotaryStruct or None."""
+    return lib.plora_kv_append(cache, batch, k, v, rotary, stream)
+
+
+def plora_kv_read(cache, batch, k, v, stream=None):
+    return lib.plora_kv_read(cache, batch, k, v, stream)
+
+
+def plora_kv_attend(cache, batch, n_heads, q, out, scale, causal=1, window=0, rotary=None, workspace_ptr=None, workspace_bytes=0, stream=None):
+    return lib.plora_kv_attend(cache, batch, n_heads, q, out, scale, int(causal), int(window), rotary, workspace_ptr, workspace_bytes, stream)
+
+
+_TORCH_DTYPE = {"torch.float16": PLORA_F16, "torch.bfloat16": PLORA_BF16, "torch.float32": PLORA_F32}
+
+
+def _rows_of(call, t, n_tokens, heads, head_dim, dtype):
+    """plora_rows of a torch tensor [tokens, heads, head_dim] (any strides the library takes, the last one 1)."""
+    if t.dim() != 3 or t.shape[0] != n_tokens or (heads and t.shape[1] != heads) or t.shape[2] != head_dim or (head_dim > 1 and t.stride(2) != 1) or \
+            _TORCH_DTYPE.get(str(t.dtype)) != dtype or not t.is_cuda:
+        raise PloraError(call, PLORA_ERR_INVAL)
+    return RowsStruct(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _ints_of(call, t, least):
+    """Device pointer of a contiguous int32 torch tensor of at least that many entries."""
+    if str(t.dtype) != "torch.int32" or not t.is_contiguous() or t.numel() < least or not t.is_cuda:
+        raise PloraError(call, PLORA_ERR_INVAL)
+    return t.data_ptr()
+
+
+class Rotary:
+    """A table of angles (torch float32 tensor [positions, rot_dim/2, 2] on the GPU) and how a head is rotated by it."""
+
+    def __init__(self, table, rot_dim, interleaved=False):
+        if str(table.dtype) != "torch.float32" or not table.is_contiguous() or table.dim() != 3 or table.shape[1] * 2 != rot_dim or \
+                table.shape[2] != 2 or not table.is_cuda:
+            raise PloraError("Rotary", PLORA_ERR_INVAL)
+        self.table = table  # kept alive
+        self.c = RotaryStruct(table.data_ptr(), table.shape[0], rot_dim, int(interleaved))
+
+    @classmethod
+    def make(cls, table, config=None, interleaved=False, stream=None):
+        """Fills `table` by `config` (a RotaryConfig) first."""
+        out = cls(table, table.shape[1] * 2, interleaved)
+        _check("plora_rotary_table", plora_rotary_table(config or RotaryConfig(), out.c.rot_dim, out.c.max_pos, table.data_ptr(), stream))
+        return out
+
+    def rotate(self, positions, x, out, inverse=False, stream=None):
+        """out = x [tokens, heads, head_dim] rotated by positions (int32 [tokens]); out may be x."""
+        n, heads, d = x.shape
+        dtype = _TORCH_DTYPE.get(str(x.dtype), -1)
+        _check("plora_rotate", plora_rotate(self.c, dtype, n, heads, d, _ints_of("plora_rotate", positions, n), _rows_of("plora_rotate", x, n, heads, d, dtype),
+                                            _rows_of("plora_rotate", out, n, heads, d, dtype), inverse, stream))
+        return out
+
+
+class KvBatch:
+    """The sequences of a step (int32 tensors on the GPU): tok_start [n + 1], kv_len [n], page_table [n, columns], positions
+    [n_tokens] or None; max_new / max_len: most tokens of a sequence in this step / in the cache."""
+
+    def __init__(self, tok_start, kv_len, page_table, n_tokens, max_new, max_len, positions=None):
+        n = kv_len.numel()
+        call = "KvBatch"
+        if page_table.dim() != 2 or page_table.shape[0] != n:
+            raise PloraError(call, PLORA_ERR_INVAL)
+        self.kept = (tok_start, kv_len, page_table, positions)
+        self.n_tokens = n_tokens
+        self.c = KvBatchStruct(n, n_tokens, max_new, max_len, page_table.shape[1], _ints_of(call, tok_start, n + 1), _ints_of(call, kv_len, n),
+                               _ints_of(call, page_table, n), None if positions is None else _ints_of(call, positions, n_tokens))
+
+
+class PagedKvCache:
+    """One layer's keys and values in 4 bits, on pages of a caller's tensor (uint8 [pages, page bytes] on the GPU)."""
+
+    def __init__(self, dtype, n_kv_heads, head_dim, page_tokens, pages):
+        self.pages = pages  # kept alive
+        self.dtype, self.heads, self.head_dim = dtype, n_kv_heads, head_dim
+        self.c = KvCacheStruct(dtype, n_kv_heads, head_dim, page_tokens, pages.shape[0], pages.data_ptr())
+        page = plora_kv_page_bytes(self.c)
+        if not page or pages.dim() != 2 or pages.shape[1] != page or not pages.is_contiguous() or str(pages.dtype) != "torch.uint8" or not pages.is_cuda:
+            raise PloraError("PagedKvCache", PLORA_ERR_INVAL)
+
+    @staticmethod
+    def page_bytes(n_kv_heads, head_dim, page_tokens):
+        return plora_kv_page_bytes(KvCacheStruct(PLORA_F16, n_kv_heads, head_dim, page_tokens, 1, None))
+
+    def _rows(self, call, batch, t):
+        return _rows_of(call, t, batch.n_tokens, self.heads, self.head_dim, self.dtype)
+
+    def append(self, batch, k, v, rotary=None, stream=None):
+        """k, v: [tokens, kv heads, head_dim]; rotary: applied to k."""
+        call = "plora_kv_append"
+        _check(call, plora_kv_append(self.c, batch.c, self._rows(call, batch, k), self._rows(call, batch, v), None if rotary is None else rotary.c, stream))
+
+    def read(self, batch, k, v, stream=None):
+        call = "plora_kv_read"
+        _check(call, plora_kv_read(self.c, batch.c, self._rows(call, batch, k), self._rows(call, batch, v), stream))
+
+    def attend(self, batch, q, out, scale, workspace=None, causal=True, window=0, rotary=None, stream=None):
+        """q, out: [tokens, heads, head_dim]; workspace: any contiguous tensor on the GPU, or None; rotary: applied to q."""
+        call = "plora_kv_attend"
+        heads = q.shape[1]
+        rows = [_rows_of(call, t, batch.n_tokens, heads, self.head_dim, self.dtype) for t in (q, out)]
+        size = 0
+        if workspace is not None:
+            if not workspace.is_contiguous() or not workspace.is_cuda:
+                raise PloraError(call, PLORA_ERR_INVAL)
+            size = workspace.numel() * workspace.element_size()
+        _check(call, plora_kv_attend(self.c, batch.c, heads, rows[0], rows[1], scale, causal, window, None if rotary is None else rotary.c,
+                                     workspace.data_ptr() if size else None, size, stream))
+        return out

@@ -1,0 +1,1165 @@
+// Rotary positions, the paged 4-bit KV cache and attention over it (gfx950).  include/plora.h has the contract of every entry
+// point and the layout of a page.
+#include "../../include/plora.h"
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+namespace plora {
+extern thread_local int g_last_hip;  // plora_pool.cpp: what plora_last_hip reports
+}
+
+namespace {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kBlockTok = 32;       // tokens of a values' block, and keys of one step of the attention
+constexpr int kKeyAlign = 64;       // parts of a sequence's keys start at multiples of this
+
+// ---- element types ------------------------------------------------------------------------------------
+
+template <int DT> struct Elt { static constexpr int B = 2, V = 8; };  // bytes, elements per 16 bytes
+template <> struct Elt<PLORA_F32> { static constexpr int B = 4, V = 4; };
+
+template <int DT>
+__device__ __forceinline__ float ld1(const uint8_t* p, int64_t i) {
+  if constexpr (DT == PLORA_F32) return reinterpret_cast<const float*>(p)[i];
+  const uint16_t h = reinterpret_cast<const uint16_t*>(p)[i];
+  if constexpr (DT == PLORA_BF16) return __uint_as_float((uint32_t)h << 16);
+  return (float)__builtin_bit_cast(_Float16, h);
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {  // round to nearest even
+  const f32x2 f = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  asm("" : "+v"(a), "+v"(b));  // the value is rounded to fp32 by the arithmetic before it is rounded to fp16
+  const f32x2 f = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, f16x2));
+}
+template <int DT>
+__device__ __forceinline__ void st1(uint8_t* p, int64_t i, float f) {
+  if constexpr (DT == PLORA_F32) reinterpret_cast<float*>(p)[i] = f;
+  else if constexpr (DT == PLORA_BF16) reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)pack_bf16(f, f);
+  else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)pack_f16(f, f);
+}
+// 8 consecutive elements, 16-byte aligned (p: the first one).
+template <int DT>
+__device__ __forceinline__ void ld8(const uint8_t* p, float* f) {
+  if constexpr (DT == PLORA_F32) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  } else {
+    const uint4 q = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (DT == PLORA_BF16) {
+        f[2 * i] = __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      } else {
+        const f16x2 h = __builtin_bit_cast(f16x2, w[i]);
+        f[2 * i] = (float)h.x;
+        f[2 * i + 1] = (float)h.y;
+      }
+    }
+  }
+}
+template <int DT>
+__device__ __forceinline__ void st8(uint8_t* p, const float* f) {
+  if constexpr (DT == PLORA_F32) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+  } else if constexpr (DT == PLORA_BF16) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+  } else {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_f16(f[0], f[1]), pack_f16(f[2], f[3]), pack_f16(f[4], f[5]), pack_f16(f[6], f[7]));
+  }
+}
+
+// ---- rotation -----------------------------------------------------------------------------------------
+
+struct Rotary {
+  const float* table;  // NULL: no rotation
+  int32_t max_pos, rot, interleaved;
+};
+
+// cos and sin of pair j at the position whose table row is cs (NULL: the position has none).
+__device__ __forceinline__ float2 angle(const float* cs, int j) {
+  if (!cs) return make_float2(__builtin_nanf(""), __builtin_nanf(""));
+  return reinterpret_cast<const float2*>(cs)[j];
+}
+__device__ __forceinline__ const float* angles_at(const Rotary& r, int32_t pos) {
+  return (uint32_t)pos < (uint32_t)r.max_pos ? r.table + (int64_t)pos * r.rot : nullptr;
+}
+// First and second member of a rotated pair; every product and sum is rounded by itself, so the same pair gives the same
+// bits wherever it is computed.
+__device__ __forceinline__ float turn_a(float a, float b, float2 cs) {
+#pragma clang fp contract(off)
+  return a * cs.x - b * cs.y;
+}
+__device__ __forceinline__ float turn_b(float a, float b, float2 cs) {
+#pragma clang fp contract(off)
+  return b * cs.x + a * cs.y;
+}
+
+// Channels c0 .. c0+7 of a row (c0 a multiple of 8), rotated.  The partners of a half-split rotation are read along: a second
+// trip to lines that the neighbouring lanes read anyway.
+template <int DT>
+__device__ __forceinline__ void rotated8(const uint8_t* row, int c0, const Rotary& r, const float* cs, float* f) {
+  ld8<DT>(row + (int64_t)c0 * Elt<DT>::B, f);
+  if (!r.table || c0 >= r.rot) return;
+  const int half = r.rot >> 1;
+  if (r.interleaved && (r.rot & 7) == 0) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const float2 w = angle(cs, (c0 + i) >> 1);
+      const float a = f[i], b = f[i + 1];
+      f[i] = turn_a(a, b, w);
+      f[i + 1] = turn_b(a, b, w);
+    }
+  } else if (!r.interleaved && (half & 7) == 0) {
+    float o[8];
+    const bool second = c0 >= half;
+    const int j0 = second ? c0 - half : c0;
+    ld8<DT>(row + (int64_t)(second ? j0 : c0 + half) * Elt<DT>::B, o);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 w = angle(cs, j0 + i);
+      f[i] = second ? turn_b(o[i], f[i], w) : turn_a(f[i], o[i], w);
+    }
+  } else {  // pairs that cross a group of 8: element by element
+    for (int i = 0; i < 8; ++i) {
+      const int c = c0 + i;
+      if (c >= r.rot) break;
+      const bool second = r.interleaved ? (c & 1) : c >= half;
+      const int j = r.interleaved ? c >> 1 : (second ? c - half : c);
+      const int p = r.interleaved ? c ^ 1 : (second ? j : c + half);
+      const float2 w = angle(cs, j);
+      const float o = ld1<DT>(row, p);
+      const float me = ld1<DT>(row, c);
+      const float v = second ? turn_b(o, me, w) : turn_a(me, o, w);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) f[k] = k == i ? v : f[k];
+    }
+  }
+}
+
+struct TableArgs {
+  float* table;
+  int32_t max_pos, half;
+  double magnitude;
+  double f[256];
+};
+__global__ __launch_bounds__(kThreads) void k_rotary_table(TableArgs a) {
+  const int64_t n = (int64_t)a.max_pos * a.half;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) {
+    const int64_t p = i / a.half;
+    double s, c;
+    sincos((double)p * a.f[i - p * a.half], &s, &c);
+    reinterpret_cast<float2*>(a.table)[i] = make_float2((float)(a.magnitude * c), (float)(a.magnitude * s));
+  }
+}
+
+struct RotateArgs {
+  Rotary r;
+  const int32_t* positions;
+  const uint8_t* x;
+  uint8_t* y;
+  int64_t xt, xh, yt, yh;  // strides in bytes
+  int64_t n_units;         // tokens * heads * units
+  int32_t heads, head_dim;
+  int32_t units;           // of a row: pair units, then units of channels that are copied
+  int32_t pair_units;
+  float sign;
+};
+// One thread, one unit.  VECTOR: a unit is 8 pairs of the half-split layout (two groups of 8 channels), 8 channels of the
+// interleaved one, or 8 channels to copy; otherwise one pair or one channel.
+// Both members of a pair are read before either is written, so y may be x.
+template <int DT, bool VECTOR>
+__global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= a.n_units) return;
+  const int64_t row = i / a.units;
+  const int u = (int)(i - row * a.units);
+  const int64_t t = row / a.heads;
+  const int h = (int)(row - t * a.heads);
+  const uint8_t* x = a.x + t * a.xt + h * a.xh;
+  uint8_t* y = a.y + t * a.yt + h * a.yh;
+  constexpr int W = VECTOR ? 8 : 1, B = Elt<DT>::B;
+  if (u >= a.pair_units) {
+    const int c = a.r.rot + (u - a.pair_units) * W;
+    if constexpr (VECTOR) {
+      float f[8];
+      ld8<DT>(x + c * B, f);
+      st8<DT>(y + c * B, f);
+    } else {
+      st1<DT>(y, c, ld1<DT>(x, c));
+    }
+    return;
+  }
+  const float* cs = angles_at(a.r, a.positions[t]);
+  const int half = a.r.rot >> 1;
+  if constexpr (VECTOR) {
+    float f[8], g[8];
+    if (a.r.interleaved) {
+      ld8<DT>(x + u * 8 * B, f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float2 w = angle(cs, u * 4 + k);
+        w.y *= a.sign;
+        g[2 * k] = turn_a(f[2 * k], f[2 * k + 1], w);
+        g[2 * k + 1] = turn_b(f[2 * k], f[2 * k + 1], w);
+      }
+      st8<DT>(y + u * 8 * B, g);
+    } else {
+      ld8<DT>(x + u * 8 * B, f);
+      ld8<DT>(x + (half + u * 8) * B, g);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        float2 w = angle(cs, u * 8 + k);
+        w.y *= a.sign;
+        const float p = f[k], q = g[k];
+        f[k] = turn_a(p, q, w);
+        g[k] = turn_b(p, q, w);
+      }
+      st8<DT>(y + u * 8 * B, f);
+      st8<DT>(y + (half + u * 8) * B, g);
+    }
+  } else {
+    const int ca = a.r.interleaved ? 2 * u : u, cb = a.r.interleaved ? 2 * u + 1 : u + half;
+    float2 w = angle(cs, u);
+    w.y *= a.sign;
+    const float p = ld1<DT>(x, ca), q = ld1<DT>(x, cb);
+    st1<DT>(y, ca, turn_a(p, q, w));
+    st1<DT>(y, cb, turn_b(p, q, w));
+  }
+}
+
+// ---- the batch ----------------------------------------------------------------------------------------
+
+struct Cache {
+  uint8_t* pages;
+  int64_t page_bytes;
+  int32_t n_pages, heads, page_tokens, page_shift;
+};
+struct Batch {
+  const int32_t *tok_start, *kv_len, *table, *positions;
+  int32_t n_seqs, n_tokens, max_len, stride;  // max_len: no more than the table covers
+};
+struct Rows {
+  uint8_t* p;
+  int64_t ts, hs;  // strides in bytes
+};
+
+// A sequence of the batch, held to what the buffers have.
+struct Seq {
+  int32_t first, n, len;  // first row of the call, rows, tokens in the cache
+};
+__device__ __forceinline__ int32_t hold(int32_t v, int32_t hi) { return v < 0 ? 0 : (v > hi ? hi : v); }
+__device__ __forceinline__ Seq seq_at(const Batch& b, int i) {
+  Seq s;
+  s.first = hold(b.tok_start[i], b.n_tokens);
+  s.n = hold(b.tok_start[i + 1], b.n_tokens) - s.first;
+  s.n = s.n < 0 ? 0 : s.n;
+  s.len = hold(b.kv_len[i], b.max_len);
+  return s;
+}
+
+// Work of ragged sequences is numbered without a list: sequence i owns the numbers from tok_start[i] * mul / div + extra * i up to
+// where the next one's begin, which are at least as many as it has work for.  This finds the sequence of a number: 64 lanes
+// look at 64 sequences at a time.
+__device__ __forceinline__ int64_t first_number(const Batch& b, int i, int mul, int div, int extra) {
+  return (int64_t)hold(b.tok_start[i], b.n_tokens) * mul / div + (int64_t)extra * i;
+}
+__device__ __forceinline__ int find_seq(const Batch& b, int64_t number, int mul, int div, int extra) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = b.n_seqs;
+  while (n > 1) {
+    const int step = (n + 63) >> 6;
+    const int at = lo + lane * step;
+    const bool in = lane * step < n && first_number(b, at, mul, div, extra) <= number;
+    const uint64_t m = __ballot(in);
+    const int k = m ? 63 - __builtin_clzll(m) : 0;
+    lo += k * step;
+    n = n - k * step < step ? n - k * step : step;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// Base of the page of a sequence's place; NULL for a hole.
+__device__ __forceinline__ uint8_t* page_of(const Cache& c, const Batch& b, int seq, int place) {
+  const int32_t page = b.table[(int64_t)seq * b.stride + (place >> c.page_shift)];
+  return (uint32_t)page < (uint32_t)c.n_pages ? c.pages + (int64_t)page * c.page_bytes : nullptr;
+}
+
+// ---- append and read ----------------------------------------------------------------------------------
+
+struct CacheArgs {
+  Cache c;
+  Batch b;
+  Rows k, v;
+  Rotary r;
+};
+
+// One workgroup, one block of 32 places of a sequence, one kv head, keys (blockIdx.z = 0) or values (1).  8 threads share a row.
+struct BlockWork {
+  Seq s;
+  int seq, place0, a;  // first place of the block; place of the sequence's first row
+};
+__device__ __forceinline__ bool block_work(const Batch& b, BlockWork* w) {
+  const int64_t number = blockIdx.x;
+  w->seq = find_seq(b, number, 1, kBlockTok, 2);
+  w->s = seq_at(b, w->seq);
+  const int64_t k = number - first_number(b, w->seq, 1, kBlockTok, 2);
+  w->a = w->s.len - w->s.n;
+  const int from = w->a < 0 ? 0 : w->a;
+  const int64_t place0 = (int64_t)(from & ~(kBlockTok - 1)) + k * kBlockTok;
+  if (w->s.n == 0 || k < 0 || (k > 0 && place0 >= w->s.len)) return false;  // (the first block also has the rows at negative places)
+  w->place0 = (int)place0;
+  return true;
+}
+
+// Word of the values' codes (of a block of 32 tokens) for channel d and token quad g.
+template <int D>
+__device__ __forceinline__ int value_word(int d, int g) {
+  const int quarter = d / (D / 4), rest = d % (D / 4), tile = rest >> 2, r = quarter * 4 + (rest & 3);
+  return ((tile >> 2) * 64 + g * 16 + r) * 4 + (tile & 3);
+}
+
+template <int DT, int D>
+__global__ __launch_bounds__(kThreads) void k_append(CacheArgs a) {
+  constexpr int C = D / 8;  // channels of a thread
+  __shared__ uint32_t codes[kBlockTok][D / 8 + 1];  // values: nibbles of a row in channel order
+  BlockWork w;
+  if (!block_work(a.b, &w)) return;
+  const int head = blockIdx.y, row = threadIdx.x >> 3, part = threadIdx.x & 7;
+  const bool values = blockIdx.z != 0;
+  const int place = w.place0 + row;
+  const bool mine = place >= w.a && place < w.s.len;
+  uint8_t* page = page_of(a.c, a.b, w.seq, w.place0);
+  if (!page) return;
+  const int tok = w.s.first + (place - w.a);
+  float x[C];
+  if (mine) {
+    const Rows& src = values ? a.v : a.k;
+    const uint8_t* p = src.p + tok * src.ts + head * src.hs;
+    Rotary r = a.r;
+    if (values) r.table = nullptr;
+    const float* cs = r.table ? angles_at(r, a.b.positions ? a.b.positions[tok] : place) : nullptr;
+#pragma unroll
+    for (int i = 0; i < C; i += 8) rotated8<DT>(p, part * C + i, r, cs, x + i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < C; ++i) x[i] = 0.f;
+  }
+  float lo = x[0], hi = x[0];
+  uint32_t big = 0;
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    lo = fminf(lo, x[i]);
+    hi = fmaxf(hi, x[i]);
+    const uint32_t m = __float_as_uint(x[i]) & 0x7fffffffu;
+    big = m > big ? m : big;
+  }
+#pragma unroll
+  for (int d = 1; d < 8; d <<= 1) {
+    lo = fminf(lo, __shfl_xor(lo, d));
+    hi = fmaxf(hi, __shfl_xor(hi, d));
+    const uint32_t m = __shfl_xor(big, d);
+    big = m > big ? m : big;
+  }
+  // scale and min are kept in bf16; the codes are chosen against what is kept
+  const uint32_t sm = pack_bf16((hi - lo) / 15.0f, lo);
+  float s = __uint_as_float(sm << 16), m = __uint_as_float(sm & 0xffff0000u);
+  const bool fine = big < 0x7f800000u && fabsf(s) < INFINITY && fabsf(m) < INFINITY;
+  if (s < 0x1p-100f) s = 0.f;
+  // (x - min) / scale rounded as by a division: quotient by the reciprocal, then one correction by the remainder
+  const float inv = s > 0.f ? 1.0f / s : 0.f;
+  uint32_t word[C / 8];
+#pragma unroll
+  for (int i = 0; i < C / 8; ++i) {
+    word[i] = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float d = x[8 * i + k] - m;
+      float q = d * inv;
+      q = __builtin_fmaf(__builtin_fmaf(-q, s, d), inv, q);
+      q = fminf(fmaxf(rintf(q), 0.f), 15.f);
+      word[i] |= (uint32_t)q << (4 * k);
+    }
+    if (!fine) word[i] = 0;
+  }
+  const uint32_t params = fine ? (__float_as_uint(s) >> 16) | (sm & 0xffff0000u) : 0x7fc07fc0u;
+  const int pt = a.c.page_tokens, slot0 = w.place0 & (pt - 1), slot = slot0 + row;
+  uint8_t* hp = page + (int64_t)head * pt * (D + 8);
+  if (mine && part == 0)
+    reinterpret_cast<uint32_t*>(hp + (int64_t)pt * D)[(values ? pt : 0) + slot] = params;
+  if (!values) {
+    if (mine) {
+#pragma unroll
+      for (int i = 0; i < C / 8; ++i) reinterpret_cast<uint32_t*>(hp + slot * (D / 2))[part * (C / 8) + i] = word[i];
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < C / 8; ++i) codes[row][part * (C / 8) + i] = word[i];
+  __syncthreads();
+  // nibbles of the block that are written: token 16 * (n/4) + 4g + n%4
+  const int first = w.a > w.place0 ? w.a - w.place0 : 0, last = w.s.len - w.place0 < kBlockTok ? w.s.len - w.place0 : kBlockTok;
+  uint32_t* out = reinterpret_cast<uint32_t*>(hp + (int64_t)pt * (D / 2) + (slot0 / kBlockTok) * (16 * D));
+  for (int i = threadIdx.x; i < 4 * D; i += kThreads) {
+    const int tile = (i & 3) + (i >> 8) * 4, l = (i >> 2) & 63, g = l >> 4, r = l & 15;
+    const int d = (r >> 2) * (D / 4) + tile * 4 + (r & 3);
+    uint32_t v = 0, mask = 0;
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      const int t = 16 * (n >> 2) + 4 * g + (n & 3);
+      v |= ((codes[t][d >> 3] >> (4 * (d & 7))) & 15u) << (4 * n);
+      mask |= t >= first && t < last ? 15u << (4 * n) : 0u;
+    }
+    if (mask == 0xffffffffu) out[i] = v;
+    else if (mask) out[i] = (out[i] & ~mask) | (v & mask);
+  }
+}
+
+template <int DT, int D>
+__global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
+  constexpr int C = D / 8;
+  BlockWork w;
+  const int head = blockIdx.y, row = threadIdx.x >> 3, part = threadIdx.x & 7;
+  const bool values = blockIdx.z != 0;
+  if (!block_work(a.b, &w)) return;
+  const Rows& dst = values ? a.v : a.k;
+  float x[C];
+  if (w.place0 == 0 && w.a < 0) {  // rows ahead of the first place
+    for (int j = row; j < -w.a && j < w.s.n; j += kBlockTok) {
+#pragma unroll
+      for (int i = 0; i < C; ++i) x[i] = __builtin_nanf("");
+#pragma unroll
+      for (int i = 0; i < C; i += 8) st8<DT>(dst.p + (w.s.first + j) * dst.ts + head * dst.hs + (part * C + i) * Elt<DT>::B, x + i);
+    }
+  }
+  const int place = w.place0 + row;
+  if (place < w.a || place >= w.s.len) return;
+  const uint8_t* page = page_of(a.c, a.b, w.seq, w.place0);
+  uint8_t* out = dst.p + (w.s.first + (place - w.a)) * dst.ts + head * dst.hs + part * C * Elt<DT>::B;
+  if (page) {
+    const int pt = a.c.page_tokens, slot = place & (pt - 1);
+    const uint8_t* hp = page + (int64_t)head * pt * (D + 8);
+    const uint32_t params = reinterpret_cast<const uint32_t*>(hp + (int64_t)pt * D)[(values ? pt : 0) + slot];
+    const float s = __uint_as_float(params << 16), m = __uint_as_float(params & 0xffff0000u);
+    const uint32_t* kw = reinterpret_cast<const uint32_t*>(hp + slot * (D / 2)) + part * (C / 8);
+    const uint32_t* vw = reinterpret_cast<const uint32_t*>(hp + (int64_t)pt * (D / 2) + (slot / kBlockTok) * (16 * D));
+    const int u = slot & (kBlockTok - 1), g = (u & 15) >> 2, nib = (u & 3) + (u >> 4) * 4;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const uint32_t code = values ? vw[value_word<D>(part * C + i, g)] >> (4 * nib) : kw[i >> 3] >> (4 * (i & 7));
+      x[i] = m + s * (float)(code & 15u);  // the product is exact: 12 bits at most
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < C; ++i) x[i] = __builtin_nanf("");
+  }
+#pragma unroll
+  for (int i = 0; i < C; i += 8) st8<DT>(out + i * Elt<DT>::B, x + i);
+}
+
+// ---- attention ----------------------------------------------------------------------------------------
+//
+// Rows are the (token, query head) pairs that share a kv head, token after token.  Matrix instructions take keys as rows and
+// query rows as columns: S^T = K Q^T, then O^T = V^T P^T, so that the weights come out of the first product in the
+// registers in which the second one takes them (a lane has 4 + 4 of 32 keys of one query row both times), and one
+// softmax reference per lane serves its column.
+//
+// Codes enter as fp16 numbers code - 8, exactly, and scale and min stay outside in fp32:
+//   q . K[s] = scale_s * (q . (code - 8)) + (min_s + 8 scale_s) * sum(q),
+//   sum p_s V[s] = sum (p_s scale_s)(code - 8) + sum p_s (min_s + 8 scale_s).
+// So a row of keys or values costs its codes' unpacking (9 instructions per 8 codes) and no multiplication by its scale, and what
+// lies in places that are not seen cannot hurt: codes are finite whatever the memory holds, and scale and min are dropped
+// where a key is masked.  q is multiplied by a power of two per row that brings it into fp16's range (undone in the softmax's
+// factor); fp32 rows, and their weights, go as a high and a low half.
+//
+// Softmax in one pass: weights are p = 2^(x - ref), x = scale * log2(e) * q.K.  w = p * scale_s has to fit fp16 without loss, so ref
+// is chosen for the largest x + log2(max(scale_s, |min_s| / 8)): that product is brought to 2^8 and may grow to 2^15
+// before ref is moved (and the sums are multiplied), which after a row's first keys hardly ever happens.
+
+constexpr float kNoRef = -3e38f;  // ref before the first key: the weight of any x is over its limit
+
+struct AttendArgs {
+  Cache c;
+  Batch b;
+  Rows q, out;
+  Rotary r;
+  int32_t heads, rep;          // query heads; query heads per kv head
+  float scale;                 // * log2(e)
+  int32_t causal, window;
+  int32_t part_keys, parts;    // keys of a part (a multiple of kKeyAlign), parts at most; 1: results go to out
+  int32_t few;                 // 1: k_attend_few has the sequences with at most kFewRows rows, 0: k_attend_many has all
+  float *part_o, *part_ml;     // [part][token][head][head_dim], [part][token][head][2]: sums, (ref, weights)
+};
+constexpr int kFewRows = 16;
+
+// Keys [lo, hi) that rows r0 .. r1-1 of a sequence see, lo on a boundary of kKeyAlign.
+__device__ __forceinline__ void keys_of_rows(const Seq& s, const AttendArgs& a, int r0, int r1, int* lo, int* hi) {
+  *lo = 0;
+  *hi = s.len;
+  if (a.causal) {
+    const int p0 = s.len - s.n + r0 / a.rep, p1 = s.len - s.n + (r1 - 1) / a.rep;
+    *hi = p1 + 1 < 0 ? 0 : p1 + 1;
+    if (a.window) *lo = (p0 - a.window + 1 < 0 ? 0 : p0 - a.window + 1) & ~(kKeyAlign - 1);
+  }
+}
+
+// 8 codes of a word as fp16 numbers code - 8; element pairs are (0,4) (1,5) (2,6) (3,7).
+__device__ __forceinline__ f16x8 codes8(uint32_t w) {
+  const uint32_t h = w >> 8;
+  const uint32_t u[4] = {(w & 0x000f000fu) | 0x64006400u, (w & 0x00f000f0u) | 0x54005400u,   // 1024 + code, 64 + code
+                         (h & 0x000f000fu) | 0x64006400u, (h & 0x00f000f0u) | 0x54005400u};
+  const f16x2 ca = {(_Float16)-1032.f, (_Float16)-1032.f}, cb = {(_Float16)-72.f, (_Float16)-72.f};
+  union { f16x2 p[4]; f16x8 v; } r;
+  r.p[0] = __builtin_bit_cast(f16x2, u[0]) + ca;
+  r.p[1] = __builtin_bit_cast(f16x2, u[1]) + cb;
+  r.p[2] = __builtin_bit_cast(f16x2, u[2]) + ca;
+  r.p[3] = __builtin_bit_cast(f16x2, u[3]) + cb;
+  return r.v;
+}
+__device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// What a lane holds of 32 keys of a kv head.
+template <int D>
+struct Block {
+  uint32_t k[2][D / 32];   // words of keys lane%16 and 16 + lane%16
+  uint4 v[D / 64];         // words of channels, keys 4g .. and 16 + 4g ..
+  uint4 kp[2], vp[2];      // scale and min of keys 4g .. 4g+3 and 16 + 4g ..
+};
+template <int D>
+__device__ __forceinline__ void load_block(Block<D>* o, const uint8_t* hp, int pt, int slot, int lane) {
+  const int r = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const uint8_t* kp = hp + (slot + 16 * t + r) * (D / 2) + g * (D / 8);
+    if constexpr (D == 64) {
+      const uint2 q = *reinterpret_cast<const uint2*>(kp);
+      o->k[t][0] = q.x;
+      o->k[t][1] = q.y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < D / 128; ++i) {
+        const uint4 q = reinterpret_cast<const uint4*>(kp)[i];
+        o->k[t][4 * i] = q.x;
+        o->k[t][4 * i + 1] = q.y;
+        o->k[t][4 * i + 2] = q.z;
+        o->k[t][4 * i + 3] = q.w;
+      }
+    }
+  }
+  const uint8_t* vp = hp + pt * (D / 2) + slot * (D / 2);
+#pragma unroll
+  for (int j = 0; j < D / 64; ++j) o->v[j] = reinterpret_cast<const uint4*>(vp)[j * 64 + lane];
+  const uint4* pp = reinterpret_cast<const uint4*>(hp + pt * D + slot * 4);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    o->kp[t] = pp[4 * t + g];
+    o->vp[t] = pp[pt / 4 + 4 * t + g];
+  }
+}
+
+// Query rows of 16 * NQ columns: the lane's columns are r0 + 16 j + lane%16, and of these the channels (lane/16) * D/4 ..
+template <int D, int NQ, int HQ>
+struct Queries {
+  f16x8 q[NQ][HQ][D / 32];  // HQ = 2: a high and a low half
+  float sum[NQ];   // of the scaled row
+  float f[NQ];     // scale * log2(e) / the row's power of two
+  int place[NQ];   // last place that the column sees
+};
+
+template <int DT, int D, int NQ, int HQ>
+__device__ __forceinline__ void load_queries(Queries<D, NQ, HQ>* o, const AttendArgs& a, const Seq& s, int kvh, int r0, int rows, int lane) {
+  const int g = lane >> 4;
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    const int row = r0 + 16 * j + (lane & 15);
+    const int rr = row < rows ? row : rows - 1;
+    const int t = rr / a.rep, h = kvh * a.rep + rr - t * a.rep, tok = s.first + t;
+    o->place[j] = a.causal ? s.len - s.n + t : 0x7fffffff;
+    const uint8_t* p = a.q.p + tok * a.q.ts + h * a.q.hs;
+    const float* cs = a.r.table ? angles_at(a.r, a.b.positions ? a.b.positions[tok] : s.len - s.n + t) : nullptr;
+    float x[D / 4];
+    float big = 0.f, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 4; i += 8) {
+      rotated8<DT>(p, g * (D / 4) + i, a.r, cs, x + i);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) big = fmaxf(big, fabsf(x[i + k]));
+    }
+    big = fmaxf(big, __shfl_xor(big, 16));
+    big = fmaxf(big, __shfl_xor(big, 32));
+    // 2^e with big * 2^e in [2^9, 2^10)
+    int e = big > 0.f ? 9 - (int)((__float_as_uint(big) >> 23) & 255) + 127 : 0;
+    e = e > 120 ? 120 : e;
+    const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      _Float16 hi[8], lo[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float y = x[8 * i + k] * up;
+        sum += y;
+        hi[k] = (_Float16)y;
+        lo[k] = (_Float16)(y - (float)hi[k]);
+      }
+      o->q[j][0][i] = f16x8{hi[0], hi[4], hi[1], hi[5], hi[2], hi[6], hi[3], hi[7]};
+      if constexpr (HQ == 2) o->q[j][1][i] = f16x8{lo[0], lo[4], lo[1], lo[5], lo[2], lo[6], lo[3], lo[7]};
+    }
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    o->sum[j] = sum;
+    o->f[j] = a.scale * __uint_as_float((uint32_t)(127 - e) << 23);
+  }
+}
+
+// Running sums of a column, per lane.
+template <int D, int NQ>
+struct Sums {
+  f32x4 o[NQ][D / 16];  // channels (lane/16) * D/4 + 4 * tile + i
+  float l[NQ], z[NQ];   // this lane's keys only: weights, weights * (min + 8 scale)
+  float ref[NQ];
+};
+
+__device__ __forceinline__ float param_scale(uint32_t p) { return __uint_as_float(p << 16); }
+__device__ __forceinline__ float param_min(uint32_t p) { return __uint_as_float(p & 0xffff0000u); }
+
+// 32 keys: places key0 .. key0 + 31, of which those below `live` exist.  MASK: some column may not see some of them.
+template <int D, int NQ, int HQ, int HW, bool MASK>
+__device__ __forceinline__ void step(const Block<D>& b, const Queries<D, NQ, HQ>& q, Sums<D, NQ>* s, int key0, int live, int window, int lane) {
+  const int g = lane >> 4;
+  f32x4 t[NQ][2];
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) t[j][0] = t[j][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const f16x8 kc = codes8(b.k[u][i]);
+#pragma unroll
+      for (int j = 0; j < NQ; ++j) {
+#pragma unroll
+        for (int h = HQ - 1; h >= 0; --h) t[j][u] = mfma(kc, q.q[j][h][i], t[j][u]);
+      }
+    }
+  }
+  const uint32_t* kp = reinterpret_cast<const uint32_t*>(&b.kp[0]);
+  const uint32_t* vp = reinterpret_cast<const uint32_t*>(&b.vp[0]);
+  f16x8 w[NQ][HW];
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    float x[8], p[8], wt[8];
+    float top = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      const float sc = param_scale(kp[n]), mc = __builtin_fmaf(8.f, sc, param_min(kp[n]));
+      x[n] = __builtin_fmaf(sc, t[j][n >> 2][n & 3], mc * q.sum[j]) * q.f[j];
+      if constexpr (MASK) {
+        const int key = key0 + 16 * (n >> 2) + 4 * g + (n & 3);
+        const bool sees = key < live && key <= q.place[j] && (window == 0 || key > q.place[j] - window);
+        x[n] = sees ? x[n] : -INFINITY;
+      }
+      p[n] = __builtin_amdgcn_exp2f(x[n] - s->ref[j]);
+      wt[n] = p[n] * param_scale(vp[n]);
+      if constexpr (MASK) wt[n] = p[n] == 0.f ? 0.f : wt[n];
+      top = fmaxf(top, fmaxf(wt[n], p[n] * 0x1p-90f));
+    }
+    if (__any(top > 0x1p15f)) {  // (a NaN is none: it stays where it is)
+      float best = -INFINITY;
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        const float m = fmaxf(fmaxf(param_scale(vp[n]), fabsf(param_min(vp[n])) * 0.125f), 0x1p-90f);
+        best = fmaxf(best, x[n] + (float)((int)(__float_as_uint(m) >> 23) - 127));
+      }
+      best = fmaxf(best, __shfl_xor(best, 16));
+      best = fmaxf(best, __shfl_xor(best, 32));
+      const float ref = fmaxf(s->ref[j], best - 8.f), down = __builtin_amdgcn_exp2f(s->ref[j] - ref);
+      s->ref[j] = ref;
+      s->l[j] *= down;
+      s->z[j] *= down;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) s->o[j][i] *= down;
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        p[n] = __builtin_amdgcn_exp2f(x[n] - ref);
+        wt[n] = p[n] * param_scale(vp[n]);
+        if constexpr (MASK) wt[n] = p[n] == 0.f ? 0.f : wt[n];
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      s->l[j] += p[n];
+      const float mc = __builtin_fmaf(8.f, param_scale(vp[n]), param_min(vp[n]));
+      if constexpr (MASK) s->z[j] += p[n] == 0.f ? 0.f : p[n] * mc;
+      else s->z[j] = __builtin_fmaf(p[n], mc, s->z[j]);
+    }
+    _Float16 hi[8], lo[8];
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      hi[n] = (_Float16)wt[n];
+      lo[n] = (_Float16)(wt[n] - (float)hi[n]);
+    }
+    w[j][0] = f16x8{hi[0], hi[4], hi[1], hi[5], hi[2], hi[6], hi[3], hi[7]};
+    if constexpr (HW == 2) w[j][1] = f16x8{lo[0], lo[4], lo[1], lo[5], lo[2], lo[6], lo[3], lo[7]};
+  }
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    const uint32_t* vw = reinterpret_cast<const uint32_t*>(&b.v[i >> 2]);
+    const f16x8 vc = codes8(vw[i & 3]);
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+#pragma unroll
+      for (int h = HW - 1; h >= 0; --h) s->o[j][i] = mfma(vc, w[j][h], s->o[j][i]);
+    }
+  }
+}
+
+// Columns over keys first, first + stride, ... (blocks of 32) below `hi`.
+template <int D, int NQ, int HQ, int HW>
+__device__ __forceinline__ void columns(const AttendArgs& a, const Queries<D, NQ, HQ>& q, Sums<D, NQ>* s, int seq, const Seq& sq, int kvh,
+                                        int first_place, int key, int stride, int hi, int lane) {
+  const int pt = a.c.page_tokens;
+  const int64_t head_at = (int64_t)kvh * pt * (D + 8);
+  Block<D> cur, nxt;
+  const uint8_t* page = key < hi ? page_of(a.c, a.b, seq, key) : nullptr;
+  load_block<D>(&cur, (page ? page : a.c.pages) + head_at, pt, key & (pt - 1), lane);
+  while (key < hi) {
+    const int next = key + stride;
+    const uint8_t* np = next < hi ? page_of(a.c, a.b, seq, next) : nullptr;
+    load_block<D>(&nxt, (np ? np : a.c.pages) + head_at, pt, next & (pt - 1), lane);
+    if (page) {
+      const bool whole = key + kBlockTok <= hi && (!a.causal || (key + kBlockTok - 1 <= first_place && !a.window));
+      if (whole) step<D, NQ, HQ, HW, false>(cur, q, s, key, hi, 0, lane);
+      else step<D, NQ, HQ, HW, true>(cur, q, s, key, hi, a.window, lane);
+    }
+    cur = nxt;
+    page = np;
+    key = next;
+  }
+}
+
+template <int D, int NQ>
+__device__ __forceinline__ void clear(Sums<D, NQ>* s) {
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    s->l[j] = s->z[j] = 0.f;
+    s->ref[j] = kNoRef;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) s->o[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+}
+// Joins a column's lanes: afterwards l is the whole sum and o has the z of its column added.
+template <int D, int NQ>
+__device__ __forceinline__ void join_lanes(Sums<D, NQ>* s) {
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    s->l[j] += __shfl_xor(s->l[j], 16);
+    s->l[j] += __shfl_xor(s->l[j], 32);
+    s->z[j] += __shfl_xor(s->z[j], 16);
+    s->z[j] += __shfl_xor(s->z[j], 32);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) s->o[j][i] += s->z[j];
+  }
+}
+
+// Channels c .. c+7 of a row: to out, or to the part's place in the workspace.
+template <int DT, int D>
+__device__ __forceinline__ void put8(const AttendArgs& a, bool to_out, int part, int tok, int h, int c, const float* o, float ref, float l) {
+  if (to_out) {
+    float f[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f[k] = l > 0.f || l != l ? o[k] / l : 0.f;
+    st8<DT>(a.out.p + tok * a.out.ts + h * a.out.hs + c * Elt<DT>::B, f);
+  } else {
+    const int64_t row = ((int64_t)part * a.b.n_tokens + tok) * a.heads + h;
+    float* p = a.part_o + row * D + c;
+    reinterpret_cast<float4*>(p)[0] = make_float4(o[0], o[1], o[2], o[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(o[4], o[5], o[6], o[7]);
+    if (c == 0) reinterpret_cast<float2*>(a.part_ml)[row] = make_float2(ref, l);
+  }
+}
+
+// How many parts the keys [lo, hi) are cut into, and where part k lies.
+__device__ __forceinline__ int parts_of(const AttendArgs& a, int lo, int hi) {
+  const int n = (hi - lo + a.part_keys - 1) / a.part_keys;
+  return n < 1 ? 1 : (n > a.parts ? a.parts : n);
+}
+
+// Sequences with few rows: one tile of up to 16 rows, which the four wavefronts share, each with every fourth block of the
+// part's keys.
+template <int DT, int D>
+__global__ __launch_bounds__(kThreads) void k_attend_few(AttendArgs a) {
+  __shared__ float so[kWaves][16][D + 4];
+  __shared__ float sm[kWaves][16], sl[kWaves][16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int seq = blockIdx.x / a.c.heads, kvh = blockIdx.x - seq * a.c.heads, part = blockIdx.y;
+  const Seq sq = seq_at(a.b, seq);
+  const int rows = sq.n * a.rep;
+  if (rows == 0 || rows > kFewRows) return;
+  int lo, hi;
+  keys_of_rows(sq, a, 0, rows, &lo, &hi);
+  const int n_parts = parts_of(a, lo, hi);
+  if (part >= n_parts) return;
+  const int from = lo + part * a.part_keys;
+  const int to = part == n_parts - 1 ? hi : from + a.part_keys;
+  constexpr int HQ = DT == PLORA_BF16 ? 1 : 2, HW = DT == PLORA_F32 ? 2 : 1;
+  Queries<D, 1, HQ> q;
+  load_queries<DT, D, 1, HQ>(&q, a, sq, kvh, 0, rows, lane);
+  Sums<D, 1> s;
+  clear(&s);
+  columns<D, 1, HQ, HW>(a, q, &s, seq, sq, kvh, sq.len - sq.n, from + wave * kBlockTok, kWaves * kBlockTok, to, lane);
+  join_lanes(&s);
+  const int r = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(&so[wave][r][g * (D / 4) + 4 * i]) = s.o[0][i];
+  if (g == 0) {
+    sm[wave][r] = s.ref[0];
+    sl[wave][r] = s.l[0];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * (D / 8); i += kThreads) {
+    const int row = i / (D / 8), c = (i - row * (D / 8)) * 8;
+    float ref = sm[0][row];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) ref = fmaxf(ref, sm[w][row]);
+    float l = 0.f, o[8] = {};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(sm[w][row] - ref);
+      l = __builtin_fmaf(f, sl[w][row], l);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o[k] = __builtin_fmaf(f, so[w][row][c + k], o[k]);
+    }
+    const int t = row / a.rep;
+    put8<DT, D>(a, n_parts == 1, part, sq.first + t, kvh * a.rep + row - t * a.rep, c, o, ref, l);
+  }
+}
+
+// Sequences with more rows: a wavefront has a tile of 16 * NQ rows of its own, and all keys of the part.
+template <int DT, int D, int NQ, int HQ>
+__global__ __launch_bounds__(kThreads) void k_attend_many(AttendArgs a) {
+  constexpr int R = 16 * NQ;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int64_t group = blockIdx.x / a.c.heads;
+  const int kvh = (int)(blockIdx.x - group * a.c.heads), part = blockIdx.y;
+  const int64_t number = group * kWaves + wave;
+  const int seq = find_seq(a.b, number, a.rep, R, 1);
+  const Seq sq = seq_at(a.b, seq);
+  const int rows = sq.n * a.rep;
+  if (rows <= kFewRows && a.few) return;
+  const int64_t tile = number - first_number(a.b, seq, a.rep, R, 1);
+  if (tile < 0 || tile * R >= rows) return;
+  const int r0 = (int)tile * R, r1 = r0 + R < rows ? r0 + R : rows;
+  int lo, hi;
+  keys_of_rows(sq, a, r0, r1, &lo, &hi);
+  const int n_parts = parts_of(a, lo, hi);
+  if (part >= n_parts) return;
+  const int from = lo + part * a.part_keys;
+  const int to = part == n_parts - 1 ? hi : from + a.part_keys;
+  constexpr int HW = DT == PLORA_F32 ? 2 : 1;
+  Queries<D, NQ, HQ> q;
+  load_queries<DT, D, NQ, HQ>(&q, a, sq, kvh, r0, rows, lane);
+  Sums<D, NQ> s;
+  clear(&s);
+  columns<D, NQ, HQ, HW>(a, q, &s, seq, sq, kvh, sq.len - sq.n + r0 / a.rep, from, kBlockTok, to, lane);
+  join_lanes(&s);
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    const int row = r0 + 16 * j + (lane & 15);
+    if (row >= r1) continue;
+    const int t = row / a.rep, h = kvh * a.rep + row - t * a.rep;
+#pragma unroll
+    for (int i = 0; i < D / 16; i += 2) {
+      const float o[8] = {s.o[j][i][0], s.o[j][i][1], s.o[j][i][2], s.o[j][i][3], s.o[j][i + 1][0], s.o[j][i + 1][1], s.o[j][i + 1][2], s.o[j][i + 1][3]};
+      put8<DT, D>(a, n_parts == 1, part, sq.first + t, h, (lane >> 4) * (D / 4) + 4 * i, o, s.ref[j], s.l[j]);
+    }
+  }
+}
+
+// Joins the parts of a row, in their order: D/8 threads a row.  R: rows of a tile of k_attend_many.
+template <int DT, int D, int R>
+__global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
+  constexpr int T = D / 8;
+  const int64_t row = (int64_t)blockIdx.x * (kThreads / T) + threadIdx.x / T;
+  const int c = (threadIdx.x % T) * 8;
+  const int64_t first_row = (int64_t)blockIdx.x * (kThreads / T);
+  if (first_row >= (int64_t)a.b.n_tokens * a.heads) return;
+  // the sequence of the row: those of a workgroup's first and last row bracket it
+  int tok = (int)(row / a.heads);
+  const bool has = tok < a.b.n_tokens;
+  tok = has ? tok : a.b.n_tokens - 1;
+  int seq = find_seq(a.b, first_row / a.heads, 1, 1, 0);
+  while (seq + 1 < a.b.n_seqs && hold(a.b.tok_start[seq + 1], a.b.n_tokens) <= tok) ++seq;
+  const Seq sq = seq_at(a.b, seq);
+  const int t = tok - sq.first, h = (int)(row - (int64_t)tok * a.heads);
+  if (!has || t < 0 || t >= sq.n) return;
+  const int kvh_row = t * a.rep + h % a.rep, rows = sq.n * a.rep;
+  const int r0 = rows <= kFewRows ? 0 : kvh_row / R * R, r1 = rows <= kFewRows ? rows : (r0 + R < rows ? r0 + R : rows);
+  int lo, hi;
+  keys_of_rows(sq, a, r0, r1, &lo, &hi);
+  const int n = parts_of(a, lo, hi);
+  if (n == 1) return;
+  const int64_t at = (int64_t)tok * a.heads + h, all = (int64_t)a.b.n_tokens * a.heads;
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
+  float ref = kNoRef;
+  for (int k = 0; k < n; ++k) ref = fmaxf(ref, ml[k * all + at].x);
+  float l = 0.f, o[8] = {};
+  for (int k = 0; k < n; ++k) {
+    const float2 m = ml[k * all + at];
+    const float f = __builtin_amdgcn_exp2f(m.x - ref);
+    const float4* p = reinterpret_cast<const float4*>(a.part_o + (k * all + at) * D + c);
+    const float4 u = p[0], v = p[1];
+    const float e[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+    l = __builtin_fmaf(f, m.y, l);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = __builtin_fmaf(f, e[i], o[i]);
+  }
+  put8<DT, D>(a, true, 0, tok, h, c, o, ref, l);
+}
+
+// ---- host side ----------------------------------------------------------------------------------------
+
+template <class A>
+int launch(void (*kernel)(A), uint64_t gx, unsigned gy, unsigned gz, const A& args, plora_stream stream) {
+  if (gx == 0 || gx * kThreads >= ((uint64_t)1 << 32) || gy > 65535) return PLORA_ERR_LIMIT;
+  A copy = args;
+  void* p[] = {&copy};
+  const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)gx, gy, gz), dim3(kThreads), p, 0, (hipStream_t)stream);
+  if (e == hipSuccess) return PLORA_OK;
+  plora::g_last_hip = (int)e;
+  (void)hipGetLastError();
+  return PLORA_ERR_HIP;
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+int elt_bytes(int dtype) { return dtype == PLORA_F32 ? 4 : 2; }
+bool good_dtype(int dtype) { return dtype == PLORA_F16 || dtype == PLORA_BF16 || dtype == PLORA_F32; }
+
+bool good_rotary(const plora_rotary* r, int head_dim) {
+  return r->table && aligned16(r->table) && r->max_pos >= 1 && r->rot_dim >= 2 && r->rot_dim % 2 == 0 && r->rot_dim <= head_dim &&
+         (r->interleaved == 0 || r->interleaved == 1);
+}
+Rotary device_rotary(const plora_rotary* r) { return r ? Rotary{r->table, r->max_pos, r->rot_dim, r->interleaved} : Rotary{nullptr, 0, 0, 0}; }
+
+bool good_rows(const plora_rows* r, int dtype) {
+  const int64_t mask = 16 / elt_bytes(dtype) - 1, most = (int64_t)1 << 40;
+  return r && r->data && aligned16(r->data) && (r->token_stride & mask) == 0 && (r->head_stride & mask) == 0 && r->token_stride >= 0 &&
+         r->head_stride >= 0 && r->token_stride <= most && r->head_stride <= most;
+}
+// Rows that are written: none overlaps another if one of the strides steps over all rows along the other.
+bool good_output(const plora_rows* r, int dtype, int64_t tokens, int64_t heads, int64_t dim) {
+  if (!good_rows(r, dtype)) return false;
+  const int64_t t = r->token_stride, h = r->head_stride;
+  const bool by_token = (heads == 1 || h >= dim) && (tokens == 1 || t >= (heads == 1 ? (__int128)dim : (__int128)(heads - 1) * h + dim));
+  const bool by_head = (tokens == 1 || t >= dim) && (heads == 1 || h >= (tokens == 1 ? (__int128)dim : (__int128)(tokens - 1) * t + dim));
+  return by_token || by_head;
+}
+Rows device_rows(const plora_rows* r, int dtype) {
+  return Rows{(uint8_t*)r->data, r->token_stride * elt_bytes(dtype), r->head_stride * elt_bytes(dtype)};
+}
+
+bool good_cache(const plora_kv_cache* c) {
+  return c && good_dtype(c->dtype) && c->n_kv_heads >= 1 && c->n_kv_heads <= 1024 && (c->head_dim == 64 || c->head_dim == 128 || c->head_dim == 256) &&
+         (c->page_tokens == 32 || c->page_tokens == 64 || c->page_tokens == 128 || c->page_tokens == 256);
+}
+int check(const plora_kv_cache* c, const plora_kv_batch* b) {
+  if (!good_cache(c) || c->n_pages < 1 || !c->pages || !aligned16(c->pages)) return PLORA_ERR_INVAL;
+  if (!b || b->n_seqs < 0 || b->n_tokens < 0 || b->max_new < 1 || b->max_len < 1 || b->table_stride < 1) return PLORA_ERR_INVAL;
+  if (b->n_seqs && b->n_tokens && (!b->tok_start || !b->kv_len || !b->page_table)) return PLORA_ERR_INVAL;
+  return PLORA_OK;
+}
+Cache device_cache(const plora_kv_cache* c) {
+  int shift = 5;
+  while ((1 << shift) < c->page_tokens) ++shift;
+  return Cache{(uint8_t*)c->pages, (int64_t)plora_kv_page_bytes(c), c->n_pages, c->n_kv_heads, c->page_tokens, shift};
+}
+Batch device_batch(const plora_kv_cache* c, const plora_kv_batch* b) {
+  const int64_t covered = (int64_t)b->table_stride * c->page_tokens;
+  return Batch{b->tok_start, b->kv_len, b->page_table, b->positions, b->n_seqs, b->n_tokens, (int32_t)(covered < b->max_len ? covered : b->max_len), b->table_stride};
+}
+
+template <int DT>
+int rotate(const RotateArgs& a, bool vector, plora_stream stream) {
+  const uint64_t grid = (uint64_t)(a.n_units + kThreads - 1) / kThreads;
+  return vector ? launch(k_rotate<DT, true>, grid, 1, 1, a, stream) : launch(k_rotate<DT, false>, grid, 1, 1, a, stream);
+}
+
+template <int DT, int D>
+int append_or_read(const CacheArgs& a, bool read, plora_stream stream) {
+  const uint64_t blocks = (uint64_t)a.b.n_tokens / kBlockTok + 2 * (uint64_t)a.b.n_seqs;
+  return launch(read ? k_read<DT, D> : k_append<DT, D>, blocks, (unsigned)a.c.heads, 2, a, stream);
+}
+template <int DT>
+int append_or_read(int head_dim, const CacheArgs& a, bool read, plora_stream stream) {
+  return head_dim == 64 ? append_or_read<DT, 64>(a, read, stream) : head_dim == 128 ? append_or_read<DT, 128>(a, read, stream) : append_or_read<DT, 256>(a, read, stream);
+}
+int append_or_read(int dtype, int head_dim, const CacheArgs& a, bool read, plora_stream stream) {
+  return dtype == PLORA_BF16 ? append_or_read<PLORA_BF16>(head_dim, a, read, stream)
+         : dtype == PLORA_F16 ? append_or_read<PLORA_F16>(head_dim, a, read, stream) : append_or_read<PLORA_F32>(head_dim, a, read, stream);
+}
+
+// Columns of a wavefront of k_attend_many.
+template <int DT, int D> constexpr int columns_of() { return DT == PLORA_F32 || D == 256 ? 1 : 2; }
+
+template <int DT, int D>
+int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace, plora_stream stream) {
+  constexpr int NQ = columns_of<DT, D>(), R = 16 * NQ;
+  const int64_t rows = (int64_t)a.b.n_tokens * a.heads;
+  if (max_new > a.b.n_tokens) max_new = a.b.n_tokens;
+  const int64_t most_rows = (int64_t)max_new * a.rep;
+  const bool some_few = a.b.n_seqs > 1 || most_rows <= kFewRows, some_many = most_rows > kFewRows;
+  const uint64_t few = some_few ? (uint64_t)a.b.n_seqs * a.c.heads : 0;
+  const uint64_t groups = ((uint64_t)a.b.n_tokens * a.rep / R + a.b.n_seqs + kWaves - 1) / kWaves;
+  const uint64_t many = some_many ? groups * a.c.heads : 0;
+  // parts: as many as keep the GPU's 1024 SIMDs in work, no shorter than 256 keys
+  const uint64_t fit = workspace ? workspace_bytes / ((uint64_t)rows * (D + 2) * 4) : 0;
+  const int64_t keys = a.window ? (a.b.max_len < a.window + (int64_t)max_new + kKeyAlign ? a.b.max_len : a.window + (int64_t)max_new + kKeyAlign) : a.b.max_len;
+  uint64_t want = (2048 + (some_many ? many : few) - 1) / (some_many ? many : few);
+  const uint64_t most = (uint64_t)(keys + 255) / 256;
+  if (want > most) want = most;
+  if (want > fit) want = fit;
+  if (want > 4096) want = 4096;
+  a.parts = want < 2 ? 1 : (int)want;
+  a.part_keys = (int)(((keys + a.parts - 1) / a.parts + kKeyAlign - 1) / kKeyAlign * kKeyAlign);
+  a.part_o = (float*)workspace;
+  a.part_ml = a.part_o + (int64_t)a.parts * rows * D;
+  a.few = some_few;
+  int rc = PLORA_OK;
+  if (few) rc = launch(k_attend_few<DT, D>, few, (unsigned)a.parts, 1, a, stream);
+  if (rc == PLORA_OK && many) {
+    // a rotated row of 16-bit elements needs more than the 11 bits of one half to be as good as its elements were; the 8 of bf16 do not
+    if (DT == PLORA_F32 || (DT == PLORA_F16 && a.r.table)) rc = launch(k_attend_many<DT, D, NQ, 2>, many, (unsigned)a.parts, 1, a, stream);
+    else rc = launch(k_attend_many<DT, D, NQ, DT == PLORA_F32 ? 2 : 1>, many, (unsigned)a.parts, 1, a, stream);
+  }
+  if (rc == PLORA_OK && a.parts > 1) rc = launch(k_attend_join<DT, D, R>, (uint64_t)(rows + kThreads / (D / 8) - 1) / (kThreads / (D / 8)), 1, 1, a, stream);
+  return rc;
+}
+template <int DT>
+int attend(int head_dim, const AttendArgs& a, int max_new, uint64_t bytes, void* ws, plora_stream stream) {
+  return head_dim == 64 ? attend<DT, 64>(a, max_new, bytes, ws, stream) : head_dim == 128 ? attend<DT, 128>(a, max_new, bytes, ws, stream) : attend<DT, 256>(a, max_new, bytes, ws, stream);
+}
+
+}  // namespace
+
+extern "C" int plora_rotary_table(const plora_rotary_config* cfg, int32_t rot_dim, int32_t max_pos, float* table, plora_stream stream) {
+  if (!cfg || rot_dim < 2 || rot_dim > 512 || rot_dim % 2 || max_pos < 1 || !table || !aligned16(table)) return PLORA_ERR_INVAL;
+  if (!(cfg->base > 0) || !isfinite(cfg->base) || !isfinite(cfg->magnitude)) return PLORA_ERR_INVAL;
+  const int s = cfg->scaling;
+  if (s < PLORA_ROTARY_NONE || s > PLORA_ROTARY_TURNS) return PLORA_ERR_INVAL;
+  if (s != PLORA_ROTARY_NONE && (!(cfg->factor >= 1) || !isfinite(cfg->factor))) return PLORA_ERR_INVAL;
+  if (s == PLORA_ROTARY_NTK && rot_dim == 2) return PLORA_ERR_INVAL;
+  if (s == PLORA_ROTARY_TURNS && (cfg->original_len < 1 || !(cfg->low >= 0) || !(cfg->high > cfg->low) || !isfinite(cfg->high))) return PLORA_ERR_INVAL;
+  TableArgs a;
+  a.table = table;
+  a.max_pos = max_pos;
+  a.half = rot_dim / 2;
+  a.magnitude = cfg->magnitude;
+  const double base = s == PLORA_ROTARY_NTK ? cfg->base * pow(cfg->factor, (double)rot_dim / (rot_dim - 2)) : cfg->base;
+  for (int j = 0; j < a.half; ++j) {
+    const double f = pow(base, -2.0 * j / rot_dim);
+    if (s == PLORA_ROTARY_LINEAR) a.f[j] = f / cfg->factor;
+    else if (s == PLORA_ROTARY_TURNS) {
+      const double r = cfg->original_len * f / (2 * M_PI);
+      const double u = r <= cfg->low ? 0 : r >= cfg->high ? 1 : (r - cfg->low) / (cfg->high - cfg->low);
+      a.f[j] = (1 - u) * f / cfg->factor + u * f;
+    } else a.f[j] = f;
+  }
+  for (int j = a.half; j < 256; ++j) a.f[j] = 0;
+  const uint64_t want = ((uint64_t)max_pos * a.half + kThreads - 1) / kThreads;
+  return launch(k_rotary_table, want < 8192 ? want : 8192, 1, 1, a, stream);
+}
+
+extern "C" int plora_rotate(const plora_rotary* rotary, int32_t dtype, int32_t n_tokens, int32_t n_heads, int32_t head_dim,
+                            const int32_t* positions, const plora_rows* x, const plora_rows* y, int32_t inverse, plora_stream stream) {
+  if (!rotary || !good_dtype(dtype) || n_tokens < 0 || n_heads < 1 || head_dim < 8 || head_dim > 1024 || head_dim % 8 || !good_rotary(rotary, head_dim))
+    return PLORA_ERR_INVAL;
+  if (n_tokens == 0) return PLORA_OK;
+  if (!positions || !good_rows(x, dtype) || !good_output(y, dtype, n_tokens, n_heads, head_dim)) return PLORA_ERR_INVAL;
+  const bool in_place = x->data == y->data;
+  if (in_place && (x->token_stride != y->token_stride || x->head_stride != y->head_stride)) return PLORA_ERR_INVAL;
+  const Rows xr = device_rows(x, dtype), yr = device_rows(y, dtype);
+  RotateArgs a;
+  a.r = device_rotary(rotary);
+  a.positions = positions;
+  a.x = xr.p;
+  a.y = yr.p;
+  a.xt = xr.ts;
+  a.xh = xr.hs;
+  a.yt = yr.ts;
+  a.yh = yr.hs;
+  a.heads = n_heads;
+  a.head_dim = head_dim;
+  a.sign = inverse ? -1.f : 1.f;
+  // groups of 8 channels where no pair and no copied channel shares a group with another kind
+  const bool vector = rotary->rot_dim % (rotary->interleaved ? 8 : 16) == 0;
+  a.pair_units = vector ? rotary->rot_dim / (rotary->interleaved ? 8 : 16) : rotary->rot_dim / 2;
+  a.units = a.pair_units + (in_place ? 0 : (head_dim - rotary->rot_dim) / (vector ? 8 : 1));
+  a.n_units = (int64_t)n_tokens * n_heads * a.units;
+  return dtype == PLORA_BF16 ? rotate<PLORA_BF16>(a, vector, stream) : dtype == PLORA_F16 ? rotate<PLORA_F16>(a, vector, stream) : rotate<PLORA_F32>(a, vector, stream);
+}
+
+extern "C" uint64_t plora_kv_page_bytes(const plora_kv_cache* c) {
+  return good_cache(c) ? (uint64_t)c->n_kv_heads * c->page_tokens * (c->head_dim + 8) : 0;
+}
+
+extern "C" int plora_kv_append(const plora_kv_cache* cache, const plora_kv_batch* batch, const plora_rows* k, const plora_rows* v,
+                               const plora_rotary* rotary, plora_stream stream) {
+  const int rc = check(cache, batch);
+  if (rc) return rc;
+  if (rotary && !good_rotary(rotary, cache->head_dim)) return PLORA_ERR_INVAL;
+  if (batch->n_tokens == 0 || batch->n_seqs == 0) return PLORA_OK;
+  if (!good_rows(k, cache->dtype) || !good_rows(v, cache->dtype)) return PLORA_ERR_INVAL;
+  const CacheArgs a{device_cache(cache), device_batch(cache, batch), device_rows(k, cache->dtype), device_rows(v, cache->dtype), device_rotary(rotary)};
+  return append_or_read(cache->dtype, cache->head_dim, a, false, stream);
+}
+
+extern "C" int plora_kv_read(const plora_kv_cache* cache, const plora_kv_batch* batch, const plora_rows* k, const plora_rows* v, plora_stream stream) {
+  const int rc = check(cache, batch);
+  if (rc) return rc;
+  if (batch->n_tokens == 0 || batch->n_seqs == 0) return PLORA_OK;
+  if (!good_output(k, cache->dtype, batch->n_tokens, cache->n_kv_heads, cache->head_dim) ||
+      !good_output(v, cache->dtype, batch->n_tokens, cache->n_kv_heads, cache->head_dim))
+    return PLORA_ERR_INVAL;
+  const CacheArgs a{device_cache(cache), device_batch(cache, batch), device_rows(k, cache->dtype), device_rows(v, cache->dtype), device_rotary(nullptr)};
+  return append_or_read(cache->dtype, cache->head_dim, a, true, stream);
+}
+
+extern "C" int plora_kv_attend(const plora_kv_cache* cache, const plora_kv_batch* batch, int32_t n_heads, const plora_rows* q, const plora_rows* out,
+                               float scale, int32_t causal, int32_t window, const plora_rotary* rotary, void* workspace, uint64_t workspace_bytes,
+                               plora_stream stream) {
+  const int rc = check(cache, batch);
+  if (rc) return rc;
+  if (n_heads < 1 || n_heads > 65536 || n_heads % cache->n_kv_heads || !(scale > 0.f) || !isfinite(scale) || window < 0 || (window && !causal) ||
+      (rotary && !good_rotary(rotary, cache->head_dim)) || (workspace && !aligned16(workspace)) || (!workspace && workspace_bytes))
+    return PLORA_ERR_INVAL;
+  if (batch->n_tokens == 0 || batch->n_seqs == 0) return PLORA_OK;
+  if (!good_rows(q, cache->dtype) || !good_output(out, cache->dtype, batch->n_tokens, n_heads, cache->head_dim)) return PLORA_ERR_INVAL;
+  if ((int64_t)batch->n_tokens * (n_heads / cache->n_kv_heads) > 0x7fffffff) return PLORA_ERR_LIMIT;
+  AttendArgs a;
+  a.c = device_cache(cache);
+  a.b = device_batch(cache, batch);
+  a.q = device_rows(q, cache->dtype);
+  a.out = device_rows(out, cache->dtype);
+  a.r = device_rotary(rotary);
+  a.heads = n_heads;
+  a.rep = n_heads / cache->n_kv_heads;
+  a.scale = scale * 1.44269504088896341f;
+  a.causal = causal != 0;
+  a.window = window;
+  return cache->dtype == PLORA_BF16  ? attend<PLORA_BF16>(cache->head_dim, a, batch->max_new, workspace_bytes, workspace, stream)
+         : cache->dtype == PLORA_F16 ? attend<PLORA_F16>(cache->head_dim, a, batch->max_new, workspace_bytes, workspace, stream)
+                                     : attend<PLORA_F32>(cache->head_dim, a, batch->max_new, workspace_bytes, workspace, stream);
+}

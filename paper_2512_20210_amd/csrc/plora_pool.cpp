@@ -11,9 +11,11 @@
 #include <string>
 #include <vector>
 
+namespace plora {
+extern thread_local int g_last_hip;
+thread_local int g_last_hip = 0;  // what plora_last_hip reports; plora_kv.hip sets it too
+}
 using namespace plora;
-
-static thread_local int g_last_hip = 0;
 
 #define HIP_TRY(expr)                                   \
   do {                                                  \
