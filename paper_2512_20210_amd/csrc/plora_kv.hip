@@ -91,13 +91,18 @@ struct Rotary {
   int32_t max_pos, rot, interleaved;
 };
 
-// cos and sin of pair j at the position whose table row is cs (NULL: the position has none).
-__device__ __forceinline__ float2 angle(const float* cs, int j) {
-  if (!cs) return make_float2(__builtin_nanf(""), __builtin_nanf(""));
-  return reinterpret_cast<const float2*>(cs)[j];
-}
-__device__ __forceinline__ const float* angles_at(const Rotary& r, int32_t pos) {
-  return (uint32_t)pos < (uint32_t)r.max_pos ? r.table + (int64_t)pos * r.rot : nullptr;
+// A position's row of the table; one outside it has row 0 in its place, and `ok` false: its angles are NaN.
+struct Angles {
+  const float2* cs;
+  bool ok;
+  __device__ __forceinline__ float2 operator[](int j) const {
+    const float2 w = cs[j];
+    return make_float2(ok ? w.x : __builtin_nanf(""), ok ? w.y : __builtin_nanf(""));
+  }
+};
+__device__ __forceinline__ Angles angles_at(const Rotary& r, int32_t pos) {
+  const bool ok = (uint32_t)pos < (uint32_t)r.max_pos;
+  return Angles{reinterpret_cast<const float2*>(r.table + (int64_t)(ok ? pos : 0) * r.rot), ok};
 }
 // First and second member of a rotated pair; every product and sum is rounded by itself, so the same pair gives the same
 // bits wherever it is computed.
@@ -113,14 +118,14 @@ __device__ __forceinline__ float turn_b(float a, float b, float2 cs) {
 // Channels c0 .. c0+7 of a row (c0 a multiple of 8), rotated.  The partners of a half-split rotation are read along: a second
 // trip to lines that the neighbouring lanes read anyway.
 template <int DT>
-__device__ __forceinline__ void rotated8(const uint8_t* row, int c0, const Rotary& r, const float* cs, float* f) {
+__device__ __forceinline__ void rotated8(const uint8_t* row, int c0, const Rotary& r, const Angles& cs, float* f) {
   ld8<DT>(row + (int64_t)c0 * Elt<DT>::B, f);
   if (!r.table || c0 >= r.rot) return;
   const int half = r.rot >> 1;
   if (r.interleaved && (r.rot & 7) == 0) {
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-      const float2 w = angle(cs, (c0 + i) >> 1);
+      const float2 w = cs[(c0 + i) >> 1];
       const float a = f[i], b = f[i + 1];
       f[i] = turn_a(a, b, w);
       f[i + 1] = turn_b(a, b, w);
@@ -132,7 +137,7 @@ __device__ __forceinline__ void rotated8(const uint8_t* row, int c0, const Rotar
     ld8<DT>(row + (int64_t)(second ? j0 : c0 + half) * Elt<DT>::B, o);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float2 w = angle(cs, j0 + i);
+      const float2 w = cs[j0 + i];
       f[i] = second ? turn_b(o[i], f[i], w) : turn_a(f[i], o[i], w);
     }
   } else {  // pairs that cross a group of 8: element by element
@@ -142,7 +147,7 @@ __device__ __forceinline__ void rotated8(const uint8_t* row, int c0, const Rotar
       const bool second = r.interleaved ? (c & 1) : c >= half;
       const int j = r.interleaved ? c >> 1 : (second ? c - half : c);
       const int p = r.interleaved ? c ^ 1 : (second ? j : c + half);
-      const float2 w = angle(cs, j);
+      const float2 w = cs[j];
       const float o = ld1<DT>(row, p);
       const float me = ld1<DT>(row, c);
       const float v = second ? turn_b(o, me, w) : turn_a(me, o, w);
@@ -205,7 +210,7 @@ __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
     }
     return;
   }
-  const float* cs = angles_at(a.r, a.positions[t]);
+  const Angles cs = angles_at(a.r, a.positions[t]);
   const int half = a.r.rot >> 1;
   if constexpr (VECTOR) {
     float f[8], g[8];
@@ -213,7 +218,7 @@ __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
       ld8<DT>(x + u * 8 * B, f);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        float2 w = angle(cs, u * 4 + k);
+        float2 w = cs[u * 4 + k];
         w.y *= a.sign;
         g[2 * k] = turn_a(f[2 * k], f[2 * k + 1], w);
         g[2 * k + 1] = turn_b(f[2 * k], f[2 * k + 1], w);
@@ -224,7 +229,7 @@ __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
       ld8<DT>(x + (half + u * 8) * B, g);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        float2 w = angle(cs, u * 8 + k);
+        float2 w = cs[u * 8 + k];
         w.y *= a.sign;
         const float p = f[k], q = g[k];
         f[k] = turn_a(p, q, w);
@@ -235,7 +240,7 @@ __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
     }
   } else {
     const int ca = a.r.interleaved ? 2 * u : u, cb = a.r.interleaved ? 2 * u + 1 : u + half;
-    float2 w = angle(cs, u);
+    float2 w = cs[u];
     w.y *= a.sign;
     const float p = ld1<DT>(x, ca), q = ld1<DT>(x, cb);
     st1<DT>(y, ca, turn_a(p, q, w));
@@ -353,7 +358,8 @@ __global__ __launch_bounds__(kThreads) void k_append(CacheArgs a) {
     const uint8_t* p = src.p + tok * src.ts + head * src.hs;
     Rotary r = a.r;
     if (values) r.table = nullptr;
-    const float* cs = r.table ? angles_at(r, a.b.positions ? a.b.positions[tok] : place) : nullptr;
+    Angles cs{nullptr, false};
+    if (r.table) cs = angles_at(r, a.b.positions ? a.b.positions[tok] : place);
 #pragma unroll
     for (int i = 0; i < C; i += 8) rotated8<DT>(p, part * C + i, r, cs, x + i);
   } else {
@@ -480,7 +486,7 @@ __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
 // softmax reference per lane serves its column.
 //
 // Codes enter as fp16 numbers code - 8, exactly, and scale and min stay outside in fp32:
-//   q . K[s] = scale_s * (q . (code - 8)) + (min_s + 8 scale_s) * sum(q),
+//   q . K[s] = scale_s * (8 sum(q) + q . (code - 8)) + min_s * sum(q),
 //   sum p_s V[s] = sum (p_s scale_s)(code - 8) + sum p_s (min_s + 8 scale_s).
 // So a row of keys or values costs its codes' unpacking (9 instructions per 8 codes) and no multiplication by its scale, and what
 // lies in places that are not seen cannot hurt: codes are finite whatever the memory holds, and scale and min are dropped
@@ -502,10 +508,10 @@ struct AttendArgs {
   float scale;                 // * log2(e)
   int32_t causal, window;
   int32_t part_keys, parts;    // keys of a part (a multiple of kKeyAlign), parts at most; 1: results go to out
-  int32_t few;                 // 1: k_attend_few has the sequences with at most kFewRows rows, 0: k_attend_many has all
+  int32_t few_rows;            // k_attend_few has the sequences with at most so many rows, k_attend_many the others
   float *part_o, *part_ml;     // [part][token][head][head_dim], [part][token][head][2]: sums, (ref, weights)
 };
-constexpr int kFewRows = 16;
+constexpr int kMostFew = 16;
 
 // Keys [lo, hi) that rows r0 .. r1-1 of a sequence see, lo on a boundary of kKeyAlign.
 __device__ __forceinline__ void keys_of_rows(const Seq& s, const AttendArgs& a, int r0, int r1, int* lo, int* hi) {
@@ -518,17 +524,31 @@ __device__ __forceinline__ void keys_of_rows(const Seq& s, const AttendArgs& a, 
   }
 }
 
-// 8 codes of a word as fp16 numbers code - 8; element pairs are (0,4) (1,5) (2,6) (3,7).
-__device__ __forceinline__ f16x8 codes8(uint32_t w) {
+// 8 codes of a word as fp16 numbers code - 8; element pairs are (0,4) (1,5) (2,6) (3,7).  A nibble with fp16's bits of 1024 (or,
+// four bits further up, of 64) around it is 1024 + code (64 + code).  (The instruction that masks and sets in one is written
+// out: the compiler takes two where both constants are no inline ones.)
+struct CodeBits {
+  uint32_t low, high;  // 1024 and 64, twice each, in vector registers: an instruction takes one constant from elsewhere
+};
+__device__ __forceinline__ CodeBits code_bits() {
+  CodeBits c;
+  asm("v_mov_b32 %0, 0x64006400" : "=v"(c.low));
+  asm("v_mov_b32 %0, 0x54005400" : "=v"(c.high));
+  return c;
+}
+__device__ __forceinline__ f16x2 code_pair(uint32_t w, uint32_t mask, uint32_t bits, f16x2 less) {
+  uint32_t r;
+  asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(w), "s"(mask), "v"(bits));
+  return __builtin_bit_cast(f16x2, r) + less;
+}
+__device__ __forceinline__ f16x8 codes8(uint32_t w, const CodeBits& c) {
   const uint32_t h = w >> 8;
-  const uint32_t u[4] = {(w & 0x000f000fu) | 0x64006400u, (w & 0x00f000f0u) | 0x54005400u,   // 1024 + code, 64 + code
-                         (h & 0x000f000fu) | 0x64006400u, (h & 0x00f000f0u) | 0x54005400u};
-  const f16x2 ca = {(_Float16)-1032.f, (_Float16)-1032.f}, cb = {(_Float16)-72.f, (_Float16)-72.f};
+  const f16x2 low = {(_Float16)-1032.f, (_Float16)-1032.f}, high = {(_Float16)-72.f, (_Float16)-72.f};
   union { f16x2 p[4]; f16x8 v; } r;
-  r.p[0] = __builtin_bit_cast(f16x2, u[0]) + ca;
-  r.p[1] = __builtin_bit_cast(f16x2, u[1]) + cb;
-  r.p[2] = __builtin_bit_cast(f16x2, u[2]) + ca;
-  r.p[3] = __builtin_bit_cast(f16x2, u[3]) + cb;
+  r.p[0] = code_pair(w, 0x000f000fu, c.low, low);
+  r.p[1] = code_pair(w, 0x00f000f0u, c.high, high);
+  r.p[2] = code_pair(h, 0x000f000fu, c.low, low);
+  r.p[3] = code_pair(h, 0x00f000f0u, c.high, high);
   return r.v;
 }
 __device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -572,58 +592,82 @@ __device__ __forceinline__ void load_block(Block<D>* o, const uint8_t* hp, int p
   }
 }
 
-// Query rows of 16 * NQ columns: the lane's columns are r0 + 16 j + lane%16, and of these the channels (lane/16) * D/4 ..
-template <int D, int NQ, int HQ>
-struct Queries {
-  f16x8 q[NQ][HQ][D / 32];  // HQ = 2: a high and a low half
-  float sum[NQ];   // of the scaled row
-  float f[NQ];     // scale * log2(e) / the row's power of two
-  int place[NQ];   // last place that the column sees
+// Query rows in LDS: fp16 numbers (a high and a low half if HQ = 2) of a row times its power of two, in the order in which codes8
+// has its elements, with 16 bytes between the rows so that 16 rows' pieces lie in different banks.
+template <int D, int HQ, int R>
+struct QueryRows {
+  uint4 q[HQ][R][D / 8 + 1];
+  float sum[R];  // of the scaled row
+  float f[R];    // scale * log2(e) / the row's power of two
 };
-
-template <int DT, int D, int NQ, int HQ>
-__device__ __forceinline__ void load_queries(Queries<D, NQ, HQ>* o, const AttendArgs& a, const Seq& s, int kvh, int r0, int rows, int lane) {
-  const int g = lane >> 4;
-#pragma unroll
-  for (int j = 0; j < NQ; ++j) {
-    const int row = r0 + 16 * j + (lane & 15);
-    const int rr = row < rows ? row : rows - 1;
+// `threads` threads (whole wavefronts, or half of one) stage rows r0 .. r0 + R-1 of a sequence; behind the last row, that one again.
+template <int DT, int D, int HQ, int R>
+__device__ __forceinline__ void stage_queries(QueryRows<D, HQ, R>* o, const AttendArgs& a, const Seq& s, int kvh, int r0, int rows, int thread, int threads) {
+  constexpr int T = D / 8;  // threads of a row
+  for (int i = thread; i < R * T; i += threads) {
+    const int row = i / T, part = i - row * T;
+    const int rr = r0 + row < rows ? r0 + row : rows - 1;
     const int t = rr / a.rep, h = kvh * a.rep + rr - t * a.rep, tok = s.first + t;
-    o->place[j] = a.causal ? s.len - s.n + t : 0x7fffffff;
-    const uint8_t* p = a.q.p + tok * a.q.ts + h * a.q.hs;
-    const float* cs = a.r.table ? angles_at(a.r, a.b.positions ? a.b.positions[tok] : s.len - s.n + t) : nullptr;
-    float x[D / 4];
+    Angles cs{nullptr, false};
+    if (a.r.table) cs = angles_at(a.r, a.b.positions ? a.b.positions[tok] : s.len - s.n + t);
+    float x[8];
+    rotated8<DT>(a.q.p + tok * a.q.ts + h * a.q.hs, part * 8, a.r, cs, x);
     float big = 0.f, sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < D / 4; i += 8) {
-      rotated8<DT>(p, g * (D / 4) + i, a.r, cs, x + i);
+    for (int k = 0; k < 8; ++k) big = fmaxf(big, fabsf(x[k]));
 #pragma unroll
-      for (int k = 0; k < 8; ++k) big = fmaxf(big, fabsf(x[i + k]));
-    }
-    big = fmaxf(big, __shfl_xor(big, 16));
-    big = fmaxf(big, __shfl_xor(big, 32));
+    for (int d = 1; d < T; d <<= 1) big = fmaxf(big, __shfl_xor(big, d));
     // 2^e with big * 2^e in [2^9, 2^10)
     int e = big > 0.f ? 9 - (int)((__float_as_uint(big) >> 23) & 255) + 127 : 0;
     e = e > 120 ? 120 : e;
     const float up = __uint_as_float((uint32_t)(e + 127) << 23);
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-      _Float16 hi[8], lo[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float y = x[8 * i + k] * up;
-        sum += y;
-        hi[k] = (_Float16)y;
-        lo[k] = (_Float16)(y - (float)hi[k]);
-      }
-      o->q[j][0][i] = f16x8{hi[0], hi[4], hi[1], hi[5], hi[2], hi[6], hi[3], hi[7]};
-      if constexpr (HQ == 2) o->q[j][1][i] = f16x8{lo[0], lo[4], lo[1], lo[5], lo[2], lo[6], lo[3], lo[7]};
+    for (int k = 0; k < 8; ++k) {
+      x[k] *= up;
+      sum += x[k];
     }
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    o->sum[j] = sum;
-    o->f[j] = a.scale * __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+    for (int d = 1; d < T; d <<= 1) sum += __shfl_xor(sum, d);
+#pragma unroll
+    for (int h2 = 0; h2 < HQ; ++h2) {
+      o->q[h2][row][part] = make_uint4(pack_f16(x[0], x[4]), pack_f16(x[1], x[5]), pack_f16(x[2], x[6]), pack_f16(x[3], x[7]));
+      if (h2 + 1 < HQ) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          asm("" : "+v"(x[k]));
+          x[k] -= (float)(_Float16)x[k];
+        }
+      }
+    }
+    if (part == 0) {
+      o->sum[row] = sum;
+      o->f[row] = a.scale * __uint_as_float((uint32_t)(127 - e) << 23);
+    }
   }
+}
+
+// What a lane holds of 16 * NQ columns: rows r0 + 16 j + lane%16, of these the channels (lane/16) * D/4 .. .
+template <int D, int NQ, int HQ>
+struct Queries {
+  f16x8 q[NQ][HQ][D / 32];
+  float sum[NQ];
+  float sum8[NQ];  // 8 sums: what code - 8 leaves out
+  float f[NQ];
+  int place[NQ];   // last place that the column sees
+};
+template <int D, int NQ, int HQ>
+__device__ __forceinline__ void take_queries(Queries<D, NQ, HQ>* o, int j, const QueryRows<D, HQ, 16>& from, const AttendArgs& a, const Seq& s, int r0, int rows, int lane) {
+  const int r = lane & 15, g = lane >> 4;
+  const int row = r0 + r < rows ? r0 + r : rows - 1;
+  o->place[j] = a.causal ? s.len - s.n + row / a.rep : 0x7fffffff;
+#pragma unroll
+  for (int h = 0; h < HQ; ++h) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) o->q[j][h][i] = __builtin_bit_cast(f16x8, from.q[h][r][g * (D / 32) + i]);
+  }
+  o->sum[j] = from.sum[r];
+  o->sum8[j] = 8.f * from.sum[r];
+  o->f[j] = from.f[r];
 }
 
 // Running sums of a column, per lane.
@@ -639,16 +683,16 @@ __device__ __forceinline__ float param_min(uint32_t p) { return __uint_as_float(
 
 // 32 keys: places key0 .. key0 + 31, of which those below `live` exist.  MASK: some column may not see some of them.
 template <int D, int NQ, int HQ, int HW, bool MASK>
-__device__ __forceinline__ void step(const Block<D>& b, const Queries<D, NQ, HQ>& q, Sums<D, NQ>* s, int key0, int live, int window, int lane) {
+__device__ __forceinline__ void step(const Block<D>& b, const Queries<D, NQ, HQ>& q, const CodeBits& bits, Sums<D, NQ>* s, int key0, int live, int window, int lane) {
   const int g = lane >> 4;
   f32x4 t[NQ][2];
 #pragma unroll
-  for (int j = 0; j < NQ; ++j) t[j][0] = t[j][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int j = 0; j < NQ; ++j) t[j][0] = t[j][1] = f32x4{q.sum8[j], q.sum8[j], q.sum8[j], q.sum8[j]};
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const f16x8 kc = codes8(b.k[u][i]);
+      const f16x8 kc = codes8(b.k[u][i], bits);
 #pragma unroll
       for (int j = 0; j < NQ; ++j) {
 #pragma unroll
@@ -665,14 +709,13 @@ __device__ __forceinline__ void step(const Block<D>& b, const Queries<D, NQ, HQ>
     float top = -INFINITY;
 #pragma unroll
     for (int n = 0; n < 8; ++n) {
-      const float sc = param_scale(kp[n]), mc = __builtin_fmaf(8.f, sc, param_min(kp[n]));
-      x[n] = __builtin_fmaf(sc, t[j][n >> 2][n & 3], mc * q.sum[j]) * q.f[j];
+      x[n] = __builtin_fmaf(param_scale(kp[n]), t[j][n >> 2][n & 3], param_min(kp[n]) * q.sum[j]);
       if constexpr (MASK) {
         const int key = key0 + 16 * (n >> 2) + 4 * g + (n & 3);
         const bool sees = key < live && key <= q.place[j] && (window == 0 || key > q.place[j] - window);
         x[n] = sees ? x[n] : -INFINITY;
       }
-      p[n] = __builtin_amdgcn_exp2f(x[n] - s->ref[j]);
+      p[n] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n], q.f[j], -s->ref[j]));
       wt[n] = p[n] * param_scale(vp[n]);
       if constexpr (MASK) wt[n] = p[n] == 0.f ? 0.f : wt[n];
       top = fmaxf(top, fmaxf(wt[n], p[n] * 0x1p-90f));
@@ -682,7 +725,7 @@ __device__ __forceinline__ void step(const Block<D>& b, const Queries<D, NQ, HQ>
 #pragma unroll
       for (int n = 0; n < 8; ++n) {
         const float m = fmaxf(fmaxf(param_scale(vp[n]), fabsf(param_min(vp[n])) * 0.125f), 0x1p-90f);
-        best = fmaxf(best, x[n] + (float)((int)(__float_as_uint(m) >> 23) - 127));
+        best = fmaxf(best, x[n] * q.f[j] + (float)((int)(__float_as_uint(m) >> 23) - 127));
       }
       best = fmaxf(best, __shfl_xor(best, 16));
       best = fmaxf(best, __shfl_xor(best, 32));
@@ -694,7 +737,7 @@ __device__ __forceinline__ void step(const Block<D>& b, const Queries<D, NQ, HQ>
       for (int i = 0; i < D / 16; ++i) s->o[j][i] *= down;
 #pragma unroll
       for (int n = 0; n < 8; ++n) {
-        p[n] = __builtin_amdgcn_exp2f(x[n] - ref);
+        p[n] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n], q.f[j], -ref));
         wt[n] = p[n] * param_scale(vp[n]);
         if constexpr (MASK) wt[n] = p[n] == 0.f ? 0.f : wt[n];
       }
@@ -718,7 +761,7 @@ __device__ __forceinline__ void step(const Block<D>& b, const Queries<D, NQ, HQ>
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
     const uint32_t* vw = reinterpret_cast<const uint32_t*>(&b.v[i >> 2]);
-    const f16x8 vc = codes8(vw[i & 3]);
+    const f16x8 vc = codes8(vw[i & 3], bits);
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
 #pragma unroll
@@ -734,6 +777,7 @@ __device__ __forceinline__ void columns(const AttendArgs& a, const Queries<D, NQ
   const int pt = a.c.page_tokens;
   const int64_t head_at = (int64_t)kvh * pt * (D + 8);
   Block<D> cur, nxt;
+  const CodeBits bits = code_bits();
   const uint8_t* page = key < hi ? page_of(a.c, a.b, seq, key) : nullptr;
   load_block<D>(&cur, (page ? page : a.c.pages) + head_at, pt, key & (pt - 1), lane);
   while (key < hi) {
@@ -742,8 +786,8 @@ __device__ __forceinline__ void columns(const AttendArgs& a, const Queries<D, NQ
     load_block<D>(&nxt, (np ? np : a.c.pages) + head_at, pt, next & (pt - 1), lane);
     if (page) {
       const bool whole = key + kBlockTok <= hi && (!a.causal || (key + kBlockTok - 1 <= first_place && !a.window));
-      if (whole) step<D, NQ, HQ, HW, false>(cur, q, s, key, hi, 0, lane);
-      else step<D, NQ, HQ, HW, true>(cur, q, s, key, hi, a.window, lane);
+      if (whole) step<D, NQ, HQ, HW, false>(cur, q, bits, s, key, hi, 0, lane);
+      else step<D, NQ, HQ, HW, true>(cur, q, bits, s, key, hi, a.window, lane);
     }
     cur = nxt;
     page = np;
@@ -798,50 +842,298 @@ __device__ __forceinline__ int parts_of(const AttendArgs& a, int lo, int hi) {
   return n < 1 ? 1 : (n > a.parts ? a.parts : n);
 }
 
-// Sequences with few rows: one tile of up to 16 rows, which the four wavefronts share, each with every fourth block of the
-// part's keys.
-template <int DT, int D>
-__global__ __launch_bounds__(kThreads) void k_attend_few(AttendArgs a) {
-  __shared__ float so[kWaves][16][D + 4];
-  __shared__ float sm[kWaves][16], sl[kWaves][16];
+// Sequences with few rows.  A tile has 16 columns and R = 4, 8 or 16 rows of the sequence, so the same row stands in 16 / R columns, and
+// each of these takes other keys: of 64 keys in 4 tiles of 16, column c has row c % R and the tiles c / R, c / R + 16 / R, ...  Every column is a
+// softmax of its own over its keys (nothing is exchanged between lanes), a lane has 4, 8 or 16 weights to compute instead
+// of 16, and the columns are joined where the wavefronts are.  The weights of keys that are other columns' are zero.
+//
+// The four wavefronts of a workgroup take every fourth 64 keys of the part.  A wavefront asks for the next keys as soon as the
+// present ones are used, and for the next values likewise, into the same registers: with three or four wavefronts on a SIMD that
+// hides memory, and a second set of registers would cost one of them.
+template <int D, int R>
+struct Keys64 {
+  static constexpr int U = R / 4;  // tiles of a column
+  uint32_t k[4][D / 32];           // words of key lane%16 of each tile
+  uint4 kp[U];                     // scale and min of keys 4g .. 4g+3 of the column's tiles
+};
+template <int D, int R>
+struct Values64 {
+  static constexpr int U = R / 4;
+  uint4 v[2][D / 64];
+  uint4 vp[U];
+};
+// Where 64 keys lie: their two blocks of 32 (NULL: a hole, or behind the last key).
+struct Place64 {
+  const uint8_t *page0, *page1;
+};
+__device__ __forceinline__ Place64 place64(const AttendArgs& a, int seq, int key, int to) {
+  Place64 p;
+  p.page0 = key < to ? page_of(a.c, a.b, seq, key) : nullptr;
+  p.page1 = key + kBlockTok < to ? page_of(a.c, a.b, seq, key + kBlockTok) : nullptr;
+  return p;
+}
+template <int D, int R>
+__device__ __forceinline__ void load_keys(Keys64<D, R>* o, const AttendArgs& a, const Place64& at, int64_t head_at, int key, int lane) {
+  const int r = lane & 15, g = lane >> 4, pt = a.c.page_tokens;
+  const uint8_t *h0 = (at.page0 ? at.page0 : a.c.pages) + head_at, *h1 = (at.page1 ? at.page1 : a.c.pages) + head_at;
+  const int slot0 = key & (pt - 1), slot1 = (key + kBlockTok) & (pt - 1);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const uint8_t* kp = (t < 2 ? h0 + slot0 * (D / 2) : h1 + slot1 * (D / 2)) + (unsigned)((16 * (t & 1) + r) * (D / 2) + g * (D / 8));
+    if constexpr (D == 64) {
+      const uint2 q = *reinterpret_cast<const uint2*>(kp);
+      o->k[t][0] = q.x;
+      o->k[t][1] = q.y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < D / 128; ++i) {
+        const uint4 q = reinterpret_cast<const uint4*>(kp)[i];
+        o->k[t][4 * i] = q.x;
+        o->k[t][4 * i + 1] = q.y;
+        o->k[t][4 * i + 2] = q.z;
+        o->k[t][4 * i + 3] = q.w;
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < Keys64<D, R>::U; ++u) {
+    const int tile = r / R + (16 / R) * u;
+    const uint8_t* h = tile & 2 ? h1 + slot1 * 4 : h0 + slot0 * 4;
+    o->kp[u] = *reinterpret_cast<const uint4*>(h + pt * D + (16 * (tile & 1) + 4 * g) * 4);
+  }
+}
+template <int D, int R>
+__device__ __forceinline__ void load_values(Values64<D, R>* o, const AttendArgs& a, const Place64& at, int64_t head_at, int key, int lane) {
+  const int r = lane & 15, g = lane >> 4, pt = a.c.page_tokens;
+  const uint8_t *h0 = (at.page0 ? at.page0 : a.c.pages) + head_at, *h1 = (at.page1 ? at.page1 : a.c.pages) + head_at;
+  const int slot0 = key & (pt - 1), slot1 = (key + kBlockTok) & (pt - 1);
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const uint8_t* vp = (b ? h1 + slot1 * (D / 2) : h0 + slot0 * (D / 2)) + pt * (D / 2);
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) o->v[b][j] = *reinterpret_cast<const uint4*>(vp + (unsigned)((j * 64 + lane) * 16));
+  }
+#pragma unroll
+  for (int u = 0; u < Values64<D, R>::U; ++u) {
+    const int tile = r / R + (16 / R) * u;
+    const uint8_t* h = tile & 2 ? h1 + slot1 * 4 : h0 + slot0 * 4;
+    o->vp[u] = *reinterpret_cast<const uint4*>(h + pt * (D + 4) + (16 * (tile & 1) + 4 * g) * 4);
+  }
+}
+
+// The row of a lane's column.
+struct Column {
+  float sum, f;
+  int place;  // last place that it sees
+};
+
+// Logits of a lane's keys, less what q.f multiplies them with.
+template <int D, int R, int HQ>
+__device__ __forceinline__ void logits64(const Keys64<D, R>& b, const QueryRows<D, HQ, R>& rows, const Column& q, const CodeBits& bits, float* x, int lane) {
+  constexpr int U = R / 4, P = 16 / R;
+  const int own = (lane & 15) / R;
+  // The row is read from LDS every time: kept in registers it would cost a wavefront of occupancy.
+  const uint4* row = &rows.q[0][(lane & 15) % R][(lane >> 4) * (D / 32)];
+  asm("" : "+v"(row));
+  f16x8 qf[HQ][D / 32];
+#pragma unroll
+  for (int h = 0; h < HQ; ++h) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) qf[h][i] = __builtin_bit_cast(f16x8, row[h * (R * (D / 8 + 1)) + i]);
+  }
+  f32x4 t[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    t[u] = f32x4{8.f * q.sum, 8.f * q.sum, 8.f * q.sum, 8.f * q.sum};
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      const f16x8 kc = codes8(b.k[u][i], bits);
+#pragma unroll
+      for (int h = HQ - 1; h >= 0; --h) t[u] = mfma(kc, qf[h][i], t[u]);
+    }
+    __builtin_amdgcn_sched_barrier(0);  // one tile's codes at a time: all at once would take 16 registers a tile
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t kp = reinterpret_cast<const uint32_t*>(&b.kp[u])[i];
+      float c = t[P * u][i];
+#pragma unroll
+      for (int j = 1; j < P; ++j) c = own == j ? t[P * u + j][i] : c;
+      x[4 * u + i] = __builtin_fmaf(param_scale(kp), c, param_min(kp) * q.sum);
+    }
+  }
+}
+
+// Keys that a lane's column does not see: a logit of minus infinity, and nothing of whatever lies where the value's scale and min are.
+template <int D, int R>
+__device__ __forceinline__ void mask64(float* x, uint4* vparams, const Column& q, const Place64& at, int key0, int live, int window, int lane) {
+  constexpr int P = 16 / R;
+  const bool there0 = at.page0 != nullptr, there1 = at.page1 != nullptr;
+  const int g = lane >> 4, own = (lane & 15) / R;
+  uint32_t* vp = reinterpret_cast<uint32_t*>(vparams);
+#pragma unroll
+  for (int n = 0; n < R; ++n) {
+    const int tile = own + P * (n >> 2), key = key0 + 16 * tile + 4 * g + (n & 3);
+    const bool sees = key < live && key <= q.place && (window == 0 || key > q.place - window) && (tile & 2 ? there1 : there0);
+    x[n] = sees ? x[n] : -INFINITY;
+    vp[n] = sees ? vp[n] : 0u;
+  }
+}
+
+// Weights of a lane's keys, into the sums but for the values; w: times the values' scale.
+template <int D, int R>
+__device__ __forceinline__ void weights64(const uint4* vparams, const Column& q, Sums<D, 1>* s, const float* x, float* w) {
+  const uint32_t* vp = reinterpret_cast<const uint32_t*>(vparams);
+  float p[R];
+  float top = 0.f;
+#pragma unroll
+  for (int n = 0; n < R; ++n) {
+    p[n] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n], q.f, -s->ref[0]));
+    w[n] = p[n] * param_scale(vp[n]);
+    top = fmaxf(top, fmaxf(w[n], p[n] * 0x1p-90f));
+  }
+  if (__any(top > 0x1p15f)) {  // (a NaN is none: it stays where it is)
+    float best = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < R; ++n) {
+      const float m = fmaxf(fmaxf(param_scale(vp[n]), fabsf(param_min(vp[n])) * 0.125f), 0x1p-90f);
+      best = fmaxf(best, x[n] * q.f + (float)((int)(__float_as_uint(m) >> 23) - 127));
+    }
+    best = fmaxf(best, __shfl_xor(best, 16));
+    best = fmaxf(best, __shfl_xor(best, 32));
+    const float ref = fmaxf(s->ref[0], best - 8.f), down = __builtin_amdgcn_exp2f(s->ref[0] - ref);
+    s->ref[0] = ref;
+    s->l[0] *= down;
+    s->z[0] *= down;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) s->o[0][i] *= down;
+#pragma unroll
+    for (int n = 0; n < R; ++n) {
+      p[n] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n], q.f, -ref));
+      w[n] = p[n] * param_scale(vp[n]);
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < R; ++n) {
+    s->l[0] += p[n];
+    s->z[0] = __builtin_fmaf(p[n], __builtin_fmaf(8.f, param_scale(vp[n]), param_min(vp[n])), s->z[0]);
+  }
+}
+
+template <int D, int R, int HW>
+__device__ __forceinline__ void add_values64(const uint4 (&v)[2][D / 64], float* w, Sums<D, 1>* s, const CodeBits& bits, int lane) {
+  constexpr int U = R / 4, N = 4 * U;
+  const int own = (lane & 15) / R;
+  // weights of block b: its first 16 keys in the low halves of a register, the others in the high ones
+  union { uint32_t u[4]; f16x8 v; } wb[2][HW];
+#pragma unroll
+  for (int h = 0; h < HW; ++h) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (R == 16) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) wb[c][h].u[i] = pack_f16(w[8 * c + i], w[8 * c + 4 + i]);
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const uint32_t e = pack_f16(w[4 * u + i], 0.f) << (own & 1 ? 16 : 0);
+          if constexpr (R == 8) wb[u][h].u[i] = e;
+          else {
+            wb[0][h].u[i] = own < 2 ? e : 0u;
+            wb[1][h].u[i] = own < 2 ? 0u : e;
+          }
+        }
+      }
+    }
+    if (h + 1 < HW) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        asm("" : "+v"(w[n]));
+        w[n] -= (float)(_Float16)w[n];
+      }
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      const f16x8 vc = codes8(reinterpret_cast<const uint32_t*>(&v[c][i >> 2])[i & 3], bits);
+#pragma unroll
+      for (int h = HW - 1; h >= 0; --h) s->o[0][i] = mfma(vc, wb[c][h].v, s->o[0][i]);
+      if ((i & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+
+template <int DT, int D, int R>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : R == 4 && DT != PLORA_F32 ? 3 : 2) void k_attend_few(AttendArgs a) {
+  constexpr int HQ = DT == PLORA_BF16 ? 1 : 2, HW = DT == PLORA_F32 ? 2 : 1, Y = kWaves * (16 / R);
+  __shared__ QueryRows<D, HQ, R> query_rows;
+  __shared__ float so[Y][R][D + 4], sm[Y][R], sl[Y][R];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int seq = blockIdx.x / a.c.heads, kvh = blockIdx.x - seq * a.c.heads, part = blockIdx.y;
   const Seq sq = seq_at(a.b, seq);
   const int rows = sq.n * a.rep;
-  if (rows == 0 || rows > kFewRows) return;
+  if (rows == 0 || rows > R) return;
   int lo, hi;
   keys_of_rows(sq, a, 0, rows, &lo, &hi);
   const int n_parts = parts_of(a, lo, hi);
   if (part >= n_parts) return;
   const int from = lo + part * a.part_keys;
   const int to = part == n_parts - 1 ? hi : from + a.part_keys;
-  constexpr int HQ = DT == PLORA_BF16 ? 1 : 2, HW = DT == PLORA_F32 ? 2 : 1;
-  Queries<D, 1, HQ> q;
-  load_queries<DT, D, 1, HQ>(&q, a, sq, kvh, 0, rows, lane);
+  const int64_t head_at = (int64_t)kvh * a.c.page_tokens * (D + 8);
+  constexpr int kStep = 64 * kWaves;
+  int key = from + 64 * wave;
+  Place64 here = place64(a, seq, key, to);
+  Keys64<D, R> k;
+  Values64<D, R> v;
+  load_keys(&k, a, here, head_at, key, lane);
+  load_values(&v, a, here, head_at, key, lane);
+  Place64 next = place64(a, seq, key + kStep, to);
+  stage_queries<DT, D, HQ, R>(&query_rows, a, sq, kvh, 0, rows, threadIdx.x, kThreads);
+  __syncthreads();
+  const int own_row = (lane & 15) % R;
+  const Column q{query_rows.sum[own_row], query_rows.f[own_row], a.causal ? sq.len - sq.n + (own_row < rows ? own_row : rows - 1) / a.rep : 0x7fffffff};
+  const CodeBits bits = code_bits();
   Sums<D, 1> s;
   clear(&s);
-  columns<D, 1, HQ, HW>(a, q, &s, seq, sq, kvh, sq.len - sq.n, from + wave * kBlockTok, kWaves * kBlockTok, to, lane);
+  const int first_place = sq.len - sq.n;
+  while (key < to) {
+    float x[R], w[R];
+    logits64<D, R, HQ>(k, query_rows, q, bits, x, lane);
+    load_keys(&k, a, next, head_at, key + kStep, lane);
+    const bool whole = here.page0 && here.page1 && key + 64 <= to && (!a.causal || (key + 63 <= first_place && (!a.window || key > first_place + sq.n - 1 - a.window)));
+    if (!whole) mask64<D, R>(x, v.vp, q, here, key, to, a.window, lane);
+    weights64<D, R>(v.vp, q, &s, x, w);
+    add_values64<D, R, HW>(v.v, w, &s, bits, lane);
+    load_values(&v, a, next, head_at, key + kStep, lane);
+    here = next;
+    key += kStep;
+    next = place64(a, seq, key + kStep, to);
+  }
   join_lanes(&s);
-  const int r = lane & 15, g = lane >> 4;
+  const int r = lane & 15, g = lane >> 4, at = wave * (16 / R) + r / R;
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(&so[wave][r][g * (D / 4) + 4 * i]) = s.o[0][i];
+  for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(&so[at][r % R][g * (D / 4) + 4 * i]) = s.o[0][i];
   if (g == 0) {
-    sm[wave][r] = s.ref[0];
-    sl[wave][r] = s.l[0];
+    sm[at][r % R] = s.ref[0];
+    sl[at][r % R] = s.l[0];
   }
   __syncthreads();
   for (int i = threadIdx.x; i < rows * (D / 8); i += kThreads) {
     const int row = i / (D / 8), c = (i - row * (D / 8)) * 8;
     float ref = sm[0][row];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) ref = fmaxf(ref, sm[w][row]);
+    for (int k = 1; k < Y; ++k) ref = fmaxf(ref, sm[k][row]);
     float l = 0.f, o[8] = {};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float f = __builtin_amdgcn_exp2f(sm[w][row] - ref);
-      l = __builtin_fmaf(f, sl[w][row], l);
+    for (int k = 0; k < Y; ++k) {
+      const float f = __builtin_amdgcn_exp2f(sm[k][row] - ref);
+      l = __builtin_fmaf(f, sl[k][row], l);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) o[k] = __builtin_fmaf(f, so[w][row][c + k], o[k]);
+      for (int e = 0; e < 8; ++e) o[e] = __builtin_fmaf(f, so[k][row][c + e], o[e]);
     }
     const int t = row / a.rep;
     put8<DT, D>(a, n_parts == 1, part, sq.first + t, kvh * a.rep + row - t * a.rep, c, o, ref, l);
@@ -852,6 +1144,7 @@ __global__ __launch_bounds__(kThreads) void k_attend_few(AttendArgs a) {
 template <int DT, int D, int NQ, int HQ>
 __global__ __launch_bounds__(kThreads) void k_attend_many(AttendArgs a) {
   constexpr int R = 16 * NQ;
+  __shared__ QueryRows<D, HQ, 16> lds[kWaves];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int64_t group = blockIdx.x / a.c.heads;
   const int kvh = (int)(blockIdx.x - group * a.c.heads), part = blockIdx.y;
@@ -859,7 +1152,7 @@ __global__ __launch_bounds__(kThreads) void k_attend_many(AttendArgs a) {
   const int seq = find_seq(a.b, number, a.rep, R, 1);
   const Seq sq = seq_at(a.b, seq);
   const int rows = sq.n * a.rep;
-  if (rows <= kFewRows && a.few) return;
+  if (rows <= a.few_rows) return;
   const int64_t tile = number - first_number(a.b, seq, a.rep, R, 1);
   if (tile < 0 || tile * R >= rows) return;
   const int r0 = (int)tile * R, r1 = r0 + R < rows ? r0 + R : rows;
@@ -871,7 +1164,13 @@ __global__ __launch_bounds__(kThreads) void k_attend_many(AttendArgs a) {
   const int to = part == n_parts - 1 ? hi : from + a.part_keys;
   constexpr int HW = DT == PLORA_F32 ? 2 : 1;
   Queries<D, NQ, HQ> q;
-  load_queries<DT, D, NQ, HQ>(&q, a, sq, kvh, r0, rows, lane);
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    stage_queries<DT, D, HQ, 16>(&lds[wave], a, sq, kvh, r0 + 16 * j, rows, lane, 64);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    take_queries<D, NQ, HQ>(&q, j, lds[wave], a, sq, r0 + 16 * j, rows, lane);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
   Sums<D, NQ> s;
   clear(&s);
   columns<D, NQ, HQ, HW>(a, q, &s, seq, sq, kvh, sq.len - sq.n + r0 / a.rep, from, kBlockTok, to, lane);
@@ -907,7 +1206,7 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
   const int t = tok - sq.first, h = (int)(row - (int64_t)tok * a.heads);
   if (!has || t < 0 || t >= sq.n) return;
   const int kvh_row = t * a.rep + h % a.rep, rows = sq.n * a.rep;
-  const int r0 = rows <= kFewRows ? 0 : kvh_row / R * R, r1 = rows <= kFewRows ? rows : (r0 + R < rows ? r0 + R : rows);
+  const int r0 = kvh_row / R * R, r1 = r0 + R < rows ? r0 + R : rows;  // (a tile of k_attend_few is one of these too: R >= 16)
   int lo, hi;
   keys_of_rows(sq, a, r0, r1, &lo, &hi);
   const int n = parts_of(a, lo, hi);
@@ -1020,7 +1319,10 @@ int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace,
   const int64_t rows = (int64_t)a.b.n_tokens * a.heads;
   if (max_new > a.b.n_tokens) max_new = a.b.n_tokens;
   const int64_t most_rows = (int64_t)max_new * a.rep;
-  const bool some_few = a.b.n_seqs > 1 || most_rows <= kFewRows, some_many = most_rows > kFewRows;
+  const bool some_few = a.b.n_seqs > 1 || most_rows <= kMostFew, some_many = most_rows > kMostFew;
+  // rows of a tile of k_attend_few: all that a sequence can have, or those of a single token next to sequences with many
+  const int64_t tile_rows = some_many ? a.rep : most_rows;
+  a.few_rows = tile_rows <= 4 ? 4 : tile_rows <= 8 ? 8 : 16;
   const uint64_t few = some_few ? (uint64_t)a.b.n_seqs * a.c.heads : 0;
   const uint64_t groups = ((uint64_t)a.b.n_tokens * a.rep / R + a.b.n_seqs + kWaves - 1) / kWaves;
   const uint64_t many = some_many ? groups * a.c.heads : 0;
@@ -1036,9 +1338,10 @@ int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace,
   a.part_keys = (int)(((keys + a.parts - 1) / a.parts + kKeyAlign - 1) / kKeyAlign * kKeyAlign);
   a.part_o = (float*)workspace;
   a.part_ml = a.part_o + (int64_t)a.parts * rows * D;
-  a.few = some_few;
+  if (!some_few) a.few_rows = 0;
   int rc = PLORA_OK;
-  if (few) rc = launch(k_attend_few<DT, D>, few, (unsigned)a.parts, 1, a, stream);
+  if (few)
+    rc = launch(a.few_rows == 4 ? k_attend_few<DT, D, 4> : a.few_rows == 8 ? k_attend_few<DT, D, 8> : k_attend_few<DT, D, 16>, few, (unsigned)a.parts, 1, a, stream);
   if (rc == PLORA_OK && many) {
     // a rotated row of 16-bit elements needs more than the 11 bits of one half to be as good as its elements were; the 8 of bf16 do not
     if (DT == PLORA_F32 || (DT == PLORA_F16 && a.r.table)) rc = launch(k_attend_many<DT, D, NQ, 2>, many, (unsigned)a.parts, 1, a, stream);
