@@ -553,45 +553,6 @@ __device__ __forceinline__ f16x8 codes8(uint32_t w, const CodeBits& c) {
 }
 __device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// What a lane holds of 32 keys of a kv head.
-template <int D>
-struct Block {
-  uint32_t k[2][D / 32];   // words of keys lane%16 and 16 + lane%16
-  uint4 v[D / 64];         // words of channels, keys 4g .. and 16 + 4g ..
-  uint4 kp[2], vp[2];      // scale and min of keys 4g .. 4g+3 and 16 + 4g ..
-};
-template <int D>
-__device__ __forceinline__ void load_block(Block<D>* o, const uint8_t* hp, int pt, int slot, int lane) {
-  const int r = lane & 15, g = lane >> 4;
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const uint8_t* kp = hp + (slot + 16 * t + r) * (D / 2) + g * (D / 8);
-    if constexpr (D == 64) {
-      const uint2 q = *reinterpret_cast<const uint2*>(kp);
-      o->k[t][0] = q.x;
-      o->k[t][1] = q.y;
-    } else {
-#pragma unroll
-      for (int i = 0; i < D / 128; ++i) {
-        const uint4 q = reinterpret_cast<const uint4*>(kp)[i];
-        o->k[t][4 * i] = q.x;
-        o->k[t][4 * i + 1] = q.y;
-        o->k[t][4 * i + 2] = q.z;
-        o->k[t][4 * i + 3] = q.w;
-      }
-    }
-  }
-  const uint8_t* vp = hp + pt * (D / 2) + slot * (D / 2);
-#pragma unroll
-  for (int j = 0; j < D / 64; ++j) o->v[j] = reinterpret_cast<const uint4*>(vp)[j * 64 + lane];
-  const uint4* pp = reinterpret_cast<const uint4*>(hp + pt * D + slot * 4);
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    o->kp[t] = pp[4 * t + g];
-    o->vp[t] = pp[pt / 4 + 4 * t + g];
-  }
-}
-
 // Query rows in LDS: fp16 numbers (a high and a low half if HQ = 2) of a row times its power of two, in the order in which codes8
 // has its elements, with 16 bytes between the rows so that 16 rows' pieces lie in different banks.
 template <int D, int HQ, int R>
@@ -680,120 +641,6 @@ struct Sums {
 
 __device__ __forceinline__ float param_scale(uint32_t p) { return __uint_as_float(p << 16); }
 __device__ __forceinline__ float param_min(uint32_t p) { return __uint_as_float(p & 0xffff0000u); }
-
-// 32 keys: places key0 .. key0 + 31, of which those below `live` exist.  MASK: some column may not see some of them.
-template <int D, int NQ, int HQ, int HW, bool MASK>
-__device__ __forceinline__ void step(const Block<D>& b, const Queries<D, NQ, HQ>& q, const CodeBits& bits, Sums<D, NQ>* s, int key0, int live, int window, int lane) {
-  const int g = lane >> 4;
-  f32x4 t[NQ][2];
-#pragma unroll
-  for (int j = 0; j < NQ; ++j) t[j][0] = t[j][1] = f32x4{q.sum8[j], q.sum8[j], q.sum8[j], q.sum8[j]};
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const f16x8 kc = codes8(b.k[u][i], bits);
-#pragma unroll
-      for (int j = 0; j < NQ; ++j) {
-#pragma unroll
-        for (int h = HQ - 1; h >= 0; --h) t[j][u] = mfma(kc, q.q[j][h][i], t[j][u]);
-      }
-    }
-  }
-  const uint32_t* kp = reinterpret_cast<const uint32_t*>(&b.kp[0]);
-  const uint32_t* vp = reinterpret_cast<const uint32_t*>(&b.vp[0]);
-  f16x8 w[NQ][HW];
-#pragma unroll
-  for (int j = 0; j < NQ; ++j) {
-    float x[8], p[8], wt[8];
-    float top = -INFINITY;
-#pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      x[n] = __builtin_fmaf(param_scale(kp[n]), t[j][n >> 2][n & 3], param_min(kp[n]) * q.sum[j]);
-      if constexpr (MASK) {
-        const int key = key0 + 16 * (n >> 2) + 4 * g + (n & 3);
-        const bool sees = key < live && key <= q.place[j] && (window == 0 || key > q.place[j] - window);
-        x[n] = sees ? x[n] : -INFINITY;
-      }
-      p[n] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n], q.f[j], -s->ref[j]));
-      wt[n] = p[n] * param_scale(vp[n]);
-      if constexpr (MASK) wt[n] = p[n] == 0.f ? 0.f : wt[n];
-      top = fmaxf(top, fmaxf(wt[n], p[n] * 0x1p-90f));
-    }
-    if (__any(top > 0x1p15f)) {  // (a NaN is none: it stays where it is)
-      float best = -INFINITY;
-#pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        const float m = fmaxf(fmaxf(param_scale(vp[n]), fabsf(param_min(vp[n])) * 0.125f), 0x1p-90f);
-        best = fmaxf(best, x[n] * q.f[j] + (float)((int)(__float_as_uint(m) >> 23) - 127));
-      }
-      best = fmaxf(best, __shfl_xor(best, 16));
-      best = fmaxf(best, __shfl_xor(best, 32));
-      const float ref = fmaxf(s->ref[j], best - 8.f), down = __builtin_amdgcn_exp2f(s->ref[j] - ref);
-      s->ref[j] = ref;
-      s->l[j] *= down;
-      s->z[j] *= down;
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) s->o[j][i] *= down;
-#pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        p[n] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n], q.f[j], -ref));
-        wt[n] = p[n] * param_scale(vp[n]);
-        if constexpr (MASK) wt[n] = p[n] == 0.f ? 0.f : wt[n];
-      }
-    }
-#pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      s->l[j] += p[n];
-      const float mc = __builtin_fmaf(8.f, param_scale(vp[n]), param_min(vp[n]));
-      if constexpr (MASK) s->z[j] += p[n] == 0.f ? 0.f : p[n] * mc;
-      else s->z[j] = __builtin_fmaf(p[n], mc, s->z[j]);
-    }
-    _Float16 hi[8], lo[8];
-#pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      hi[n] = (_Float16)wt[n];
-      lo[n] = (_Float16)(wt[n] - (float)hi[n]);
-    }
-    w[j][0] = f16x8{hi[0], hi[4], hi[1], hi[5], hi[2], hi[6], hi[3], hi[7]};
-    if constexpr (HW == 2) w[j][1] = f16x8{lo[0], lo[4], lo[1], lo[5], lo[2], lo[6], lo[3], lo[7]};
-  }
-#pragma unroll
-  for (int i = 0; i < D / 16; ++i) {
-    const uint32_t* vw = reinterpret_cast<const uint32_t*>(&b.v[i >> 2]);
-    const f16x8 vc = codes8(vw[i & 3], bits);
-#pragma unroll
-    for (int j = 0; j < NQ; ++j) {
-#pragma unroll
-      for (int h = HW - 1; h >= 0; --h) s->o[j][i] = mfma(vc, w[j][h], s->o[j][i]);
-    }
-  }
-}
-
-// Columns over keys first, first + stride, ... (blocks of 32) below `hi`.
-template <int D, int NQ, int HQ, int HW>
-__device__ __forceinline__ void columns(const AttendArgs& a, const Queries<D, NQ, HQ>& q, Sums<D, NQ>* s, int seq, const Seq& sq, int kvh,
-                                        int first_place, int key, int stride, int hi, int lane) {
-  const int pt = a.c.page_tokens;
-  const int64_t head_at = (int64_t)kvh * pt * (D + 8);
-  Block<D> cur, nxt;
-  const CodeBits bits = code_bits();
-  const uint8_t* page = key < hi ? page_of(a.c, a.b, seq, key) : nullptr;
-  load_block<D>(&cur, (page ? page : a.c.pages) + head_at, pt, key & (pt - 1), lane);
-  while (key < hi) {
-    const int next = key + stride;
-    const uint8_t* np = next < hi ? page_of(a.c, a.b, seq, next) : nullptr;
-    load_block<D>(&nxt, (np ? np : a.c.pages) + head_at, pt, next & (pt - 1), lane);
-    if (page) {
-      const bool whole = key + kBlockTok <= hi && (!a.causal || (key + kBlockTok - 1 <= first_place && !a.window));
-      if (whole) step<D, NQ, HQ, HW, false>(cur, q, bits, s, key, hi, 0, lane);
-      else step<D, NQ, HQ, HW, true>(cur, q, bits, s, key, hi, a.window, lane);
-    }
-    cur = nxt;
-    page = np;
-    key = next;
-  }
-}
 
 template <int D, int NQ>
 __device__ __forceinline__ void clear(Sums<D, NQ>* s) {
@@ -1140,40 +987,244 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : R == 4 && DT != PLORA_F32 
   }
 }
 
-// Sequences with more rows: a wavefront has a tile of 16 * NQ rows of its own, and all keys of the part.
+// Sequences with more rows: a workgroup has 64 * NQ of them, a wavefront 16 * NQ, and all keys of the part.  What bounds it are the
+// vector instructions of the softmax (11 issue slots a logit, 4 of them the exponential), so the codes' unpacking is shared: of
+// kStage keys each wavefront turns a quarter of the codes into the operands that all four then read from LDS (in operand
+// order: a lane's 16 bytes beside the next lane's), a stage ahead of their use, with one barrier a stage.
+template <int D> constexpr int stage_keys() { return D == 256 ? 32 : 64; }
+template <int D>
+struct Stage {
+  static constexpr int K = stage_keys<D>(), W = K / 16 * (D / 32) / kWaves;  // keys; words of keys, and of values, of a lane
+  uint4 keys[K / 16 * (D / 32)][64];    // [tile of 16 keys][32 channels], then lanes
+  uint4 values[K / 32 * (D / 16)][64];  // [32 keys][16 channels]
+  float ks[K], km[K], vs[K], vm[K];     // scale and min of keys; scale and min + 8 scale of values, 0 where there is no row
+};
+// What a wavefront fetches of a stage.
+template <int D>
+struct Fetched {
+  uint32_t k[Stage<D>::W], v[Stage<D>::W];
+  uint32_t kp, vp;
+};
+template <int W>
+__device__ __forceinline__ void ld_words(uint32_t* o, const uint8_t* p) {
+  if constexpr (W == 2) {
+    const uint2 q = *reinterpret_cast<const uint2*>(p);
+    o[0] = q.x;
+    o[1] = q.y;
+  } else {
+    const uint4 q = *reinterpret_cast<const uint4*>(p);
+    o[0] = q.x;
+    o[1] = q.y;
+    o[2] = q.z;
+    o[3] = q.w;
+  }
+}
+// Keys key .. key + K-1 (behind `to` and in holes: anything, with a value's scale and min 0).
+template <int D>
+__device__ __forceinline__ void fetch(Fetched<D>* o, const AttendArgs& a, int seq, int64_t head_at, int key, int to, int wave, int lane) {
+  constexpr int K = Stage<D>::K, W = Stage<D>::W;
+  const int r = lane & 15, g = lane >> 4, pt = a.c.page_tokens;
+  const uint8_t* p0 = key < to ? page_of(a.c, a.b, seq, key) : nullptr;
+  const uint8_t* p1 = K > kBlockTok && key + kBlockTok < to ? page_of(a.c, a.b, seq, key + kBlockTok) : nullptr;
+  const uint8_t *h0 = (p0 ? p0 : a.c.pages) + head_at, *h1 = (p1 ? p1 : a.c.pages) + head_at;
+  const int slot0 = key & (pt - 1), slot1 = (key + kBlockTok) & (pt - 1);
+  {
+    const int tile = wave * W / (D / 32), i0 = wave * W % (D / 32);
+    const uint8_t* h = tile < 2 ? h0 + slot0 * (D / 2) : h1 + slot1 * (D / 2);
+    ld_words<W>(o->k, h + (16 * (tile & 1) + r) * (D / 2) + g * (D / 8) + 4 * i0);
+  }
+  {
+    const int block = wave * W / (D / 16), t0 = wave * W % (D / 16);
+    const uint8_t* h = (block == 0 ? h0 + slot0 * (D / 2) : h1 + slot1 * (D / 2)) + pt * (D / 2);
+    ld_words<W>(o->v, h + ((t0 >> 2) * 64 + lane) * 16 + (t0 & 3) * 4);
+  }
+  if (wave == 0) {
+    const bool second = K > kBlockTok && lane >= kBlockTok;
+    const uint8_t* h = (second ? h1 + slot1 * 4 : h0 + slot0 * 4) + pt * D + (lane & (kBlockTok - 1)) * 4;
+    const bool there = (second ? p1 : p0) && key + lane < to;
+    o->kp = *reinterpret_cast<const uint32_t*>(h);
+    o->vp = *reinterpret_cast<const uint32_t*>(h + pt * 4);
+    o->vp = there ? o->vp : 0u;
+  }
+}
+template <int D>
+__device__ __forceinline__ void unpack(Stage<D>* o, const Fetched<D>& f, const CodeBits& bits, int wave, int lane) {
+  constexpr int W = Stage<D>::W;
+#pragma unroll
+  for (int i = 0; i < W; ++i) o->keys[wave * W + i][lane] = __builtin_bit_cast(uint4, codes8(f.k[i], bits));
+#pragma unroll
+  for (int i = 0; i < W; ++i) o->values[wave * W + i][lane] = __builtin_bit_cast(uint4, codes8(f.v[i], bits));
+  if (wave == 0 && lane < Stage<D>::K) {
+    // A row of values that is none (NaN) makes its key NaN and itself 0: whoever sees it has a NaN for a weight, and whoever does
+    // not has a weight of 0 that meets nothing but numbers.
+    const float s = param_scale(f.vp), m = __builtin_fmaf(8.f, s, param_min(f.vp));
+    const bool fine = fabsf(s) < INFINITY && fabsf(m) < INFINITY;
+    o->ks[lane] = fine ? param_scale(f.kp) : __builtin_nanf("");
+    o->km[lane] = param_min(f.kp);
+    o->vs[lane] = fine ? s : 0.f;
+    o->vm[lane] = fine ? m : 0.f;
+  }
+}
+
+// 32 keys of a stage, places key0 .. key0 + 31, of which those below `live` exist.  whole: every column sees all of them.
+template <int D, int NQ, int HQ, int HW>
+__device__ __forceinline__ void step32(const Stage<D>& b, int block, const Queries<D, NQ, HQ>& q, Sums<D, NQ>* s, bool whole, int key0, int live, int window, int lane) {
+  const int g = lane >> 4;
+  f32x4 t[NQ][2];
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) t[j][0] = t[j][1] = f32x4{q.sum8[j], q.sum8[j], q.sum8[j], q.sum8[j]};
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const f16x8 kc = __builtin_bit_cast(f16x8, b.keys[(2 * block + u) * (D / 32) + i][lane]);
+#pragma unroll
+      for (int j = 0; j < NQ; ++j) {
+#pragma unroll
+        for (int h = HQ - 1; h >= 0; --h) t[j][u] = mfma(kc, q.q[j][h][i], t[j][u]);
+      }
+    }
+  }
+  f32x4 ks[2], km[2], vs[2], vm[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int at = block * kBlockTok + 16 * u + 4 * g;
+    ks[u] = *reinterpret_cast<const f32x4*>(&b.ks[at]);
+    km[u] = *reinterpret_cast<const f32x4*>(&b.km[at]);
+    vs[u] = *reinterpret_cast<const f32x4*>(&b.vs[at]);
+    vm[u] = *reinterpret_cast<const f32x4*>(&b.vm[at]);
+  }
+  union { uint32_t u[4]; f16x8 v; } wb[NQ][HW];
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    float x[8], p[8], w[8];
+    float top = 0.f, l = 0.f, z = 0.f;
+#pragma unroll
+    for (int n = 0; n < 8; ++n) x[n] = __builtin_fmaf(ks[n >> 2][n & 3], t[j][n >> 2][n & 3], km[n >> 2][n & 3] * q.sum[j]);
+    if (!whole) {
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        const int key = key0 + 16 * (n >> 2) + 4 * g + (n & 3);
+        x[n] = key < live && key <= q.place[j] && (window == 0 || key > q.place[j] - window) ? x[n] : -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      p[n] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n], q.f[j], -s->ref[j]));
+      w[n] = p[n] * vs[n >> 2][n & 3];
+      top = fmaxf(top, w[n]);
+      l += p[n];
+      z = __builtin_fmaf(p[n], vm[n >> 2][n & 3], z);
+    }
+    if (__any(fmaxf(top, l * 0x1p-93f) > 0x1p15f)) {  // (a NaN is none: it stays where it is)
+      float best = -INFINITY;
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        const float sc = vs[n >> 2][n & 3], m = fmaxf(fmaxf(sc, fabsf(__builtin_fmaf(-8.f, sc, vm[n >> 2][n & 3])) * 0.125f), 0x1p-90f);
+        best = fmaxf(best, x[n] * q.f[j] + (float)((int)(__float_as_uint(m) >> 23) - 127));
+      }
+      best = fmaxf(best, __shfl_xor(best, 16));
+      best = fmaxf(best, __shfl_xor(best, 32));
+      const float ref = fmaxf(s->ref[j], best - 8.f), down = __builtin_amdgcn_exp2f(s->ref[j] - ref);
+      s->ref[j] = ref;
+      s->l[j] *= down;
+      s->z[j] *= down;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) s->o[j][i] *= down;
+      l = z = 0.f;
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        p[n] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n], q.f[j], -ref));
+        w[n] = p[n] * vs[n >> 2][n & 3];
+        l += p[n];
+        z = __builtin_fmaf(p[n], vm[n >> 2][n & 3], z);
+      }
+    }
+    s->l[j] += l;
+    s->z[j] += z;
+#pragma unroll
+    for (int h = 0; h < HW; ++h) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) wb[j][h].u[i] = pack_f16(w[i], w[4 + i]);
+      if (h + 1 < HW) {
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+          asm("" : "+v"(w[n]));
+          w[n] -= (float)(_Float16)w[n];
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    const f16x8 vc = __builtin_bit_cast(f16x8, b.values[block * (D / 16) + i][lane]);
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+#pragma unroll
+      for (int h = HW - 1; h >= 0; --h) s->o[j][i] = mfma(vc, wb[j][h].v, s->o[j][i]);
+    }
+  }
+}
+
 template <int DT, int D, int NQ, int HQ>
-__global__ __launch_bounds__(kThreads) void k_attend_many(AttendArgs a) {
-  constexpr int R = 16 * NQ;
-  __shared__ QueryRows<D, HQ, 16> lds[kWaves];
+__global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
+  constexpr int HW = DT == PLORA_F32 ? 2 : 1, R = 16 * NQ, K = Stage<D>::K;
+  __shared__ union {
+    Stage<D> stage[2];
+    QueryRows<D, HQ, 16> rows[kWaves];
+  } lds;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const int64_t group = blockIdx.x / a.c.heads;
-  const int kvh = (int)(blockIdx.x - group * a.c.heads), part = blockIdx.y;
-  const int64_t number = group * kWaves + wave;
-  const int seq = find_seq(a.b, number, a.rep, R, 1);
+  const int64_t number = blockIdx.x / a.c.heads;
+  const int kvh = (int)(blockIdx.x - number * a.c.heads), part = blockIdx.y;
+  const int seq = find_seq(a.b, number, a.rep, R * kWaves, 1);
   const Seq sq = seq_at(a.b, seq);
   const int rows = sq.n * a.rep;
   if (rows <= a.few_rows) return;
-  const int64_t tile = number - first_number(a.b, seq, a.rep, R, 1);
-  if (tile < 0 || tile * R >= rows) return;
-  const int r0 = (int)tile * R, r1 = r0 + R < rows ? r0 + R : rows;
+  const int64_t tile = number - first_number(a.b, seq, a.rep, R * kWaves, 1);
+  if (tile < 0 || tile * (R * kWaves) >= rows) return;
+  const int w0 = (int)tile * (R * kWaves), w1 = w0 + R * kWaves < rows ? w0 + R * kWaves : rows;  // rows of the workgroup
   int lo, hi;
-  keys_of_rows(sq, a, r0, r1, &lo, &hi);
+  keys_of_rows(sq, a, w0, w1, &lo, &hi);
   const int n_parts = parts_of(a, lo, hi);
   if (part >= n_parts) return;
   const int from = lo + part * a.part_keys;
   const int to = part == n_parts - 1 ? hi : from + a.part_keys;
-  constexpr int HW = DT == PLORA_F32 ? 2 : 1;
+  const int64_t head_at = (int64_t)kvh * a.c.page_tokens * (D + 8);
+  const int r0 = w0 + wave * R, r1 = r0 + R < w1 ? r0 + R : w1;  // rows of the wavefront: none if r0 >= r1
+  const CodeBits bits = code_bits();
+  Fetched<D> f;
+  fetch<D>(&f, a, seq, head_at, from, to, wave, lane);
   Queries<D, NQ, HQ> q;
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
-    stage_queries<DT, D, HQ, 16>(&lds[wave], a, sq, kvh, r0 + 16 * j, rows, lane, 64);
+    stage_queries<DT, D, HQ, 16>(&lds.rows[wave], a, sq, kvh, r0 + 16 * j, w1, lane, 64);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    take_queries<D, NQ, HQ>(&q, j, lds[wave], a, sq, r0 + 16 * j, rows, lane);
+    take_queries<D, NQ, HQ>(&q, j, lds.rows[wave], a, sq, r0 + 16 * j, w1, lane);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
+  __syncthreads();
+  unpack<D>(&lds.stage[0], f, bits, wave, lane);
+  fetch<D>(&f, a, seq, head_at, from + K, to, wave, lane);
+  __syncthreads();
   Sums<D, NQ> s;
   clear(&s);
-  columns<D, NQ, HQ, HW>(a, q, &s, seq, sq, kvh, sq.len - sq.n + r0 / a.rep, from, kBlockTok, to, lane);
+  // places of the wavefront's first and last row, if what a row sees goes by its place
+  const int first = a.causal ? sq.len - sq.n + r0 / a.rep : 0x7fffffff, last = a.causal ? sq.len - sq.n + (r1 - 1) / a.rep : 0x7fffffff;
+  int at = 0;
+  for (int key = from; key < to; key += K) {
+#pragma unroll 1
+    for (int block = 0; block < K / kBlockTok; ++block) {
+      const int key0 = key + block * kBlockTok;
+      if (key0 < to && r0 < r1 && key0 <= last && (!a.window || key0 + kBlockTok - 1 > first - a.window)) {
+        const bool whole = key0 + kBlockTok <= to && key0 + kBlockTok - 1 <= first && (!a.window || key0 > last - a.window);
+        if (page_of(a.c, a.b, seq, key0)) step32<D, NQ, HQ, HW>(lds.stage[at], block, q, &s, whole, key0, to, a.window, lane);
+      }
+    }
+    at ^= 1;
+    if (key + K < to) unpack<D>(&lds.stage[at], f, bits, wave, lane);
+    fetch<D>(&f, a, seq, head_at, key + 2 * K, to, wave, lane);
+    __syncthreads();
+  }
   join_lanes(&s);
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
@@ -1310,12 +1361,12 @@ int append_or_read(int dtype, int head_dim, const CacheArgs& a, bool read, plora
          : dtype == PLORA_F16 ? append_or_read<PLORA_F16>(head_dim, a, read, stream) : append_or_read<PLORA_F32>(head_dim, a, read, stream);
 }
 
-// Columns of a wavefront of k_attend_many.
+// Tiles of 16 columns of a wavefront of k_attend_many.
 template <int DT, int D> constexpr int columns_of() { return DT == PLORA_F32 || D == 256 ? 1 : 2; }
 
 template <int DT, int D>
 int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace, plora_stream stream) {
-  constexpr int NQ = columns_of<DT, D>(), R = 16 * NQ;
+  constexpr int NQ = columns_of<DT, D>(), R = 16 * NQ * kWaves;
   const int64_t rows = (int64_t)a.b.n_tokens * a.heads;
   if (max_new > a.b.n_tokens) max_new = a.b.n_tokens;
   const int64_t most_rows = (int64_t)max_new * a.rep;
@@ -1324,7 +1375,7 @@ int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace,
   const int64_t tile_rows = some_many ? a.rep : most_rows;
   a.few_rows = tile_rows <= 4 ? 4 : tile_rows <= 8 ? 8 : 16;
   const uint64_t few = some_few ? (uint64_t)a.b.n_seqs * a.c.heads : 0;
-  const uint64_t groups = ((uint64_t)a.b.n_tokens * a.rep / R + a.b.n_seqs + kWaves - 1) / kWaves;
+  const uint64_t groups = (uint64_t)a.b.n_tokens * a.rep / R + a.b.n_seqs;
   const uint64_t many = some_many ? groups * a.c.heads : 0;
   // parts: as many as keep the GPU's 1024 SIMDs in work, no shorter than 256 keys
   const uint64_t fit = workspace ? workspace_bytes / ((uint64_t)rows * (D + 2) * 4) : 0;
