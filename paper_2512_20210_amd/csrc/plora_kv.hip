@@ -616,13 +616,13 @@ struct Queries {
   float f[NQ];
   int place[NQ];   // last place that the column sees
 };
-template <int D, int NQ, int HQ>
-__device__ __forceinline__ void take_queries(Queries<D, NQ, HQ>* o, int j, const QueryRows<D, HQ, 16>& from, const AttendArgs& a, const Seq& s, int r0, int rows, int lane) {
+template <int D, int NQ, int H, int HQ>
+__device__ __forceinline__ void take_queries(Queries<D, NQ, H>* o, int j, const QueryRows<D, HQ, 16>& from, const AttendArgs& a, const Seq& s, int r0, int rows, int lane) {
   const int r = lane & 15, g = lane >> 4;
   const int row = r0 + r < rows ? r0 + r : rows - 1;
   o->place[j] = a.causal ? s.len - s.n + row / a.rep : 0x7fffffff;
 #pragma unroll
-  for (int h = 0; h < HQ; ++h) {
+  for (int h = 0; h < H; ++h) {
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) o->q[j][h][i] = __builtin_bit_cast(f16x8, from.q[h][r][g * (D / 32) + i]);
   }
@@ -991,18 +991,17 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : R == 4 && DT != PLORA_F32 
 // vector instructions of the softmax (11 issue slots a logit, 4 of them the exponential), so the codes' unpacking is shared: of
 // kStage keys each wavefront turns a quarter of the codes into the operands that all four then read from LDS (in operand
 // order: a lane's 16 bytes beside the next lane's), a stage ahead of their use, with one barrier a stage.
-template <int D> constexpr int stage_keys() { return D == 256 ? 32 : 64; }
-template <int D>
+template <int D, int KEYS>
 struct Stage {
-  static constexpr int K = stage_keys<D>(), W = K / 16 * (D / 32) / kWaves;  // keys; words of keys, and of values, of a lane
+  static constexpr int K = KEYS, W = K / 16 * (D / 32) / kWaves;  // keys; words of keys, and of values, of a lane
   uint4 keys[K / 16 * (D / 32)][64];    // [tile of 16 keys][32 channels], then lanes
   uint4 values[K / 32 * (D / 16)][64];  // [32 keys][16 channels]
   float ks[K], km[K], vs[K], vm[K];     // scale and min of keys; scale and min + 8 scale of values, 0 where there is no row
 };
 // What a wavefront fetches of a stage.
-template <int D>
+template <int W>
 struct Fetched {
-  uint32_t k[Stage<D>::W], v[Stage<D>::W];
+  uint32_t k[W], v[W];
   uint32_t kp, vp;
 };
 template <int W>
@@ -1020,9 +1019,8 @@ __device__ __forceinline__ void ld_words(uint32_t* o, const uint8_t* p) {
   }
 }
 // Keys key .. key + K-1 (behind `to` and in holes: anything, with a value's scale and min 0).
-template <int D>
-__device__ __forceinline__ void fetch(Fetched<D>* o, const AttendArgs& a, int seq, int64_t head_at, int key, int to, int wave, int lane) {
-  constexpr int K = Stage<D>::K, W = Stage<D>::W;
+template <int D, int K, int W>
+__device__ __forceinline__ void fetch(Fetched<W>* o, const AttendArgs& a, int seq, int64_t head_at, int key, int to, int wave, int lane) {
   const int r = lane & 15, g = lane >> 4, pt = a.c.page_tokens;
   const uint8_t* p0 = key < to ? page_of(a.c, a.b, seq, key) : nullptr;
   const uint8_t* p1 = K > kBlockTok && key + kBlockTok < to ? page_of(a.c, a.b, seq, key + kBlockTok) : nullptr;
@@ -1047,14 +1045,13 @@ __device__ __forceinline__ void fetch(Fetched<D>* o, const AttendArgs& a, int se
     o->vp = there ? o->vp : 0u;
   }
 }
-template <int D>
-__device__ __forceinline__ void unpack(Stage<D>* o, const Fetched<D>& f, const CodeBits& bits, int wave, int lane) {
-  constexpr int W = Stage<D>::W;
+template <int D, int K, int W>
+__device__ __forceinline__ void unpack(Stage<D, K>* o, const Fetched<W>& f, const CodeBits& bits, int wave, int lane) {
 #pragma unroll
   for (int i = 0; i < W; ++i) o->keys[wave * W + i][lane] = __builtin_bit_cast(uint4, codes8(f.k[i], bits));
 #pragma unroll
   for (int i = 0; i < W; ++i) o->values[wave * W + i][lane] = __builtin_bit_cast(uint4, codes8(f.v[i], bits));
-  if (wave == 0 && lane < Stage<D>::K) {
+  if (wave == 0 && lane < K) {
     // A row of values that is none (NaN) makes its key NaN and itself 0: whoever sees it has a NaN for a weight, and whoever does
     // not has a weight of 0 that meets nothing but numbers.
     const float s = param_scale(f.vp), m = __builtin_fmaf(8.f, s, param_min(f.vp));
@@ -1067,61 +1064,85 @@ __device__ __forceinline__ void unpack(Stage<D>* o, const Fetched<D>& f, const C
 }
 
 // 32 keys of a stage, places key0 .. key0 + 31, of which those below `live` exist.  whole: every column sees all of them.
-template <int D, int NQ, int HQ, int HW>
-__device__ __forceinline__ void step32(const Stage<D>& b, int block, const Queries<D, NQ, HQ>& q, Sums<D, NQ>* s, bool whole, int key0, int live, int window, int lane) {
+// low: the low halves of the query rows, in LDS in operand order, if they are not in q.
+template <int D, int NQ, int HQ, int HW, int K, bool LOW_IN_LDS>
+__device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Queries<D, NQ, LOW_IN_LDS ? 1 : HQ>& q, const uint4 (*low)[64], Sums<D, NQ>* s, bool whole,
+                                       int key0, int live, int window, int lane) {
   const int g = lane >> 4;
   f32x4 t[NQ][2];
 #pragma unroll
   for (int j = 0; j < NQ; ++j) t[j][0] = t[j][1] = f32x4{q.sum8[j], q.sum8[j], q.sum8[j], q.sum8[j]};
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
+    const f16x8 k0 = __builtin_bit_cast(f16x8, b.keys[2 * block * (D / 32) + i][lane]), k1 = __builtin_bit_cast(f16x8, b.keys[(2 * block + 1) * (D / 32) + i][lane]);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const f16x8 kc = __builtin_bit_cast(f16x8, b.keys[(2 * block + u) * (D / 32) + i][lane]);
+    for (int h = HQ - 1; h >= 0; --h) {
 #pragma unroll
       for (int j = 0; j < NQ; ++j) {
-#pragma unroll
-        for (int h = HQ - 1; h >= 0; --h) t[j][u] = mfma(kc, q.q[j][h][i], t[j][u]);
+        f16x8 qf;
+        if constexpr (LOW_IN_LDS) qf = h == 1 ? __builtin_bit_cast(f16x8, low[j * (D / 32) + i][lane]) : q.q[j][0][i];
+        else qf = q.q[j][h][i];
+        t[j][0] = mfma(k0, qf, t[j][0]);
+        t[j][1] = mfma(k1, qf, t[j][1]);
       }
     }
   }
-  f32x4 ks[2], km[2], vs[2], vm[2];
+  float x[NQ][8], p[NQ][8], w[NQ][8], l[NQ], z[NQ];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int at = block * kBlockTok + 16 * u + 4 * g;
-    ks[u] = *reinterpret_cast<const f32x4*>(&b.ks[at]);
-    km[u] = *reinterpret_cast<const f32x4*>(&b.km[at]);
+    const f32x4 ks = *reinterpret_cast<const f32x4*>(&b.ks[at]), km = *reinterpret_cast<const f32x4*>(&b.km[at]);
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[j][4 * u + i] = __builtin_fmaf(ks[i], t[j][u][i], km[i] * q.sum[j]);
+    }
+  }
+  if (!whole) {
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+      // keys of the lane from `since` to `until` are seen, counted from its first one
+      const int base = key0 + 4 * g, until = (live - 1 < q.place[j] ? live - 1 : q.place[j]) - base, since = window ? q.place[j] - window + 1 - base : -64;
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        const int k = 16 * (n >> 2) + (n & 3);
+        x[j][n] = k <= until && k >= since ? x[j][n] : -INFINITY;
+      }
+    }
+  }
+  f32x4 vs[2], vm[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int at = block * kBlockTok + 16 * u + 4 * g;
     vs[u] = *reinterpret_cast<const f32x4*>(&b.vs[at]);
     vm[u] = *reinterpret_cast<const f32x4*>(&b.vm[at]);
   }
-  union { uint32_t u[4]; f16x8 v; } wb[NQ][HW];
-#pragma unroll
-  for (int j = 0; j < NQ; ++j) {
-    float x[8], p[8], w[8];
-    float top = 0.f, l = 0.f, z = 0.f;
-#pragma unroll
-    for (int n = 0; n < 8; ++n) x[n] = __builtin_fmaf(ks[n >> 2][n & 3], t[j][n >> 2][n & 3], km[n >> 2][n & 3] * q.sum[j]);
-    if (!whole) {
-#pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        const int key = key0 + 16 * (n >> 2) + 4 * g + (n & 3);
-        x[n] = key < live && key <= q.place[j] && (window == 0 || key > q.place[j] - window) ? x[n] : -INFINITY;
-      }
-    }
+  float top = 0.f;
+  auto weights = [&](int j) {
+    l[j] = z[j] = 0.f;
 #pragma unroll
     for (int n = 0; n < 8; ++n) {
-      p[n] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n], q.f[j], -s->ref[j]));
-      w[n] = p[n] * vs[n >> 2][n & 3];
-      top = fmaxf(top, w[n]);
-      l += p[n];
-      z = __builtin_fmaf(p[n], vm[n >> 2][n & 3], z);
+      p[j][n] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][n], q.f[j], -s->ref[j]));
+      w[j][n] = p[j][n] * vs[n >> 2][n & 3];
+      l[j] += p[j][n];
+      z[j] = __builtin_fmaf(p[j][n], vm[n >> 2][n & 3], z[j]);
     }
-    if (__any(fmaxf(top, l * 0x1p-93f) > 0x1p15f)) {  // (a NaN is none: it stays where it is)
+  };
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    weights(j);
+    top = fmaxf(top, l[j] * 0x1p-93f);
+#pragma unroll
+    for (int n = 0; n < 8; ++n) top = fmaxf(top, w[j][n]);
+  }
+  if (__any(top > 0x1p15f)) {  // (a NaN is none: it stays where it is)
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
       float best = -INFINITY;
 #pragma unroll
       for (int n = 0; n < 8; ++n) {
         const float sc = vs[n >> 2][n & 3], m = fmaxf(fmaxf(sc, fabsf(__builtin_fmaf(-8.f, sc, vm[n >> 2][n & 3])) * 0.125f), 0x1p-90f);
-        best = fmaxf(best, x[n] * q.f[j] + (float)((int)(__float_as_uint(m) >> 23) - 127));
+        best = fmaxf(best, x[j][n] * q.f[j] + (float)((int)(__float_as_uint(m) >> 23) - 127));
       }
       best = fmaxf(best, __shfl_xor(best, 16));
       best = fmaxf(best, __shfl_xor(best, 32));
@@ -1131,26 +1152,23 @@ __device__ __forceinline__ void step32(const Stage<D>& b, int block, const Queri
       s->z[j] *= down;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) s->o[j][i] *= down;
-      l = z = 0.f;
-#pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        p[n] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n], q.f[j], -ref));
-        w[n] = p[n] * vs[n >> 2][n & 3];
-        l += p[n];
-        z = __builtin_fmaf(p[n], vm[n >> 2][n & 3], z);
-      }
+      weights(j);
     }
-    s->l[j] += l;
-    s->z[j] += z;
+  }
+  union { uint32_t u[4]; f16x8 v; } wb[NQ][HW];
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    s->l[j] += l[j];
+    s->z[j] += z[j];
 #pragma unroll
     for (int h = 0; h < HW; ++h) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) wb[j][h].u[i] = pack_f16(w[i], w[4 + i]);
+      for (int i = 0; i < 4; ++i) wb[j][h].u[i] = pack_f16(w[j][i], w[j][4 + i]);
       if (h + 1 < HW) {
 #pragma unroll
         for (int n = 0; n < 8; ++n) {
-          asm("" : "+v"(w[n]));
-          w[n] -= (float)(_Float16)w[n];
+          asm("" : "+v"(w[j][n]));
+          w[j][n] -= (float)(_Float16)w[j][n];
         }
       }
     }
@@ -1168,11 +1186,16 @@ __device__ __forceinline__ void step32(const Stage<D>& b, int block, const Queri
 
 template <int DT, int D, int NQ, int HQ>
 __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
-  constexpr int HW = DT == PLORA_F32 ? 2 : 1, R = 16 * NQ, K = Stage<D>::K;
+  constexpr int HW = DT == PLORA_F32 ? 2 : 1, R = 16 * NQ;
+  // Two workgroups share a CU.  Low halves of 32 rows of 128 channels do not fit the registers beside the rest; with them in LDS
+  // a stage is 32 keys.
+  constexpr bool LOW_IN_LDS = HQ == 2 && NQ == 2 && D == 128;
+  constexpr int K = D == 256 || LOW_IN_LDS ? 32 : 64, W = Stage<D, K>::W;
   __shared__ union {
-    Stage<D> stage[2];
+    Stage<D, K> stage[2];
     QueryRows<D, HQ, 16> rows[kWaves];
   } lds;
+  __shared__ uint4 low[LOW_IN_LDS ? kWaves : 1][LOW_IN_LDS ? NQ * (D / 32) : 1][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int64_t number = blockIdx.x / a.c.heads;
   const int kvh = (int)(blockIdx.x - number * a.c.heads), part = blockIdx.y;
@@ -1192,19 +1215,23 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
   const int64_t head_at = (int64_t)kvh * a.c.page_tokens * (D + 8);
   const int r0 = w0 + wave * R, r1 = r0 + R < w1 ? r0 + R : w1;  // rows of the wavefront: none if r0 >= r1
   const CodeBits bits = code_bits();
-  Fetched<D> f;
-  fetch<D>(&f, a, seq, head_at, from, to, wave, lane);
-  Queries<D, NQ, HQ> q;
+  Fetched<W> f;
+  fetch<D, K>(&f, a, seq, head_at, from, to, wave, lane);
+  Queries<D, NQ, LOW_IN_LDS ? 1 : HQ> q;
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
     stage_queries<DT, D, HQ, 16>(&lds.rows[wave], a, sq, kvh, r0 + 16 * j, w1, lane, 64);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    take_queries<D, NQ, HQ>(&q, j, lds.rows[wave], a, sq, r0 + 16 * j, w1, lane);
+    take_queries(&q, j, lds.rows[wave], a, sq, r0 + 16 * j, w1, lane);
+    if constexpr (LOW_IN_LDS) {
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) low[wave][j * (D / 32) + i][lane] = lds.rows[wave].q[1][lane & 15][(lane >> 4) * (D / 32) + i];
+    }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
   __syncthreads();
-  unpack<D>(&lds.stage[0], f, bits, wave, lane);
-  fetch<D>(&f, a, seq, head_at, from + K, to, wave, lane);
+  unpack<D, K>(&lds.stage[0], f, bits, wave, lane);
+  fetch<D, K>(&f, a, seq, head_at, from + K, to, wave, lane);
   __syncthreads();
   Sums<D, NQ> s;
   clear(&s);
@@ -1217,12 +1244,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
       const int key0 = key + block * kBlockTok;
       if (key0 < to && r0 < r1 && key0 <= last && (!a.window || key0 + kBlockTok - 1 > first - a.window)) {
         const bool whole = key0 + kBlockTok <= to && key0 + kBlockTok - 1 <= first && (!a.window || key0 > last - a.window);
-        if (page_of(a.c, a.b, seq, key0)) step32<D, NQ, HQ, HW>(lds.stage[at], block, q, &s, whole, key0, to, a.window, lane);
+        if (page_of(a.c, a.b, seq, key0)) step32<D, NQ, HQ, HW, K, LOW_IN_LDS>(lds.stage[at], block, q, low[LOW_IN_LDS ? wave : 0], &s, whole, key0, to, a.window, lane);
       }
     }
     at ^= 1;
-    if (key + K < to) unpack<D>(&lds.stage[at], f, bits, wave, lane);
-    fetch<D>(&f, a, seq, head_at, key + 2 * K, to, wave, lane);
+    if (key + K < to) unpack<D, K>(&lds.stage[at], f, bits, wave, lane);
+    fetch<D, K>(&f, a, seq, head_at, key + 2 * K, to, wave, lane);
     __syncthreads();
   }
   join_lanes(&s);
