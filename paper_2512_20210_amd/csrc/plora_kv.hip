@@ -998,9 +998,22 @@ struct Stage {
   uint4 values[K / 32 * (D / 16)][64];  // [32 keys][16 channels]
   float ks[K], km[K], vs[K], vm[K];     // scale and min of keys; scale and min + 8 scale of values, 0 where there is no row
 };
+// The pages of a stage's two blocks of 32 keys, read a stage before they are used: -1 behind `to`.
+struct PageIds {
+  int32_t p0, p1;
+};
+template <int K>
+__device__ __forceinline__ PageIds page_ids(const AttendArgs& a, int seq, int key, int to) {
+  const int32_t* row = a.b.table + (int64_t)seq * a.b.stride;
+  PageIds p{-1, -1};
+  if (key < to) p.p0 = row[key >> a.c.page_shift];
+  if (K > kBlockTok && key + kBlockTok < to) p.p1 = row[(key + kBlockTok) >> a.c.page_shift];
+  return p;
+}
 // What a wavefront fetches of a stage.
 template <int W>
 struct Fetched {
+  bool there0, there1;  // whether its blocks have a page
   uint32_t k[W], v[W];
   uint32_t kp, vp;
 };
@@ -1020,11 +1033,11 @@ __device__ __forceinline__ void ld_words(uint32_t* o, const uint8_t* p) {
 }
 // Keys key .. key + K-1 (behind `to` and in holes: anything, with a value's scale and min 0).
 template <int D, int K, int W>
-__device__ __forceinline__ void fetch(Fetched<W>* o, const AttendArgs& a, int seq, int64_t head_at, int key, int to, int wave, int lane) {
+__device__ __forceinline__ void fetch(Fetched<W>* o, const AttendArgs& a, PageIds ids, int64_t head_at, int key, int to, int wave, int lane) {
   const int r = lane & 15, g = lane >> 4, pt = a.c.page_tokens;
-  const uint8_t* p0 = key < to ? page_of(a.c, a.b, seq, key) : nullptr;
-  const uint8_t* p1 = K > kBlockTok && key + kBlockTok < to ? page_of(a.c, a.b, seq, key + kBlockTok) : nullptr;
-  const uint8_t *h0 = (p0 ? p0 : a.c.pages) + head_at, *h1 = (p1 ? p1 : a.c.pages) + head_at;
+  o->there0 = (uint32_t)ids.p0 < (uint32_t)a.c.n_pages;
+  o->there1 = (uint32_t)ids.p1 < (uint32_t)a.c.n_pages;
+  const uint8_t *h0 = a.c.pages + (o->there0 ? ids.p0 : 0) * a.c.page_bytes + head_at, *h1 = a.c.pages + (o->there1 ? ids.p1 : 0) * a.c.page_bytes + head_at;
   const int slot0 = key & (pt - 1), slot1 = (key + kBlockTok) & (pt - 1);
   {
     const int tile = wave * W / (D / 32), i0 = wave * W % (D / 32);
@@ -1039,7 +1052,7 @@ __device__ __forceinline__ void fetch(Fetched<W>* o, const AttendArgs& a, int se
   if (wave == 0) {
     const bool second = K > kBlockTok && lane >= kBlockTok;
     const uint8_t* h = (second ? h1 + slot1 * 4 : h0 + slot0 * 4) + pt * D + (lane & (kBlockTok - 1)) * 4;
-    const bool there = (second ? p1 : p0) && key + lane < to;
+    const bool there = (second ? o->there1 : o->there0) && key + lane < to;
     o->kp = *reinterpret_cast<const uint32_t*>(h);
     o->vp = *reinterpret_cast<const uint32_t*>(h + pt * 4);
     o->vp = there ? o->vp : 0u;
@@ -1135,6 +1148,11 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
 #pragma unroll
     for (int n = 0; n < 8; ++n) top = fmaxf(top, w[j][n]);
   }
+  // the first operands of the second product are on their way before the branch
+  constexpr int kAhead = 4;
+  f16x8 vc[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) vc[i] = __builtin_bit_cast(f16x8, b.values[block * (D / 16) + i][lane]);
   if (__any(top > 0x1p15f)) {  // (a NaN is none: it stays where it is)
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
@@ -1175,11 +1193,12 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
   }
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
-    const f16x8 vc = __builtin_bit_cast(f16x8, b.values[block * (D / 16) + i][lane]);
+    const f16x8 v = vc[i % kAhead];
+    if (i + kAhead < D / 16) vc[i % kAhead] = __builtin_bit_cast(f16x8, b.values[block * (D / 16) + i + kAhead][lane]);
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
 #pragma unroll
-      for (int h = HW - 1; h >= 0; --h) s->o[j][i] = mfma(vc, wb[j][h].v, s->o[j][i]);
+      for (int h = HW - 1; h >= 0; --h) s->o[j][i] = mfma(v, wb[j][h].v, s->o[j][i]);
     }
   }
 }
@@ -1216,7 +1235,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
   const int r0 = w0 + wave * R, r1 = r0 + R < w1 ? r0 + R : w1;  // rows of the wavefront: none if r0 >= r1
   const CodeBits bits = code_bits();
   Fetched<W> f;
-  fetch<D, K>(&f, a, seq, head_at, from, to, wave, lane);
+  fetch<D, K>(&f, a, page_ids<K>(a, seq, from, to), head_at, from, to, wave, lane);
+  PageIds ids = page_ids<K>(a, seq, from + K, to);
   Queries<D, NQ, LOW_IN_LDS ? 1 : HQ> q;
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
@@ -1231,7 +1251,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
   }
   __syncthreads();
   unpack<D, K>(&lds.stage[0], f, bits, wave, lane);
-  fetch<D, K>(&f, a, seq, head_at, from + K, to, wave, lane);
+  bool there0 = f.there0, there1 = f.there1;
+  fetch<D, K>(&f, a, ids, head_at, from + K, to, wave, lane);
+  ids = page_ids<K>(a, seq, from + 2 * K, to);
   __syncthreads();
   Sums<D, NQ> s;
   clear(&s);
@@ -1244,12 +1266,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
       const int key0 = key + block * kBlockTok;
       if (key0 < to && r0 < r1 && key0 <= last && (!a.window || key0 + kBlockTok - 1 > first - a.window)) {
         const bool whole = key0 + kBlockTok <= to && key0 + kBlockTok - 1 <= first && (!a.window || key0 > last - a.window);
-        if (page_of(a.c, a.b, seq, key0)) step32<D, NQ, HQ, HW, K, LOW_IN_LDS>(lds.stage[at], block, q, low[LOW_IN_LDS ? wave : 0], &s, whole, key0, to, a.window, lane);
+        if (block ? there1 : there0) step32<D, NQ, HQ, HW, K, LOW_IN_LDS>(lds.stage[at], block, q, low[LOW_IN_LDS ? wave : 0], &s, whole, key0, to, a.window, lane);
       }
     }
     at ^= 1;
-    if (key + K < to) unpack<D, K>(&lds.stage[at], f, bits, wave, lane);
-    fetch<D, K>(&f, a, seq, head_at, key + 2 * K, to, wave, lane);
+    unpack<D, K>(&lds.stage[at], f, bits, wave, lane);
+    there0 = f.there0;
+    there1 = f.there1;
+    fetch<D, K>(&f, a, ids, head_at, key + 2 * K, to, wave, lane);
+    ids = page_ids<K>(a, seq, key + 3 * K, to);
     __syncthreads();
   }
   join_lanes(&s);
