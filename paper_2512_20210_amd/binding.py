@@ -715,22 +715,38 @@ def plora_kv_attend(cache, batch, n_heads, q, out, scale, causal=1, window=0, ro
     return lib.plora_kv_attend(cache, batch, n_heads, q, out, scale, int(causal), int(window), rotary, workspace_ptr, workspace_bytes, stream)
 
 
-_TORCH_DTYPE = {"torch.float16": PLORA_F16, "torch.bfloat16": PLORA_BF16, "torch.float32": PLORA_F32}
+_INT32 = 100
+_DTYPE_NAMES = {"torch.float16": PLORA_F16, "torch.bfloat16": PLORA_BF16, "torch.float32": PLORA_F32, "torch.int32": _INT32}
+_dtypes = {}  # torch dtype object -> plora_dtype, _INT32, or -1 for others (filled as they are met: this module does without torch)
+
+
+def _dtype_of(t):
+    d = t.dtype
+    code = _dtypes.get(d)
+    if code is None:
+        code = _dtypes[d] = _DTYPE_NAMES.get(str(d), -1)
+    return code
 
 
 def _rows_of(call, t, n_tokens, heads, head_dim, dtype):
     """plora_rows of a torch tensor [tokens, heads, head_dim] (any strides the library takes, the last one 1)."""
-    if t.dim() != 3 or t.shape[0] != n_tokens or (heads and t.shape[1] != heads) or t.shape[2] != head_dim or (head_dim > 1 and t.stride(2) != 1) or \
-            _TORCH_DTYPE.get(str(t.dtype)) != dtype or not t.is_cuda:
+    st = t.stride()
+    if t.shape != (n_tokens, heads, head_dim) or st[2] != 1 or _dtype_of(t) != dtype or not t.is_cuda:
         raise PloraError(call, PLORA_ERR_INVAL)
-    return RowsStruct(t.data_ptr(), t.stride(0), t.stride(1))
+    return RowsStruct(t.data_ptr(), st[0], st[1])
 
 
 def _ints_of(call, t, least):
     """Device pointer of a contiguous int32 torch tensor of at least that many entries."""
-    if str(t.dtype) != "torch.int32" or not t.is_contiguous() or t.numel() < least or not t.is_cuda:
+    if _dtype_of(t) != _INT32 or not t.is_contiguous() or t.numel() < least or not t.is_cuda:
         raise PloraError(call, PLORA_ERR_INVAL)
     return t.data_ptr()
+
+
+def _three(call, t):
+    if t.dim() != 3:
+        raise PloraError(call, PLORA_ERR_INVAL)
+    return t.shape
 
 
 class Rotary:
@@ -752,10 +768,13 @@ class Rotary:
 
     def rotate(self, positions, x, out, inverse=False, stream=None):
         """out = x [tokens, heads, head_dim] rotated by positions (int32 [tokens]); out may be x."""
-        n, heads, d = x.shape
-        dtype = _TORCH_DTYPE.get(str(x.dtype), -1)
-        _check("plora_rotate", plora_rotate(self.c, dtype, n, heads, d, _ints_of("plora_rotate", positions, n), _rows_of("plora_rotate", x, n, heads, d, dtype),
-                                            _rows_of("plora_rotate", out, n, heads, d, dtype), inverse, stream))
+        n, heads, d = _three("plora_rotate", x)
+        dtype = _dtype_of(x)
+        rows = _rows_of("plora_rotate", x, n, heads, d, dtype)
+        rc = lib.plora_rotate(self.c, dtype, n, heads, d, _ints_of("plora_rotate", positions, n), rows, rows if out is x else _rows_of("plora_rotate", out, n, heads, d, dtype),
+                              inverse, stream)
+        if rc:
+            _check("plora_rotate", rc)
         return out
 
 
@@ -794,23 +813,30 @@ class PagedKvCache:
 
     def append(self, batch, k, v, rotary=None, stream=None):
         """k, v: [tokens, kv heads, head_dim]; rotary: applied to k."""
-        call = "plora_kv_append"
-        _check(call, plora_kv_append(self.c, batch.c, self._rows(call, batch, k), self._rows(call, batch, v), None if rotary is None else rotary.c, stream))
+        rc = lib.plora_kv_append(self.c, batch.c, self._rows("plora_kv_append", batch, k), self._rows("plora_kv_append", batch, v),
+                                 None if rotary is None else rotary.c, stream)
+        if rc:
+            _check("plora_kv_append", rc)
 
     def read(self, batch, k, v, stream=None):
-        call = "plora_kv_read"
-        _check(call, plora_kv_read(self.c, batch.c, self._rows(call, batch, k), self._rows(call, batch, v), stream))
+        rc = lib.plora_kv_read(self.c, batch.c, self._rows("plora_kv_read", batch, k), self._rows("plora_kv_read", batch, v), stream)
+        if rc:
+            _check("plora_kv_read", rc)
 
     def attend(self, batch, q, out, scale, workspace=None, causal=True, window=0, rotary=None, stream=None):
         """q, out: [tokens, heads, head_dim]; workspace: any contiguous tensor on the GPU, or None; rotary: applied to q."""
         call = "plora_kv_attend"
-        heads = q.shape[1]
-        rows = [_rows_of(call, t, batch.n_tokens, heads, self.head_dim, self.dtype) for t in (q, out)]
-        size = 0
+        n, heads, d = _three(call, q)
+        if d != self.head_dim or n != batch.n_tokens:
+            raise PloraError(call, PLORA_ERR_INVAL)
+        ws, size = None, 0
         if workspace is not None:
             if not workspace.is_contiguous() or not workspace.is_cuda:
                 raise PloraError(call, PLORA_ERR_INVAL)
-            size = workspace.numel() * workspace.element_size()
-        _check(call, plora_kv_attend(self.c, batch.c, heads, rows[0], rows[1], scale, causal, window, None if rotary is None else rotary.c,
-                                     workspace.data_ptr() if size else None, size, stream))
+            size = workspace.nbytes
+            ws = workspace.data_ptr() if size else None
+        rc = lib.plora_kv_attend(self.c, batch.c, heads, _rows_of(call, q, n, heads, d, self.dtype), _rows_of(call, out, n, heads, d, self.dtype), scale,
+                                 causal, window, None if rotary is None else rotary.c, ws, size, stream)
+        if rc:
+            _check(call, rc)
         return out

@@ -115,32 +115,42 @@ __device__ __forceinline__ float turn_b(float a, float b, float2 cs) {
   return b * cs.x + a * cs.y;
 }
 
+// How groups of 8 channels are rotated: not at all; with a partner group (half-split layout); within themselves (interleaved
+// layout); element by element, where a pair crosses groups.  One kind holds for a whole launch, so kernels branch on it once,
+// outside their loops, and the loads of a loop go out together.
+enum RotaryKind { kPlain, kHalf, kWithin, kElements };
+__device__ __forceinline__ RotaryKind kind_of(const Rotary& r) {
+  return !r.table ? kPlain : r.interleaved ? ((r.rot & 7) == 0 ? kWithin : kElements) : ((r.rot & 15) == 0 ? kHalf : kElements);
+}
 // Channels c0 .. c0+7 of a row (c0 a multiple of 8), rotated.  The partners of a half-split rotation are read along: a second
 // trip to lines that the neighbouring lanes read anyway.
-template <int DT>
+template <int DT, RotaryKind KIND>
 __device__ __forceinline__ void rotated8(const uint8_t* row, int c0, const Rotary& r, const Angles& cs, float* f) {
   ld8<DT>(row + (int64_t)c0 * Elt<DT>::B, f);
-  if (!r.table || c0 >= r.rot) return;
   const int half = r.rot >> 1;
-  if (r.interleaved && (r.rot & 7) == 0) {
+  if constexpr (KIND == kWithin) {
+    const bool in = c0 < r.rot;
+    const int j0 = in ? c0 >> 1 : 0;
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      const float2 w = cs[(c0 + i) >> 1];
-      const float a = f[i], b = f[i + 1];
-      f[i] = turn_a(a, b, w);
-      f[i + 1] = turn_b(a, b, w);
+    for (int i = 0; i < 4; ++i) {
+      const float2 w = cs[j0 + i];
+      const float a = f[2 * i], b = f[2 * i + 1];
+      f[2 * i] = in ? turn_a(a, b, w) : a;
+      f[2 * i + 1] = in ? turn_b(a, b, w) : b;
     }
-  } else if (!r.interleaved && (half & 7) == 0) {
+  } else if constexpr (KIND == kHalf) {
+    const bool in = c0 < r.rot, second = c0 >= half;
+    const int j0 = in ? (second ? c0 - half : c0) : 0;
     float o[8];
-    const bool second = c0 >= half;
-    const int j0 = second ? c0 - half : c0;
-    ld8<DT>(row + (int64_t)(second ? j0 : c0 + half) * Elt<DT>::B, o);
+    ld8<DT>(row + (int64_t)(in ? (second ? j0 : c0 + half) : c0) * Elt<DT>::B, o);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float2 w = cs[j0 + i];
-      f[i] = second ? turn_b(o[i], f[i], w) : turn_a(f[i], o[i], w);
+      // b cos + a sin = b cos - a (-sin): one form for both members
+      const float v = turn_a(f[i], o[i], make_float2(w.x, second ? -w.y : w.y));
+      f[i] = in ? v : f[i];
     }
-  } else {  // pairs that cross a group of 8: element by element
+  } else if constexpr (KIND == kElements) {
     for (int i = 0; i < 8; ++i) {
       const int c = c0 + i;
       if (c >= r.rot) break;
@@ -314,102 +324,237 @@ struct CacheArgs {
   Rotary r;
 };
 
-// One workgroup, one block of 32 places of a sequence, one kv head, keys (blockIdx.z = 0) or values (1).  8 threads share a row.
-struct BlockWork {
+// What 8 threads have to do: one row of keys or values.
+struct RowWork {
   Seq s;
-  int seq, place0, a;  // first place of the block; place of the sequence's first row
+  int seq, head, place, tok;
+  bool values, mine;  // mine: the place is one of the call's, and not negative
 };
-__device__ __forceinline__ bool block_work(const Batch& b, BlockWork* w) {
+// Calls of one token a sequence: a workgroup has 32 rows, one behind the other over sequences, keys and values, heads.
+__device__ __forceinline__ bool row_of_single(const Cache& c, const Batch& b, RowWork* w) {
+  const int64_t row = (int64_t)blockIdx.x * (kThreads / 8) + (threadIdx.x >> 3);
+  const int64_t seq = row / (2 * c.heads);
+  if (seq >= b.n_seqs) return false;
+  const int rest = (int)(row - seq * (2 * c.heads));
+  w->seq = (int)seq;
+  w->values = rest >= c.heads;
+  w->head = w->values ? rest - c.heads : rest;
+  w->s = seq_at(b, w->seq);
+  w->place = w->s.len - w->s.n;
+  w->tok = w->s.first;
+  w->mine = w->s.n > 0 && w->place >= 0;
+  return w->s.n > 0;
+}
+// Other calls: a workgroup has one block of 32 places of a sequence, one kv head, keys (blockIdx.z = 0) or values (1).
+// place0: the block's first place; a: the place of the sequence's first row.
+__device__ __forceinline__ bool row_of_block(const Batch& b, RowWork* w, int* place0, int* a) {
   const int64_t number = blockIdx.x;
   w->seq = find_seq(b, number, 1, kBlockTok, 2);
   w->s = seq_at(b, w->seq);
   const int64_t k = number - first_number(b, w->seq, 1, kBlockTok, 2);
-  w->a = w->s.len - w->s.n;
-  const int from = w->a < 0 ? 0 : w->a;
-  const int64_t place0 = (int64_t)(from & ~(kBlockTok - 1)) + k * kBlockTok;
-  if (w->s.n == 0 || k < 0 || (k > 0 && place0 >= w->s.len)) return false;  // (the first block also has the rows at negative places)
-  w->place0 = (int)place0;
+  *a = w->s.len - w->s.n;
+  const int from = *a < 0 ? 0 : *a;
+  const int64_t p0 = (int64_t)(from & ~(kBlockTok - 1)) + k * kBlockTok;
+  if (w->s.n == 0 || k < 0 || (k > 0 && p0 >= w->s.len)) return false;  // (the first block also has the rows at negative places)
+  *place0 = (int)p0;
+  w->values = blockIdx.z != 0;
+  w->head = blockIdx.y;
+  w->place = *place0 + (threadIdx.x >> 3);
+  w->mine = w->place >= *a && w->place < w->s.len;
+  w->tok = w->s.first + (w->place - *a);
   return true;
 }
 
-// Word of the values' codes (of a block of 32 tokens) for channel d and token quad g.
-template <int D>
-__device__ __forceinline__ int value_word(int d, int g) {
-  const int quarter = d / (D / 4), rest = d % (D / 4), tile = rest >> 2, r = quarter * 4 + (rest & 3);
-  return ((tile >> 2) * 64 + g * 16 + r) * 4 + (tile & 3);
+// Where the codes of a thread's channels (part * D/8 ..) of a value lie: 4 groups (r % 4) of TILES words, of which up to 4 are
+// neighbours.  f(group word index, first channel of the thread in it, words): channels of a group are 4 apart.
+template <int D> struct ValueWords {
+  static constexpr int TILES = D / 32;            // tiles of a thread's channels, all in one quarter
+  static constexpr int RUN = TILES < 4 ? TILES : 4;
+  template <class F>
+  static __device__ __forceinline__ void each(int part, int g, F f) {
+    const int quarter = part >> 1, tile0 = (part & 1) * TILES;
+#pragma unroll
+    for (int rr = 0; rr < 4; ++rr) {
+#pragma unroll
+      for (int k = 0; k < TILES; k += RUN) {
+        const int tile = tile0 + k;
+        f(((tile >> 2) * 64 + g * 16 + quarter * 4 + rr) * 4 + (tile & 3), 4 * k + rr);
+      }
+    }
+  }
+};
+template <int N>
+__device__ __forceinline__ void ld_run(uint32_t* o, const uint32_t* p) {
+  if constexpr (N == 2) {
+    const uint2 q = *reinterpret_cast<const uint2*>(p);
+    o[0] = q.x;
+    o[1] = q.y;
+  } else {
+    const uint4 q = *reinterpret_cast<const uint4*>(p);
+    o[0] = q.x;
+    o[1] = q.y;
+    o[2] = q.z;
+    o[3] = q.w;
+  }
+}
+template <int N>
+__device__ __forceinline__ void st_run(uint32_t* p, const uint32_t* o) {
+  if constexpr (N == 2) *reinterpret_cast<uint2*>(p) = make_uint2(o[0], o[1]);
+  else *reinterpret_cast<uint4*>(p) = make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-template <int DT, int D>
-__global__ __launch_bounds__(kThreads) void k_append(CacheArgs a) {
-  constexpr int C = D / 8;  // channels of a thread
-  __shared__ uint32_t codes[kBlockTok][D / 8 + 1];  // values: nibbles of a row in channel order
-  BlockWork w;
-  if (!block_work(a.b, &w)) return;
-  const int head = blockIdx.y, row = threadIdx.x >> 3, part = threadIdx.x & 7;
-  const bool values = blockIdx.z != 0;
-  const int place = w.place0 + row;
-  const bool mine = place >= w.a && place < w.s.len;
-  uint8_t* page = page_of(a.c, a.b, w.seq, w.place0);
-  if (!page) return;
-  const int tok = w.s.first + (place - w.a);
-  float x[C];
-  if (mine) {
-    const Rows& src = values ? a.v : a.k;
-    const uint8_t* p = src.p + tok * src.ts + head * src.hs;
-    Rotary r = a.r;
-    if (values) r.table = nullptr;
-    Angles cs{nullptr, false};
-    if (r.table) cs = angles_at(r, a.b.positions ? a.b.positions[tok] : place);
+// Channels c0 .. c0 + C-1 of a row of keys, rotated, or of values.
+template <int DT, int C, RotaryKind KIND>
+__device__ __forceinline__ void row_part(const CacheArgs& a, const Rows& src, const RowWork& w, int c0, float* x) {
+  const uint8_t* p = src.p + w.tok * src.ts + w.head * src.hs;
+  Angles cs{nullptr, false};
+  if constexpr (KIND != kPlain) cs = angles_at(a.r, a.b.positions ? a.b.positions[w.tok] : w.place);
 #pragma unroll
-    for (int i = 0; i < C; i += 8) rotated8<DT>(p, part * C + i, r, cs, x + i);
-  } else {
-#pragma unroll
-    for (int i = 0; i < C; ++i) x[i] = 0.f;
+  for (int i = 0; i < C; i += 8) rotated8<DT, KIND>(p, c0 + i, a.r, cs, x + i);
+}
+template <int DT, int C>
+__device__ __forceinline__ void row_part(const CacheArgs& a, const RowWork& w, int c0, float* x) {
+  switch (w.values ? kPlain : kind_of(a.r)) {
+    case kPlain: row_part<DT, C, kPlain>(a, w.values ? a.v : a.k, w, c0, x); break;
+    case kHalf: row_part<DT, C, kHalf>(a, a.k, w, c0, x); break;
+    case kWithin: row_part<DT, C, kWithin>(a, a.k, w, c0, x); break;
+    default: row_part<DT, C, kElements>(a, a.k, w, c0, x); break;
   }
-  float lo = x[0], hi = x[0];
-  uint32_t big = 0;
+}
+
+// The 4-bit form of a row of which 8 threads have C channels each: codes (8 a word) and scale, min.
+template <int C>
+__device__ __forceinline__ uint32_t quantise(const float* x, uint32_t* word) {
+#pragma clang fp contract(off)
+  float lo = x[0], hi = x[0], none = 0.f;
 #pragma unroll
   for (int i = 0; i < C; ++i) {
     lo = fminf(lo, x[i]);
     hi = fmaxf(hi, x[i]);
-    const uint32_t m = __float_as_uint(x[i]) & 0x7fffffffu;
-    big = m > big ? m : big;
+    none = __builtin_fmaf(x[i], 0.f, none);  // NaN if any value is not finite
   }
 #pragma unroll
   for (int d = 1; d < 8; d <<= 1) {
     lo = fminf(lo, __shfl_xor(lo, d));
     hi = fmaxf(hi, __shfl_xor(hi, d));
-    const uint32_t m = __shfl_xor(big, d);
-    big = m > big ? m : big;
+    none += __shfl_xor(none, d);
   }
   // scale and min are kept in bf16; the codes are chosen against what is kept
   const uint32_t sm = pack_bf16((hi - lo) / 15.0f, lo);
-  float s = __uint_as_float(sm << 16), m = __uint_as_float(sm & 0xffff0000u);
-  const bool fine = big < 0x7f800000u && fabsf(s) < INFINITY && fabsf(m) < INFINITY;
+  float s = __uint_as_float(sm << 16);
+  const float m = __uint_as_float(sm & 0xffff0000u);
+  const bool fine = none == 0.f && fabsf(s) < INFINITY && fabsf(m) < INFINITY;
   if (s < 0x1p-100f) s = 0.f;
-  // (x - min) / scale rounded as by a division: quotient by the reciprocal, then one correction by the remainder
+  // (x - min) / scale rounded as by a division: the quotient by the reciprocal, and one correction by its remainder
   const float inv = s > 0.f ? 1.0f / s : 0.f;
-  uint32_t word[C / 8];
 #pragma unroll
   for (int i = 0; i < C / 8; ++i) {
-    word[i] = 0;
+    float half[2];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float d = x[8 * i + k] - m;
-      float q = d * inv;
-      q = __builtin_fmaf(__builtin_fmaf(-q, s, d), inv, q);
-      q = fminf(fmaxf(rintf(q), 0.f), 15.f);
-      word[i] |= (uint32_t)q << (4 * k);
+    for (int h = 0; h < 2; ++h) {
+      float sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float d = x[8 * i + 4 * h + k] - m;
+        float q = d * inv;
+        q = __builtin_fmaf(__builtin_fmaf(-q, s, d), inv, q);
+        q = __builtin_amdgcn_fmed3f(__builtin_rintf(q), 0.f, 15.f);
+        sum = __builtin_fmaf(q, (float)(1 << (4 * k)), sum);  // whole numbers below 2^16: exact
+      }
+      half[h] = sum;
     }
-    if (!fine) word[i] = 0;
+    word[i] = fine ? (uint32_t)half[0] | (uint32_t)half[1] << 16 : 0u;
   }
-  const uint32_t params = fine ? (__float_as_uint(s) >> 16) | (sm & 0xffff0000u) : 0x7fc07fc0u;
-  const int pt = a.c.page_tokens, slot0 = w.place0 & (pt - 1), slot = slot0 + row;
-  uint8_t* hp = page + (int64_t)head * pt * (D + 8);
-  if (mine && part == 0)
-    reinterpret_cast<uint32_t*>(hp + (int64_t)pt * D)[(values ? pt : 0) + slot] = params;
-  if (!values) {
-    if (mine) {
+  return fine ? (__float_as_uint(s) >> 16) | (sm & 0xffff0000u) : 0x7fc07fc0u;
+}
+
+// Bound by the latency of its chain (first rows and lengths, page, row and angles, the values' words that it changes one nibble of).
+template <int DT, int D>
+__global__ __launch_bounds__(kThreads) void k_append_single(CacheArgs a) {
+  constexpr int C = D / 8, RUN = ValueWords<D>::RUN;
+  RowWork w;
+  if (!row_of_single(a.c, a.b, &w) || !w.mine) return;
+  const int part = threadIdx.x & 7;
+  uint8_t* page = page_of(a.c, a.b, w.seq, w.place);
+  float x[C];
+  row_part<DT, C>(a, w, part * C, x);
+  if (!page) return;
+  const int pt = a.c.page_tokens, slot = w.place & (pt - 1);
+  uint8_t* hp = page + (int64_t)w.head * pt * (D + 8);
+  const int u = slot & (kBlockTok - 1), g = (u & 15) >> 2, shift = 4 * ((u & 3) + (u >> 4) * 4);
+  uint32_t* vw = reinterpret_cast<uint32_t*>(hp + (int64_t)pt * (D / 2) + (slot / kBlockTok) * (16 * D));
+  uint32_t old[C];  // (of values: asked for ahead of the choice of codes)
+  if (w.values) ValueWords<D>::each(part, g, [&](int at, int c) {
+    ld_run<RUN>(&old[(c & 3) * ValueWords<D>::TILES + (c >> 2)], vw + at);
+  });
+  uint32_t word[C / 8];
+  const uint32_t params = quantise<C>(x, word);
+  if (part == 0) reinterpret_cast<uint32_t*>(hp + (int64_t)pt * D)[(w.values ? pt : 0) + slot] = params;
+  if (!w.values) {
+#pragma unroll
+    for (int i = 0; i < C / 8; ++i) reinterpret_cast<uint32_t*>(hp + slot * (D / 2))[part * (C / 8) + i] = word[i];
+  } else {
+    ValueWords<D>::each(part, g, [&](int at, int c) {
+      uint32_t* o = &old[(c & 3) * ValueWords<D>::TILES + (c >> 2)];
+#pragma unroll
+      for (int i = 0; i < RUN; ++i) {
+        const int ch = c + 4 * i;
+        o[i] = (o[i] & ~(15u << shift)) | ((word[ch >> 3] >> (4 * (ch & 7))) & 15u) << shift;
+      }
+      st_run<RUN>(vw + at, o);
+    });
+  }
+}
+
+// Word n of 8 has nibble c: afterwards word c has nibble n.
+__device__ __forceinline__ void transpose_nibbles(uint32_t* w) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {  // halves of words 4 apart
+    const uint32_t a = w[i], b = w[i + 4];
+    w[i] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+    w[i + 4] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {  // bytes of words 2 apart
+    const int i = (k & 1) + (k >> 1) * 4;
+    const uint32_t a = w[i], b = w[i + 2];
+    w[i] = __builtin_amdgcn_perm(b, a, 0x06020400u);
+    w[i + 2] = __builtin_amdgcn_perm(b, a, 0x07030501u);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {  // nibbles of neighbours
+    const uint32_t a = w[i], b = w[i + 1];
+    w[i] = (a & 0x0f0f0f0fu) | (b << 4 & 0xf0f0f0f0u);
+    w[i + 1] = (a >> 4 & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u);
+  }
+}
+
+// Values: codes of 32 rows through LDS, then one thread takes 8 channels of the 8 tokens of a quad and transposes them into 8
+// words.  Words of which only some tokens are the call's are read first.
+template <int DT, int D>
+__global__ __launch_bounds__(kThreads) void k_append(CacheArgs a) {
+  constexpr int C = D / 8;
+  __shared__ uint32_t codes[kBlockTok][D / 8 + 1];
+  RowWork w;
+  int place0, from;
+  if (!row_of_block(a.b, &w, &place0, &from)) return;
+  const int row = threadIdx.x >> 3, part = threadIdx.x & 7;
+  uint8_t* page = page_of(a.c, a.b, w.seq, place0);
+  if (!page) return;
+  float x[C];
+  if (w.mine) {
+    row_part<DT, C>(a, w, part * C, x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < C; ++i) x[i] = 0.f;
+  }
+  uint32_t word[C / 8];
+  const uint32_t params = quantise<C>(x, word);
+  const int pt = a.c.page_tokens, slot0 = place0 & (pt - 1), slot = slot0 + row;
+  uint8_t* hp = page + (int64_t)w.head * pt * (D + 8);
+  if (w.mine && part == 0) reinterpret_cast<uint32_t*>(hp + (int64_t)pt * D)[(w.values ? pt : 0) + slot] = params;
+  if (!w.values) {
+    if (w.mine) {
 #pragma unroll
       for (int i = 0; i < C / 8; ++i) reinterpret_cast<uint32_t*>(hp + slot * (D / 2))[part * (C / 8) + i] = word[i];
     }
@@ -418,64 +563,83 @@ __global__ __launch_bounds__(kThreads) void k_append(CacheArgs a) {
 #pragma unroll
   for (int i = 0; i < C / 8; ++i) codes[row][part * (C / 8) + i] = word[i];
   __syncthreads();
-  // nibbles of the block that are written: token 16 * (n/4) + 4g + n%4
-  const int first = w.a > w.place0 ? w.a - w.place0 : 0, last = w.s.len - w.place0 < kBlockTok ? w.s.len - w.place0 : kBlockTok;
-  uint32_t* out = reinterpret_cast<uint32_t*>(hp + (int64_t)pt * (D / 2) + (slot0 / kBlockTok) * (16 * D));
-  for (int i = threadIdx.x; i < 4 * D; i += kThreads) {
-    const int tile = (i & 3) + (i >> 8) * 4, l = (i >> 2) & 63, g = l >> 4, r = l & 15;
-    const int d = (r >> 2) * (D / 4) + tile * 4 + (r & 3);
-    uint32_t v = 0, mask = 0;
+  if (threadIdx.x >= D / 2) return;
+  const int g = threadIdx.x & 3, group = threadIdx.x >> 2;  // tokens 4g .. and 16 + 4g .., channels 8 * group ..
+  const int first = from > place0 ? from - place0 : 0, last = w.s.len - place0 < kBlockTok ? w.s.len - place0 : kBlockTok;
+  uint32_t o[8], mask = 0;
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      const int t = 16 * (n >> 2) + 4 * g + (n & 3);
-      v |= ((codes[t][d >> 3] >> (4 * (d & 7))) & 15u) << (4 * n);
-      mask |= t >= first && t < last ? 15u << (4 * n) : 0u;
+  for (int n = 0; n < 8; ++n) {
+    const int t = 16 * (n >> 2) + 4 * g + (n & 3);
+    o[n] = codes[t][group];
+    mask |= t >= first && t < last ? 15u << (4 * n) : 0u;
+  }
+  if (!mask) return;
+  transpose_nibbles(o);
+  // channels 8 * group .. are the tiles 2h and 2h + 1 of a quarter: their words lie side by side
+  const int c = 8 * group, quarter = c / (D / 4), tile = c % (D / 4) >> 2;
+  uint32_t* out = reinterpret_cast<uint32_t*>(hp + (int64_t)pt * (D / 2) + (slot0 / kBlockTok) * (16 * D)) + ((tile >> 2) * 64 + g * 16 + quarter * 4) * 4 + (tile & 3);
+#pragma unroll
+  for (int rr = 0; rr < 4; ++rr) {
+    uint2* p = reinterpret_cast<uint2*>(out + 4 * rr);
+    uint2 v = make_uint2(o[rr], o[4 + rr]);
+    if (mask != 0xffffffffu) {
+      const uint2 old = *p;
+      v.x = (old.x & ~mask) | (v.x & mask);
+      v.y = (old.y & ~mask) | (v.y & mask);
     }
-    if (mask == 0xffffffffu) out[i] = v;
-    else if (mask) out[i] = (out[i] & ~mask) | (v & mask);
+    *p = v;
   }
 }
 
-template <int DT, int D>
+template <int DT, int D, bool SINGLE>
 __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
-  constexpr int C = D / 8;
-  BlockWork w;
-  const int head = blockIdx.y, row = threadIdx.x >> 3, part = threadIdx.x & 7;
-  const bool values = blockIdx.z != 0;
-  if (!block_work(a.b, &w)) return;
-  const Rows& dst = values ? a.v : a.k;
+  constexpr int C = D / 8, RUN = ValueWords<D>::RUN;
+  RowWork w;
+  const int part = threadIdx.x & 7;
   float x[C];
-  if (w.place0 == 0 && w.a < 0) {  // rows ahead of the first place
-    for (int j = row; j < -w.a && j < w.s.n; j += kBlockTok) {
 #pragma unroll
-      for (int i = 0; i < C; ++i) x[i] = __builtin_nanf("");
+  for (int i = 0; i < C; ++i) x[i] = __builtin_nanf("");
+  auto put = [&](const Rows& dst, int tok) {
+    uint8_t* out = dst.p + tok * dst.ts + w.head * dst.hs + part * C * Elt<DT>::B;
 #pragma unroll
-      for (int i = 0; i < C; i += 8) st8<DT>(dst.p + (w.s.first + j) * dst.ts + head * dst.hs + (part * C + i) * Elt<DT>::B, x + i);
-    }
-  }
-  const int place = w.place0 + row;
-  if (place < w.a || place >= w.s.len) return;
-  const uint8_t* page = page_of(a.c, a.b, w.seq, w.place0);
-  uint8_t* out = dst.p + (w.s.first + (place - w.a)) * dst.ts + head * dst.hs + part * C * Elt<DT>::B;
-  if (page) {
-    const int pt = a.c.page_tokens, slot = place & (pt - 1);
-    const uint8_t* hp = page + (int64_t)head * pt * (D + 8);
-    const uint32_t params = reinterpret_cast<const uint32_t*>(hp + (int64_t)pt * D)[(values ? pt : 0) + slot];
-    const float s = __uint_as_float(params << 16), m = __uint_as_float(params & 0xffff0000u);
-    const uint32_t* kw = reinterpret_cast<const uint32_t*>(hp + slot * (D / 2)) + part * (C / 8);
-    const uint32_t* vw = reinterpret_cast<const uint32_t*>(hp + (int64_t)pt * (D / 2) + (slot / kBlockTok) * (16 * D));
-    const int u = slot & (kBlockTok - 1), g = (u & 15) >> 2, nib = (u & 3) + (u >> 4) * 4;
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-      const uint32_t code = values ? vw[value_word<D>(part * C + i, g)] >> (4 * nib) : kw[i >> 3] >> (4 * (i & 7));
-      x[i] = m + s * (float)(code & 15u);  // the product is exact: 12 bits at most
-    }
+    for (int i = 0; i < C; i += 8) st8<DT>(out + i * Elt<DT>::B, x + i);
+  };
+  if constexpr (SINGLE) {
+    if (!row_of_single(a.c, a.b, &w)) return;
   } else {
-#pragma unroll
-    for (int i = 0; i < C; ++i) x[i] = __builtin_nanf("");
+    int place0, from;
+    if (!row_of_block(a.b, &w, &place0, &from)) return;
+    if (place0 == 0 && from < 0) {  // rows ahead of the first place
+      for (int j = threadIdx.x >> 3; j < -from && j < w.s.n; j += kBlockTok) put(w.values ? a.v : a.k, w.s.first + j);
+    }
+    if (!w.mine) return;
   }
+  const uint8_t* page = w.mine ? page_of(a.c, a.b, w.seq, w.place) : nullptr;
+  if (page) {
+    const int pt = a.c.page_tokens, slot = w.place & (pt - 1);
+    const uint8_t* hp = page + (int64_t)w.head * pt * (D + 8);
+    const uint32_t params = reinterpret_cast<const uint32_t*>(hp + (int64_t)pt * D)[(w.values ? pt : 0) + slot];
+    const float s = __uint_as_float(params << 16), m = __uint_as_float(params & 0xffff0000u);
+    if (!w.values) {
+      const uint32_t* kw = reinterpret_cast<const uint32_t*>(hp + slot * (D / 2)) + part * (C / 8);
 #pragma unroll
-  for (int i = 0; i < C; i += 8) st8<DT>(out + i * Elt<DT>::B, x + i);
+      for (int i = 0; i < C / 8; ++i) {
+        const uint32_t q = kw[i];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[8 * i + k] = m + s * (float)(q >> (4 * k) & 15u);  // the product is exact: 12 bits at most
+      }
+    } else {
+      const uint32_t* vw = reinterpret_cast<const uint32_t*>(hp + (int64_t)pt * (D / 2) + (slot / kBlockTok) * (16 * D));
+      const int u = slot & (kBlockTok - 1), g = (u & 15) >> 2, shift = 4 * ((u & 3) + (u >> 4) * 4);
+      ValueWords<D>::each(part, g, [&](int at, int c) {
+        uint32_t q[RUN];
+        ld_run<RUN>(q, vw + at);
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) x[c + 4 * i] = m + s * (float)(q[i] >> shift & 15u);
+      });
+    }
+  }
+  put(w.values ? a.v : a.k, w.tok);
 }
 
 // ---- attention ----------------------------------------------------------------------------------------
@@ -561,21 +725,28 @@ struct QueryRows {
   float sum[R];  // of the scaled row
   float f[R];    // scale * log2(e) / the row's power of two
 };
-// `threads` threads (whole wavefronts, or half of one) stage rows r0 .. r0 + R-1 of a sequence; behind the last row, that one again.
-template <int DT, int D, int HQ, int R>
-__device__ __forceinline__ void stage_queries(QueryRows<D, HQ, R>* o, const AttendArgs& a, const Seq& s, int kvh, int r0, int rows, int thread, int threads) {
+// THREADS threads (whole wavefronts) stage rows r0 .. r0 + R-1 of a sequence; behind the last row, that one again.
+template <int DT, int D, int HQ, int R, int THREADS, RotaryKind KIND>
+__device__ __forceinline__ void stage_queries_of(QueryRows<D, HQ, R>* o, const AttendArgs& a, const Seq& s, int kvh, int r0, int rows, int thread) {
   constexpr int T = D / 8;  // threads of a row
-  for (int i = thread; i < R * T; i += threads) {
-    const int row = i / T, part = i - row * T;
+  constexpr int N = (R * T + THREADS - 1) / THREADS;
+  float x[N][8];
+  const int part = thread % T;
+#pragma unroll
+  for (int n = 0; n < N; ++n) {  // (threads behind the last row read it along, so that no load waits for a branch)
+    const int row = (thread + n * THREADS) / T;
     const int rr = r0 + row < rows ? r0 + row : rows - 1;
     const int t = rr / a.rep, h = kvh * a.rep + rr - t * a.rep, tok = s.first + t;
     Angles cs{nullptr, false};
-    if (a.r.table) cs = angles_at(a.r, a.b.positions ? a.b.positions[tok] : s.len - s.n + t);
-    float x[8];
-    rotated8<DT>(a.q.p + tok * a.q.ts + h * a.q.hs, part * 8, a.r, cs, x);
+    if constexpr (KIND != kPlain) cs = angles_at(a.r, a.b.positions ? a.b.positions[tok] : s.len - s.n + t);
+    rotated8<DT, KIND>(a.q.p + tok * a.q.ts + h * a.q.hs, part * 8, a.r, cs, x[n]);
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int row = (thread + n * THREADS) / T;
     float big = 0.f, sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) big = fmaxf(big, fabsf(x[k]));
+    for (int k = 0; k < 8; ++k) big = fmaxf(big, fabsf(x[n][k]));
 #pragma unroll
     for (int d = 1; d < T; d <<= 1) big = fmaxf(big, __shfl_xor(big, d));
     // 2^e with big * 2^e in [2^9, 2^10)
@@ -584,26 +755,37 @@ __device__ __forceinline__ void stage_queries(QueryRows<D, HQ, R>* o, const Atte
     const float up = __uint_as_float((uint32_t)(e + 127) << 23);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      x[k] *= up;
-      sum += x[k];
+      x[n][k] *= up;
+      sum += x[n][k];
     }
 #pragma unroll
     for (int d = 1; d < T; d <<= 1) sum += __shfl_xor(sum, d);
+    if (row < R) {
 #pragma unroll
-    for (int h2 = 0; h2 < HQ; ++h2) {
-      o->q[h2][row][part] = make_uint4(pack_f16(x[0], x[4]), pack_f16(x[1], x[5]), pack_f16(x[2], x[6]), pack_f16(x[3], x[7]));
-      if (h2 + 1 < HQ) {
+      for (int h2 = 0; h2 < HQ; ++h2) {
+        o->q[h2][row][part] = make_uint4(pack_f16(x[n][0], x[n][4]), pack_f16(x[n][1], x[n][5]), pack_f16(x[n][2], x[n][6]), pack_f16(x[n][3], x[n][7]));
+        if (h2 + 1 < HQ) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          asm("" : "+v"(x[k]));
-          x[k] -= (float)(_Float16)x[k];
+          for (int k = 0; k < 8; ++k) {
+            asm("" : "+v"(x[n][k]));
+            x[n][k] -= (float)(_Float16)x[n][k];
+          }
         }
       }
+      if (part == 0) {
+        o->sum[row] = sum;
+        o->f[row] = a.scale * __uint_as_float((uint32_t)(127 - e) << 23);
+      }
     }
-    if (part == 0) {
-      o->sum[row] = sum;
-      o->f[row] = a.scale * __uint_as_float((uint32_t)(127 - e) << 23);
-    }
+  }
+}
+template <int DT, int D, int HQ, int R, int THREADS>
+__device__ __forceinline__ void stage_queries(QueryRows<D, HQ, R>* o, const AttendArgs& a, const Seq& s, int kvh, int r0, int rows, int thread) {
+  switch (kind_of(a.r)) {
+    case kPlain: stage_queries_of<DT, D, HQ, R, THREADS, kPlain>(o, a, s, kvh, r0, rows, thread); break;
+    case kHalf: stage_queries_of<DT, D, HQ, R, THREADS, kHalf>(o, a, s, kvh, r0, rows, thread); break;
+    case kWithin: stage_queries_of<DT, D, HQ, R, THREADS, kWithin>(o, a, s, kvh, r0, rows, thread); break;
+    default: stage_queries_of<DT, D, HQ, R, THREADS, kElements>(o, a, s, kvh, r0, rows, thread); break;
   }
 }
 
@@ -670,9 +852,10 @@ __device__ __forceinline__ void join_lanes(Sums<D, NQ>* s) {
 template <int DT, int D>
 __device__ __forceinline__ void put8(const AttendArgs& a, bool to_out, int part, int tok, int h, int c, const float* o, float ref, float l) {
   if (to_out) {
+    const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
     float f[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) f[k] = l > 0.f || l != l ? o[k] / l : 0.f;
+    for (int k = 0; k < 8; ++k) f[k] = o[k] * inv;
     st8<DT>(a.out.p + tok * a.out.ts + h * a.out.hs + c * Elt<DT>::B, f);
   } else {
     const int64_t row = ((int64_t)part * a.b.n_tokens + tok) * a.heads + h;
@@ -939,7 +1122,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : R == 4 && DT != PLORA_F32 
   load_keys(&k, a, here, head_at, key, lane);
   load_values(&v, a, here, head_at, key, lane);
   Place64 next = place64(a, seq, key + kStep, to);
-  stage_queries<DT, D, HQ, R>(&query_rows, a, sq, kvh, 0, rows, threadIdx.x, kThreads);
+  stage_queries<DT, D, HQ, R, kThreads>(&query_rows, a, sq, kvh, 0, rows, threadIdx.x);
   __syncthreads();
   const int own_row = (lane & 15) % R;
   const Column q{query_rows.sum[own_row], query_rows.f[own_row], a.causal ? sq.len - sq.n + (own_row < rows ? own_row : rows - 1) / a.rep : 0x7fffffff};
@@ -1240,7 +1423,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
   Queries<D, NQ, LOW_IN_LDS ? 1 : HQ> q;
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
-    stage_queries<DT, D, HQ, 16>(&lds.rows[wave], a, sq, kvh, r0 + 16 * j, w1, lane, 64);
+    stage_queries<DT, D, HQ, 16, 64>(&lds.rows[wave], a, sq, kvh, r0 + 16 * j, w1, lane);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     take_queries(&q, j, lds.rows[wave], a, sq, r0 + 16 * j, w1, lane);
     if constexpr (LOW_IN_LDS) {
@@ -1291,45 +1474,68 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
   }
 }
 
-// Joins the parts of a row, in their order: D/8 threads a row.  R: rows of a tile of k_attend_many.
-template <int DT, int D, int R>
+// Joins the parts of a row.  D/8 threads have 8 channels each, G times over: group g of them takes the parts g, g + G, ..., and the
+// groups' sums are joined in their order.  R: rows of a tile of k_attend_many.
+template <int DT, int D, int R, int G>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
-  constexpr int T = D / 8;
-  const int64_t row = (int64_t)blockIdx.x * (kThreads / T) + threadIdx.x / T;
-  const int c = (threadIdx.x % T) * 8;
-  const int64_t first_row = (int64_t)blockIdx.x * (kThreads / T);
-  if (first_row >= (int64_t)a.b.n_tokens * a.heads) return;
-  // the sequence of the row: those of a workgroup's first and last row bracket it
-  int tok = (int)(row / a.heads);
-  const bool has = tok < a.b.n_tokens;
-  tok = has ? tok : a.b.n_tokens - 1;
+  constexpr int T = D / 8, ROWS = kThreads / (T * G);
+  __shared__ float so[G][ROWS][D + 4], sm[G][ROWS], sl[G][ROWS];
+  const int64_t first_row = (int64_t)blockIdx.x * ROWS, all = (int64_t)a.b.n_tokens * a.heads;
+  const int mine = threadIdx.x / (T * G), g = threadIdx.x / T % G, c = (threadIdx.x % T) * 8;
+  const int64_t row = first_row + mine < all ? first_row + mine : all - 1;
+  // the sequence of the row: from that of the workgroup's first row on
+  const int tok = (int)(row / a.heads), h = (int)(row - (int64_t)tok * a.heads);
   int seq = find_seq(a.b, first_row / a.heads, 1, 1, 0);
   while (seq + 1 < a.b.n_seqs && hold(a.b.tok_start[seq + 1], a.b.n_tokens) <= tok) ++seq;
   const Seq sq = seq_at(a.b, seq);
-  const int t = tok - sq.first, h = (int)(row - (int64_t)tok * a.heads);
-  if (!has || t < 0 || t >= sq.n) return;
-  const int kvh_row = t * a.rep + h % a.rep, rows = sq.n * a.rep;
-  const int r0 = kvh_row / R * R, r1 = r0 + R < rows ? r0 + R : rows;  // (a tile of k_attend_few is one of these too: R >= 16)
-  int lo, hi;
-  keys_of_rows(sq, a, r0, r1, &lo, &hi);
-  const int n = parts_of(a, lo, hi);
-  if (n == 1) return;
-  const int64_t at = (int64_t)tok * a.heads + h, all = (int64_t)a.b.n_tokens * a.heads;
-  const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
-  float ref = kNoRef;
-  for (int k = 0; k < n; ++k) ref = fmaxf(ref, ml[k * all + at].x);
-  float l = 0.f, o[8] = {};
-  for (int k = 0; k < n; ++k) {
-    const float2 m = ml[k * all + at];
-    const float f = __builtin_amdgcn_exp2f(m.x - ref);
-    const float4* p = reinterpret_cast<const float4*>(a.part_o + (k * all + at) * D + c);
-    const float4 u = p[0], v = p[1];
-    const float e[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-    l = __builtin_fmaf(f, m.y, l);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = __builtin_fmaf(f, e[i], o[i]);
+  const int t = tok - sq.first, rows = sq.n * a.rep;
+  int n = 1;
+  if (t >= 0 && t < sq.n) {
+    const int r0 = (t * a.rep + h % a.rep) / R * R, r1 = r0 + R < rows ? r0 + R : rows;  // (a tile of k_attend_few is one of these too: R >= 16)
+    int lo, hi;
+    keys_of_rows(sq, a, r0, r1, &lo, &hi);
+    n = parts_of(a, lo, hi);
   }
-  put8<DT, D>(a, true, 0, tok, h, c, o, ref, l);
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
+  float ref = kNoRef, l = 0.f, o[8] = {};
+  if (n > 1) {
+#pragma unroll 4
+    for (int k = g; k < n; k += G) ref = fmaxf(ref, ml[k * all + row].x);
+#pragma unroll 4
+    for (int k = g; k < n; k += G) {
+      const float2 m = ml[k * all + row];
+      const float f = __builtin_amdgcn_exp2f(m.x - ref);
+      const float4* p = reinterpret_cast<const float4*>(a.part_o + (k * all + row) * D + c);
+      const float4 u = p[0], v = p[1];
+      const float e[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+      l = __builtin_fmaf(f, m.y, l);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = __builtin_fmaf(f, e[i], o[i]);
+    }
+  }
+  if constexpr (G > 1) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) so[g][mine][c + i] = o[i];
+    if (c == 0) {
+      sm[g][mine] = ref;
+      sl[g][mine] = l;
+    }
+    __syncthreads();
+    if (g != 0) return;
+#pragma unroll
+    for (int k = 1; k < G; ++k) ref = fmaxf(ref, sm[k][mine]);
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < G; ++k) {
+      const float f = __builtin_amdgcn_exp2f(sm[k][mine] - ref);
+      l = __builtin_fmaf(f, sl[k][mine], l);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = __builtin_fmaf(f, so[k][mine][c + i], o[i]);
+    }
+  }
+  if (n > 1 && first_row + mine < all) put8<DT, D>(a, true, 0, tok, h, c, o, ref, l);
 }
 
 // ---- host side ----------------------------------------------------------------------------------------
@@ -1400,18 +1606,28 @@ int rotate(const RotateArgs& a, bool vector, plora_stream stream) {
 }
 
 template <int DT, int D>
-int append_or_read(const CacheArgs& a, bool read, plora_stream stream) {
+int append_or_read(const CacheArgs& a, bool single, bool read, plora_stream stream) {
+  if (single) {  // rows one behind the other: 26.6 -> 13 us for append and read of 256 tokens, 8 heads, against blocks of 32 places
+    const uint64_t rows = (uint64_t)a.b.n_seqs * 2 * a.c.heads;
+    return launch(read ? k_read<DT, D, true> : k_append_single<DT, D>, (rows + kThreads / 8 - 1) / (kThreads / 8), 1, 1, a, stream);
+  }
   const uint64_t blocks = (uint64_t)a.b.n_tokens / kBlockTok + 2 * (uint64_t)a.b.n_seqs;
-  return launch(read ? k_read<DT, D> : k_append<DT, D>, blocks, (unsigned)a.c.heads, 2, a, stream);
+  return launch(read ? k_read<DT, D, false> : k_append<DT, D>, blocks, (unsigned)a.c.heads, 2, a, stream);
 }
 template <int DT>
-int append_or_read(int head_dim, const CacheArgs& a, bool read, plora_stream stream) {
-  return head_dim == 64 ? append_or_read<DT, 64>(a, read, stream) : head_dim == 128 ? append_or_read<DT, 128>(a, read, stream) : append_or_read<DT, 256>(a, read, stream);
+int append_or_read(int head_dim, const CacheArgs& a, bool single, bool read, plora_stream stream) {
+  return head_dim == 64    ? append_or_read<DT, 64>(a, single, read, stream)
+         : head_dim == 128 ? append_or_read<DT, 128>(a, single, read, stream)
+                           : append_or_read<DT, 256>(a, single, read, stream);
 }
-int append_or_read(int dtype, int head_dim, const CacheArgs& a, bool read, plora_stream stream) {
-  return dtype == PLORA_BF16 ? append_or_read<PLORA_BF16>(head_dim, a, read, stream)
-         : dtype == PLORA_F16 ? append_or_read<PLORA_F16>(head_dim, a, read, stream) : append_or_read<PLORA_F32>(head_dim, a, read, stream);
+int append_or_read(const plora_kv_cache* c, const CacheArgs& a, bool single, bool read, plora_stream stream) {
+  return c->dtype == PLORA_BF16  ? append_or_read<PLORA_BF16>(c->head_dim, a, single, read, stream)
+         : c->dtype == PLORA_F16 ? append_or_read<PLORA_F16>(c->head_dim, a, single, read, stream)
+                                 : append_or_read<PLORA_F32>(c->head_dim, a, single, read, stream);
 }
+
+// Workgroups that fill the GPU, and keys that are worth a part of their own.
+constexpr int kFillFew = 768, kFillMany = 512, kLeastPart = 512;
 
 // Tiles of 16 columns of a wavefront of k_attend_many.
 template <int DT, int D> constexpr int columns_of() { return DT == PLORA_F32 || D == 256 ? 1 : 2; }
@@ -1422,18 +1638,20 @@ int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace,
   const int64_t rows = (int64_t)a.b.n_tokens * a.heads;
   if (max_new > a.b.n_tokens) max_new = a.b.n_tokens;
   const int64_t most_rows = (int64_t)max_new * a.rep;
-  const bool some_few = a.b.n_seqs > 1 || most_rows <= kMostFew, some_many = most_rows > kMostFew;
+  const bool some_many = most_rows > kMostFew;
+  // Sequences of few rows among ones of many are left to k_attend_many where they are rare and their keys not many: a launch
+  // that finds nothing to do costs 4.6 us, 1024 keys in one workgroup of the other kernel 15.
+  const bool some_few = !some_many || (a.b.n_seqs > 1 && (a.b.max_len > 1024 || a.b.n_tokens < 16 * (int64_t)a.b.n_seqs));
   // rows of a tile of k_attend_few: all that a sequence can have, or those of a single token next to sequences with many
   const int64_t tile_rows = some_many ? a.rep : most_rows;
   a.few_rows = tile_rows <= 4 ? 4 : tile_rows <= 8 ? 8 : 16;
   const uint64_t few = some_few ? (uint64_t)a.b.n_seqs * a.c.heads : 0;
   const uint64_t groups = (uint64_t)a.b.n_tokens * a.rep / R + a.b.n_seqs;
   const uint64_t many = some_many ? groups * a.c.heads : 0;
-  // parts: as many as keep the GPU's 1024 SIMDs in work, no shorter than 256 keys
   const uint64_t fit = workspace ? workspace_bytes / ((uint64_t)rows * (D + 2) * 4) : 0;
   const int64_t keys = a.window ? (a.b.max_len < a.window + (int64_t)max_new + kKeyAlign ? a.b.max_len : a.window + (int64_t)max_new + kKeyAlign) : a.b.max_len;
-  uint64_t want = (2048 + (some_many ? many : few) - 1) / (some_many ? many : few);
-  const uint64_t most = (uint64_t)(keys + 255) / 256;
+  uint64_t want = (some_many ? kFillMany + many - 1 : kFillFew + few - 1) / (some_many ? many : few);
+  const uint64_t most = (uint64_t)keys / kLeastPart;
   if (want > most) want = most;
   if (want > fit) want = fit;
   if (want > 4096) want = 4096;
@@ -1450,7 +1668,13 @@ int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace,
     if (DT == PLORA_F32 || (DT == PLORA_F16 && a.r.table)) rc = launch(k_attend_many<DT, D, NQ, 2>, many, (unsigned)a.parts, 1, a, stream);
     else rc = launch(k_attend_many<DT, D, NQ, DT == PLORA_F32 ? 2 : 1>, many, (unsigned)a.parts, 1, a, stream);
   }
-  if (rc == PLORA_OK && a.parts > 1) rc = launch(k_attend_join<DT, D, R>, (uint64_t)(rows + kThreads / (D / 8) - 1) / (kThreads / (D / 8)), 1, 1, a, stream);
+  if (rc == PLORA_OK && a.parts > 1) {
+    // threads of a row, times D/8: as many as there are parts, up to a workgroup's
+    constexpr int MOST = kThreads / (D / 8);
+    const int g = a.parts <= 4 ? 1 : a.parts <= 16 ? 4 : MOST;
+    rc = launch(g == 1 ? k_attend_join<DT, D, R, 1> : g == 4 ? k_attend_join<DT, D, R, 4> : k_attend_join<DT, D, R, MOST>,
+                ((uint64_t)rows * (g * (D / 8)) + kThreads - 1) / kThreads, 1, 1, a, stream);
+  }
   return rc;
 }
 template <int DT>
@@ -1529,7 +1753,7 @@ extern "C" int plora_kv_append(const plora_kv_cache* cache, const plora_kv_batch
   if (batch->n_tokens == 0 || batch->n_seqs == 0) return PLORA_OK;
   if (!good_rows(k, cache->dtype) || !good_rows(v, cache->dtype)) return PLORA_ERR_INVAL;
   const CacheArgs a{device_cache(cache), device_batch(cache, batch), device_rows(k, cache->dtype), device_rows(v, cache->dtype), device_rotary(rotary)};
-  return append_or_read(cache->dtype, cache->head_dim, a, false, stream);
+  return append_or_read(cache, a, batch->max_new == 1, false, stream);
 }
 
 extern "C" int plora_kv_read(const plora_kv_cache* cache, const plora_kv_batch* batch, const plora_rows* k, const plora_rows* v, plora_stream stream) {
@@ -1540,7 +1764,7 @@ extern "C" int plora_kv_read(const plora_kv_cache* cache, const plora_kv_batch* 
       !good_output(v, cache->dtype, batch->n_tokens, cache->n_kv_heads, cache->head_dim))
     return PLORA_ERR_INVAL;
   const CacheArgs a{device_cache(cache), device_batch(cache, batch), device_rows(k, cache->dtype), device_rows(v, cache->dtype), device_rotary(nullptr)};
-  return append_or_read(cache->dtype, cache->head_dim, a, true, stream);
+  return append_or_read(cache, a, batch->max_new == 1, true, stream);
 }
 
 extern "C" int plora_kv_attend(const plora_kv_cache* cache, const plora_kv_batch* batch, int32_t n_heads, const plora_rows* q, const plora_rows* out,
