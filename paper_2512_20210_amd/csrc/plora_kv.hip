@@ -1389,10 +1389,10 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
 template <int DT, int D, int NQ, int HQ>
 __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
   constexpr int HW = DT == PLORA_F32 ? 2 : 1, R = 16 * NQ;
-  // Two workgroups share a CU.  Low halves of 32 rows of 128 channels do not fit the registers beside the rest; with them in LDS
-  // a stage is 32 keys.
+  // Two workgroups share a CU.  Low halves of 32 rows of 128 channels do not fit the registers beside the rest: they stay in LDS.
+  // A stage is 32 keys (64 channels: 64, a word a lane is too little to fetch): with 64 the same took 1.40 ms instead of 1.34.
   constexpr bool LOW_IN_LDS = HQ == 2 && NQ == 2 && D == 128;
-  constexpr int K = D == 256 || LOW_IN_LDS ? 32 : 64, W = Stage<D, K>::W;
+  constexpr int K = D == 64 ? 64 : 32, W = Stage<D, K>::W;
   __shared__ union {
     Stage<D, K> stage[2];
     QueryRows<D, HQ, 16> rows[kWaves];
