@@ -715,6 +715,19 @@ __device__ __forceinline__ f16x8 codes8(uint32_t w, const CodeBits& c) {
   r.p[3] = code_pair(h, 0x00f000f0u, c.high, high);
   return r.v;
 }
+// The same as 64 + code, in 7 instructions instead of 9: good for keys in the 16-bit types, where -64 sum(q) in the accumulator
+// takes the offset off again at the price of 6 of its 24 bits.  (With values it would cost bits of the weights.)
+__device__ __forceinline__ f16x8 codes8_over64(uint32_t w, const CodeBits& c) {
+  union { f16x2 p[4]; f16x8 v; } r;
+  const uint32_t s[4] = {w << 4, w, w >> 4, w >> 8};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t u;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(u) : "v"(s[i]), "s"(0x00f000f0u), "v"(c.high));
+    r.p[i] = __builtin_bit_cast(f16x2, u);
+  }
+  return r.v;
+}
 __device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 // Query rows in LDS: fp16 numbers (a high and a low half if HQ = 2) of a row times its power of two, in the order in which codes8
@@ -953,33 +966,33 @@ __device__ __forceinline__ void load_values(Values64<D, R>* o, const AttendArgs&
 
 // The row of a lane's column.
 struct Column {
-  float sum, f;
+  float sum, start, f;  // start: times sum, what the keys' offset is too much or too little
   int place;  // last place that it sees
 };
 
 // Logits of a lane's keys, less what q.f multiplies them with.
-template <int D, int R, int HQ>
+template <int D, int R, int HQ, bool OVER64>
 __device__ __forceinline__ void logits64(const Keys64<D, R>& b, const QueryRows<D, HQ, R>& rows, const Column& q, const CodeBits& bits, float* x, int lane) {
   constexpr int U = R / 4, P = 16 / R;
   const int own = (lane & 15) / R;
-  // The row is read from LDS every time: kept in registers it would cost a wavefront of occupancy.
+  // The row is read from LDS for every tile: kept in registers it would cost a wavefront of occupancy.
   const uint4* row = &rows.q[0][(lane & 15) % R][(lane >> 4) * (D / 32)];
-  asm("" : "+v"(row));
-  f16x8 qf[HQ][D / 32];
-#pragma unroll
-  for (int h = 0; h < HQ; ++h) {
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) qf[h][i] = __builtin_bit_cast(f16x8, row[h * (R * (D / 8 + 1)) + i]);
-  }
-  f32x4 t[4];
+  f32x4 c[U];
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
-    t[u] = f32x4{8.f * q.sum, 8.f * q.sum, 8.f * q.sum, 8.f * q.sum};
+    int again = 0;
+    asm volatile("" : "+v"(again));  // (no reading ahead of the loop)
+    f32x4 t = f32x4{q.start, q.start, q.start, q.start};
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
-      const f16x8 kc = codes8(b.k[u][i], bits);
+      const f16x8 kc = OVER64 ? codes8_over64(b.k[u][i], bits) : codes8(b.k[u][i], bits);
 #pragma unroll
-      for (int h = HQ - 1; h >= 0; --h) t[u] = mfma(kc, qf[h][i], t[u]);
+      for (int h = HQ - 1; h >= 0; --h) t = mfma(kc, __builtin_bit_cast(f16x8, row[again + h * (R * (D / 8 + 1)) + i]), t);
+    }
+    if (u % P == 0) c[u / P] = t;
+    else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[u / P][i] = own == u % P ? t[i] : c[u / P][i];
     }
     __builtin_amdgcn_sched_barrier(0);  // one tile's codes at a time: all at once would take 16 registers a tile
   }
@@ -988,10 +1001,7 @@ __device__ __forceinline__ void logits64(const Keys64<D, R>& b, const QueryRows<
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t kp = reinterpret_cast<const uint32_t*>(&b.kp[u])[i];
-      float c = t[P * u][i];
-#pragma unroll
-      for (int j = 1; j < P; ++j) c = own == j ? t[P * u + j][i] : c;
-      x[4 * u + i] = __builtin_fmaf(param_scale(kp), c, param_min(kp) * q.sum);
+      x[4 * u + i] = __builtin_fmaf(param_scale(kp), c[u][i], param_min(kp) * q.sum);
     }
   }
 }
@@ -1012,19 +1022,24 @@ __device__ __forceinline__ void mask64(float* x, uint4* vparams, const Column& q
   }
 }
 
-// Weights of a lane's keys, into the sums but for the values; w: times the values' scale.
+// Weights of a lane's keys, into the sums but for the values; w: times the values' scale.  (Written as a loop that is left at once
+// unless ref has to move: as a branch, the compiler copies all sums on the way that does not move it.)
 template <int D, int R>
 __device__ __forceinline__ void weights64(const uint4* vparams, const Column& q, Sums<D, 1>* s, const float* x, float* w) {
   const uint32_t* vp = reinterpret_cast<const uint32_t*>(vparams);
-  float p[R];
-  float top = 0.f;
+  float l, z;
+  for (int turn = 0;; ++turn) {  // twice at most, whatever the numbers are
+    float top = 0.f;
+    l = z = 0.f;
 #pragma unroll
-  for (int n = 0; n < R; ++n) {
-    p[n] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n], q.f, -s->ref[0]));
-    w[n] = p[n] * param_scale(vp[n]);
-    top = fmaxf(top, fmaxf(w[n], p[n] * 0x1p-90f));
-  }
-  if (__any(top > 0x1p15f)) {  // (a NaN is none: it stays where it is)
+    for (int n = 0; n < R; ++n) {
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n], q.f, -s->ref[0]));
+      w[n] = p * param_scale(vp[n]);
+      l += p;
+      z = __builtin_fmaf(p, __builtin_fmaf(8.f, param_scale(vp[n]), param_min(vp[n])), z);
+      top = fmaxf(top, w[n]);
+    }
+    if (turn || !__any(fmaxf(top, l * 0x1p-93f) > 0x1p15f)) break;  // (a NaN is none: it stays where it is)
     float best = -INFINITY;
 #pragma unroll
     for (int n = 0; n < R; ++n) {
@@ -1039,17 +1054,9 @@ __device__ __forceinline__ void weights64(const uint4* vparams, const Column& q,
     s->z[0] *= down;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) s->o[0][i] *= down;
-#pragma unroll
-    for (int n = 0; n < R; ++n) {
-      p[n] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n], q.f, -ref));
-      w[n] = p[n] * param_scale(vp[n]);
-    }
   }
-#pragma unroll
-  for (int n = 0; n < R; ++n) {
-    s->l[0] += p[n];
-    s->z[0] = __builtin_fmaf(p[n], __builtin_fmaf(8.f, param_scale(vp[n]), param_min(vp[n])), s->z[0]);
-  }
+  s->l[0] += l;
+  s->z[0] += z;
 }
 
 template <int D, int R, int HW>
@@ -1097,8 +1104,10 @@ __device__ __forceinline__ void add_values64(const uint4 (&v)[2][D / 64], float*
   }
 }
 
+// Wavefronts of a SIMD that the registers are shared among: as many as the sums and a step's rows leave room for without spills.
+template <int DT, int D, int R> constexpr int few_waves() { return D == 256 ? (R == 16 ? 1 : 2) : R == 4 ? 4 : R == 8 ? 3 : 2; }
 template <int DT, int D, int R>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : R == 4 && DT != PLORA_F32 ? 3 : 2) void k_attend_few(AttendArgs a) {
+__global__ __launch_bounds__(kThreads, (few_waves<DT, D, R>())) void k_attend_few(AttendArgs a) {
   constexpr int HQ = DT == PLORA_BF16 ? 1 : 2, HW = DT == PLORA_F32 ? 2 : 1, Y = kWaves * (16 / R);
   __shared__ QueryRows<D, HQ, R> query_rows;
   __shared__ float so[Y][R][D + 4], sm[Y][R], sl[Y][R];
@@ -1125,14 +1134,14 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : R == 4 && DT != PLORA_F32 
   stage_queries<DT, D, HQ, R, kThreads>(&query_rows, a, sq, kvh, 0, rows, threadIdx.x);
   __syncthreads();
   const int own_row = (lane & 15) % R;
-  const Column q{query_rows.sum[own_row], query_rows.f[own_row], a.causal ? sq.len - sq.n + (own_row < rows ? own_row : rows - 1) / a.rep : 0x7fffffff};
+  const Column q{query_rows.sum[own_row], (HW == 1 ? -64.f : 8.f) * query_rows.sum[own_row], query_rows.f[own_row], a.causal ? sq.len - sq.n + (own_row < rows ? own_row : rows - 1) / a.rep : 0x7fffffff};
   const CodeBits bits = code_bits();
   Sums<D, 1> s;
   clear(&s);
   const int first_place = sq.len - sq.n;
   while (key < to) {
     float x[R], w[R];
-    logits64<D, R, HQ>(k, query_rows, q, bits, x, lane);
+    logits64<D, R, HQ, HW == 1>(k, query_rows, q, bits, x, lane);
     load_keys(&k, a, next, head_at, key + kStep, lane);
     const bool whole = here.page0 && here.page1 && key + 64 <= to && (!a.causal || (key + 63 <= first_place && (!a.window || key > first_place + sq.n - 1 - a.window)));
     if (!whole) mask64<D, R>(x, v.vp, q, here, key, to, a.window, lane);
@@ -1158,7 +1167,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : R == 4 && DT != PLORA_F32 
 #pragma unroll
     for (int k = 1; k < Y; ++k) ref = fmaxf(ref, sm[k][row]);
     float l = 0.f, o[8] = {};
-#pragma unroll
+#pragma unroll 2
     for (int k = 0; k < Y; ++k) {
       const float f = __builtin_amdgcn_exp2f(sm[k][row] - ref);
       l = __builtin_fmaf(f, sl[k][row], l);
@@ -1283,7 +1292,7 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
       }
     }
   }
-  float x[NQ][8], p[NQ][8], w[NQ][8], l[NQ], z[NQ];
+  float x[NQ][8], w[NQ][8], l[NQ], z[NQ];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int at = block * kBlockTok + 16 * u + 4 * g;
@@ -1313,30 +1322,27 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
     vs[u] = *reinterpret_cast<const f32x4*>(&b.vs[at]);
     vm[u] = *reinterpret_cast<const f32x4*>(&b.vm[at]);
   }
-  float top = 0.f;
-  auto weights = [&](int j) {
-    l[j] = z[j] = 0.f;
-#pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      p[j][n] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][n], q.f[j], -s->ref[j]));
-      w[j][n] = p[j][n] * vs[n >> 2][n & 3];
-      l[j] += p[j][n];
-      z[j] = __builtin_fmaf(p[j][n], vm[n >> 2][n & 3], z[j]);
-    }
-  };
-#pragma unroll
-  for (int j = 0; j < NQ; ++j) {
-    weights(j);
-    top = fmaxf(top, l[j] * 0x1p-93f);
-#pragma unroll
-    for (int n = 0; n < 8; ++n) top = fmaxf(top, w[j][n]);
-  }
   // the first operands of the second product are on their way before the branch
   constexpr int kAhead = 4;
   f16x8 vc[kAhead];
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) vc[i] = __builtin_bit_cast(f16x8, b.values[block * (D / 16) + i][lane]);
-  if (__any(top > 0x1p15f)) {  // (a NaN is none: it stays where it is)
+  for (int turn = 0;; ++turn) {  // (as in weights64)
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+      l[j] = z[j] = 0.f;
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][n], q.f[j], -s->ref[j]));
+        w[j][n] = p * vs[n >> 2][n & 3];
+        l[j] += p;
+        z[j] = __builtin_fmaf(p, vm[n >> 2][n & 3], z[j]);
+        top = fmaxf(top, w[j][n]);
+      }
+      top = fmaxf(top, l[j] * 0x1p-93f);
+    }
+    if (turn || !__any(top > 0x1p15f)) break;
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
       float best = -INFINITY;
@@ -1353,7 +1359,6 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
       s->z[j] *= down;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) s->o[j][i] *= down;
-      weights(j);
     }
   }
   union { uint32_t u[4]; f16x8 v; } wb[NQ][HW];
@@ -1627,7 +1632,7 @@ int append_or_read(const plora_kv_cache* c, const CacheArgs& a, bool single, boo
 }
 
 // Workgroups that fill the GPU, and keys that are worth a part of their own.
-constexpr int kFillFew = 768, kFillMany = 512, kLeastPart = 512;
+constexpr int kFillFew = 1024, kFillMany = 512, kLeastPart = 512;
 
 // Tiles of 16 columns of a wavefront of k_attend_many.
 template <int DT, int D> constexpr int columns_of() { return DT == PLORA_F32 || D == 256 ? 1 : 2; }
