@@ -91,18 +91,19 @@ struct Rotary {
   int32_t max_pos, rot, interleaved;
 };
 
-// A position's row of the table; one outside it has row 0 in its place, and `ok` false: its angles are NaN.
+// A position's row of the table; one outside it has row 0 in its place, and `one` NaN instead of 1: the sines are multiplied by it.
 struct Angles {
   const float2* cs;
-  bool ok;
-  __device__ __forceinline__ float2 operator[](int j) const {
-    const float2 w = cs[j];
-    return make_float2(ok ? w.x : __builtin_nanf(""), ok ? w.y : __builtin_nanf(""));
-  }
+  float one;
 };
 __device__ __forceinline__ Angles angles_at(const Rotary& r, int32_t pos) {
   const bool ok = (uint32_t)pos < (uint32_t)r.max_pos;
-  return Angles{reinterpret_cast<const float2*>(r.table + (int64_t)(ok ? pos : 0) * r.rot), ok};
+  return Angles{reinterpret_cast<const float2*>(r.table + (int64_t)(ok ? pos : 0) * r.rot), ok ? 1.f : __builtin_nanf("")};
+}
+// cos and sin of pair j; by: 1 or -1 (exact, and the same bits as the sign changed).
+__device__ __forceinline__ float2 angle(const Angles& a, int j, float by) {
+  const float2 w = a.cs[j];
+  return make_float2(w.x, w.y * by);
 }
 // First and second member of a rotated pair; every product and sum is rounded by itself, so the same pair gives the same
 // bits wherever it is computed.
@@ -133,7 +134,7 @@ __device__ __forceinline__ void rotated8(const uint8_t* row, int c0, const Rotar
     const int j0 = in ? c0 >> 1 : 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float2 w = cs[j0 + i];
+      const float2 w = angle(cs, j0 + i, cs.one);
       const float a = f[2 * i], b = f[2 * i + 1];
       f[2 * i] = in ? turn_a(a, b, w) : a;
       f[2 * i + 1] = in ? turn_b(a, b, w) : b;
@@ -141,13 +142,13 @@ __device__ __forceinline__ void rotated8(const uint8_t* row, int c0, const Rotar
   } else if constexpr (KIND == kHalf) {
     const bool in = c0 < r.rot, second = c0 >= half;
     const int j0 = in ? (second ? c0 - half : c0) : 0;
+    const float by = second ? -cs.one : cs.one;
     float o[8];
     ld8<DT>(row + (int64_t)(in ? (second ? j0 : c0 + half) : c0) * Elt<DT>::B, o);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float2 w = cs[j0 + i];
       // b cos + a sin = b cos - a (-sin): one form for both members
-      const float v = turn_a(f[i], o[i], make_float2(w.x, second ? -w.y : w.y));
+      const float v = turn_a(f[i], o[i], angle(cs, j0 + i, by));
       f[i] = in ? v : f[i];
     }
   } else if constexpr (KIND == kElements) {
@@ -157,7 +158,7 @@ __device__ __forceinline__ void rotated8(const uint8_t* row, int c0, const Rotar
       const bool second = r.interleaved ? (c & 1) : c >= half;
       const int j = r.interleaved ? c >> 1 : (second ? c - half : c);
       const int p = r.interleaved ? c ^ 1 : (second ? j : c + half);
-      const float2 w = cs[j];
+      const float2 w = angle(cs, j, cs.one);
       const float o = ld1<DT>(row, p);
       const float me = ld1<DT>(row, c);
       const float v = second ? turn_b(o, me, w) : turn_a(me, o, w);
@@ -220,7 +221,8 @@ __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
     }
     return;
   }
-  const Angles cs = angles_at(a.r, a.positions[t]);
+  Angles cs = angles_at(a.r, a.positions[t]);
+  cs.one *= a.sign;
   const int half = a.r.rot >> 1;
   if constexpr (VECTOR) {
     float f[8], g[8];
@@ -228,8 +230,7 @@ __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
       ld8<DT>(x + u * 8 * B, f);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        float2 w = cs[u * 4 + k];
-        w.y *= a.sign;
+        const float2 w = angle(cs, u * 4 + k, cs.one);
         g[2 * k] = turn_a(f[2 * k], f[2 * k + 1], w);
         g[2 * k + 1] = turn_b(f[2 * k], f[2 * k + 1], w);
       }
@@ -239,8 +240,7 @@ __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
       ld8<DT>(x + (half + u * 8) * B, g);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        float2 w = cs[u * 8 + k];
-        w.y *= a.sign;
+        const float2 w = angle(cs, u * 8 + k, cs.one);
         const float p = f[k], q = g[k];
         f[k] = turn_a(p, q, w);
         g[k] = turn_b(p, q, w);
@@ -250,8 +250,7 @@ __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
     }
   } else {
     const int ca = a.r.interleaved ? 2 * u : u, cb = a.r.interleaved ? 2 * u + 1 : u + half;
-    float2 w = cs[u];
-    w.y *= a.sign;
+    const float2 w = angle(cs, u, cs.one);
     const float p = ld1<DT>(x, ca), q = ld1<DT>(x, cb);
     st1<DT>(y, ca, turn_a(p, q, w));
     st1<DT>(y, cb, turn_b(p, q, w));
@@ -407,7 +406,7 @@ __device__ __forceinline__ void st_run(uint32_t* p, const uint32_t* o) {
 template <int DT, int C, RotaryKind KIND>
 __device__ __forceinline__ void row_part(const CacheArgs& a, const Rows& src, const RowWork& w, int c0, float* x) {
   const uint8_t* p = src.p + w.tok * src.ts + w.head * src.hs;
-  Angles cs{nullptr, false};
+  Angles cs{nullptr, 1.f};
   if constexpr (KIND != kPlain) cs = angles_at(a.r, a.b.positions ? a.b.positions[w.tok] : w.place);
 #pragma unroll
   for (int i = 0; i < C; i += 8) rotated8<DT, KIND>(p, c0 + i, a.r, cs, x + i);
@@ -422,6 +421,12 @@ __device__ __forceinline__ void row_part(const CacheArgs& a, const RowWork& w, i
   }
 }
 
+// What the lane has that is 1, 2 or 4 (after steps 1 and 2: of lane 7 - i) away among 8.
+template <int STEP>
+__device__ __forceinline__ float of_eight(float v) {
+  constexpr int ctrl = STEP == 1 ? 0xB1 : STEP == 2 ? 0x4E : 0x141;  // quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror
+  return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), ctrl, 0xf, 0xf, true));
+}
 // The 4-bit form of a row of which 8 threads have C channels each: codes (8 a word) and scale, min.
 template <int C>
 __device__ __forceinline__ uint32_t quantise(const float* x, uint32_t* word) {
@@ -433,12 +438,15 @@ __device__ __forceinline__ uint32_t quantise(const float* x, uint32_t* word) {
     hi = fmaxf(hi, x[i]);
     none = __builtin_fmaf(x[i], 0.f, none);  // NaN if any value is not finite
   }
-#pragma unroll
-  for (int d = 1; d < 8; d <<= 1) {
-    lo = fminf(lo, __shfl_xor(lo, d));
-    hi = fmaxf(hi, __shfl_xor(hi, d));
-    none += __shfl_xor(none, d);
-  }
+  lo = fminf(lo, of_eight<1>(lo));
+  lo = fminf(lo, of_eight<2>(lo));
+  lo = fminf(lo, of_eight<4>(lo));
+  hi = fmaxf(hi, of_eight<1>(hi));
+  hi = fmaxf(hi, of_eight<2>(hi));
+  hi = fmaxf(hi, of_eight<4>(hi));
+  none += of_eight<1>(none);
+  none += of_eight<2>(none);
+  none += of_eight<4>(none);
   // scale and min are kept in bf16; the codes are chosen against what is kept
   const uint32_t sm = pack_bf16((hi - lo) / 15.0f, lo);
   float s = __uint_as_float(sm << 16);
@@ -750,7 +758,7 @@ __device__ __forceinline__ void stage_queries_of(QueryRows<D, HQ, R>* o, const A
     const int row = (thread + n * THREADS) / T;
     const int rr = r0 + row < rows ? r0 + row : rows - 1;
     const int t = rr / a.rep, h = kvh * a.rep + rr - t * a.rep, tok = s.first + t;
-    Angles cs{nullptr, false};
+    Angles cs{nullptr, 1.f};
     if constexpr (KIND != kPlain) cs = angles_at(a.r, a.b.positions ? a.b.positions[tok] : s.len - s.n + t);
     rotated8<DT, KIND>(a.q.p + tok * a.q.ts + h * a.q.hs, part * 8, a.r, cs, x[n]);
   }
@@ -915,6 +923,13 @@ __device__ __forceinline__ Place64 place64(const AttendArgs& a, int seq, int key
   p.page1 = key + kBlockTok < to ? page_of(a.c, a.b, seq, key + kBlockTok) : nullptr;
   return p;
 }
+// Codes are read once a call (a prefix that sequences share: once a sequence): streaming loads leave the caches to what is read
+// again.  256 sequences 124 -> 113 us, 5.8 and for longer ones 6.3 TB/s.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 ldnt(const uint8_t* p) {
+  const u32x4 q = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+  return make_uint4(q.x, q.y, q.z, q.w);
+}
 template <int D, int R>
 __device__ __forceinline__ void load_keys(Keys64<D, R>* o, const AttendArgs& a, const Place64& at, int64_t head_at, int key, int lane) {
   const int r = lane & 15, g = lane >> 4, pt = a.c.page_tokens;
@@ -930,7 +945,7 @@ __device__ __forceinline__ void load_keys(Keys64<D, R>* o, const AttendArgs& a, 
     } else {
 #pragma unroll
       for (int i = 0; i < D / 128; ++i) {
-        const uint4 q = reinterpret_cast<const uint4*>(kp)[i];
+        const uint4 q = ldnt(kp + 16 * i);
         o->k[t][4 * i] = q.x;
         o->k[t][4 * i + 1] = q.y;
         o->k[t][4 * i + 2] = q.z;
@@ -954,7 +969,7 @@ __device__ __forceinline__ void load_values(Values64<D, R>* o, const AttendArgs&
   for (int b = 0; b < 2; ++b) {
     const uint8_t* vp = (b ? h1 + slot1 * (D / 2) : h0 + slot0 * (D / 2)) + pt * (D / 2);
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) o->v[b][j] = *reinterpret_cast<const uint4*>(vp + (unsigned)((j * 64 + lane) * 16));
+    for (int j = 0; j < D / 64; ++j) o->v[b][j] = ldnt(vp + (unsigned)((j * 64 + lane) * 16));
   }
 #pragma unroll
   for (int u = 0; u < Values64<D, R>::U; ++u) {
