@@ -116,12 +116,26 @@ __device__ __forceinline__ float turn_b(float a, float b, float2 cs) {
   return b * cs.x + a * cs.y;
 }
 
-// How groups of 8 channels are rotated: not at all; with a partner group (half-split layout); within themselves (interleaved
-// layout); element by element, where a pair crosses groups.  One kind holds for a whole launch, so kernels branch on it once,
-// outside their loops, and the loads of a loop go out together.
-enum RotaryKind { kPlain, kHalf, kWithin, kElements };
+// How groups of 8 channels are rotated: not at all; with a partner group (half-split layout), which the same thread has too if
+// the whole head is rotated; within themselves (interleaved layout); element by element, where a pair crosses groups.  One
+// kind holds for a whole launch, so kernels branch on it once, outside their loops, and the loads of a loop go out together.
+enum RotaryKind { kPlain, kWhole, kHalf, kWithin, kElements };
+template <int D>
 __device__ __forceinline__ RotaryKind kind_of(const Rotary& r) {
-  return !r.table ? kPlain : r.interleaved ? ((r.rot & 7) == 0 ? kWithin : kElements) : ((r.rot & 15) == 0 ? kHalf : kElements);
+  return !r.table ? kPlain : r.interleaved ? ((r.rot & 7) == 0 ? kWithin : kElements) : r.rot == D ? kWhole : ((r.rot & 15) == 0 ? kHalf : kElements);
+}
+// Channels c0 .. c0+7 and c0 + D/2 .. of a row whose whole head is rotated, half-split: each angle serves both members.
+template <int DT, int D>
+__device__ __forceinline__ void rotated_pair(const uint8_t* row, int c0, const Angles& cs, float* a, float* b) {
+  ld8<DT>(row + c0 * Elt<DT>::B, a);
+  ld8<DT>(row + (c0 + D / 2) * Elt<DT>::B, b);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float2 w = angle(cs, c0 + i, cs.one);
+    const float u = a[i], v = b[i];
+    a[i] = turn_a(u, v, w);
+    b[i] = turn_b(u, v, w);
+  }
 }
 // Channels c0 .. c0+7 of a row (c0 a multiple of 8), rotated.  The partners of a half-split rotation are read along: a second
 // trip to lines that the neighbouring lanes read anyway.
@@ -402,22 +416,45 @@ __device__ __forceinline__ void st_run(uint32_t* p, const uint32_t* o) {
   else *reinterpret_cast<uint4*>(p) = make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-// Channels c0 .. c0 + C-1 of a row of keys, rotated, or of values.
-template <int DT, int C, RotaryKind KIND>
-__device__ __forceinline__ void row_part(const CacheArgs& a, const Rows& src, const RowWork& w, int c0, float* x) {
+// The groups of 8 channels that one of a row's 8 threads has: neighbours, or (paired: keys rotated over the whole head, of 128
+// channels or more) 64 apart, so that it has both members of its pairs.
+template <int DT, int D, RotaryKind KIND>
+__device__ __forceinline__ void row_part(const CacheArgs& a, const Rows& src, const RowWork& w, int part, float* x) {
+  constexpr int C = D / 8, G = C / 8;
   const uint8_t* p = src.p + w.tok * src.ts + w.head * src.hs;
   Angles cs{nullptr, 1.f};
   if constexpr (KIND != kPlain) cs = angles_at(a.r, a.b.positions ? a.b.positions[w.tok] : w.place);
+  if constexpr (KIND == kWhole && G > 1) {
 #pragma unroll
-  for (int i = 0; i < C; i += 8) rotated8<DT, KIND>(p, c0 + i, a.r, cs, x + i);
+    for (int i = 0; i < G / 2; ++i) rotated_pair<DT, D>(p, part * 8 + 64 * i, cs, x + 8 * i, x + 8 * (i + G / 2));
+  } else {
+#pragma unroll
+    for (int i = 0; i < C; i += 8) rotated8<DT, KIND == kWhole ? kHalf : KIND>(p, part * C + i, a.r, cs, x + i);
+  }
 }
-template <int DT, int C>
-__device__ __forceinline__ void row_part(const CacheArgs& a, const RowWork& w, int c0, float* x) {
-  switch (w.values ? kPlain : kind_of(a.r)) {
-    case kPlain: row_part<DT, C, kPlain>(a, w.values ? a.v : a.k, w, c0, x); break;
-    case kHalf: row_part<DT, C, kHalf>(a, a.k, w, c0, x); break;
-    case kWithin: row_part<DT, C, kWithin>(a, a.k, w, c0, x); break;
-    default: row_part<DT, C, kElements>(a, a.k, w, c0, x); break;
+template <int DT, int D>
+__device__ __forceinline__ bool row_part(const CacheArgs& a, const RowWork& w, int part, float* x) {
+  const RotaryKind kind = w.values ? kPlain : kind_of<D>(a.r);
+  switch (kind) {
+    case kPlain: row_part<DT, D, kPlain>(a, w.values ? a.v : a.k, w, part, x); break;
+    case kWhole: row_part<DT, D, kWhole>(a, a.k, w, part, x); break;
+    case kHalf: row_part<DT, D, kHalf>(a, a.k, w, part, x); break;
+    case kWithin: row_part<DT, D, kWithin>(a, a.k, w, part, x); break;
+    default: row_part<DT, D, kElements>(a, a.k, w, part, x); break;
+  }
+  return kind == kWhole && D > 64;
+}
+// A row's codes of keys to its place.
+template <int D>
+__device__ __forceinline__ void put_key(uint8_t* row, int part, bool paired, const uint32_t* word) {
+  constexpr int G = D / 64;
+  uint32_t* o = reinterpret_cast<uint32_t*>(row);
+  if (paired) {
+#pragma unroll
+    for (int i = 0; i < G; ++i) o[part + 8 * i] = word[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < G; ++i) o[part * G + i] = word[i];
   }
 }
 
@@ -485,7 +522,7 @@ __global__ __launch_bounds__(kThreads) void k_append_single(CacheArgs a) {
   const int part = threadIdx.x & 7;
   uint8_t* page = page_of(a.c, a.b, w.seq, w.place);
   float x[C];
-  row_part<DT, C>(a, w, part * C, x);
+  const bool paired = row_part<DT, D>(a, w, part, x);
   if (!page) return;
   const int pt = a.c.page_tokens, slot = w.place & (pt - 1);
   uint8_t* hp = page + (int64_t)w.head * pt * (D + 8);
@@ -499,8 +536,7 @@ __global__ __launch_bounds__(kThreads) void k_append_single(CacheArgs a) {
   const uint32_t params = quantise<C>(x, word);
   if (part == 0) reinterpret_cast<uint32_t*>(hp + (int64_t)pt * D)[(w.values ? pt : 0) + slot] = params;
   if (!w.values) {
-#pragma unroll
-    for (int i = 0; i < C / 8; ++i) reinterpret_cast<uint32_t*>(hp + slot * (D / 2))[part * (C / 8) + i] = word[i];
+    put_key<D>(hp + slot * (D / 2), part, paired, word);
   } else {
     ValueWords<D>::each(part, g, [&](int at, int c) {
       uint32_t* o = &old[(c & 3) * ValueWords<D>::TILES + (c >> 2)];
@@ -550,8 +586,9 @@ __global__ __launch_bounds__(kThreads) void k_append(CacheArgs a) {
   uint8_t* page = page_of(a.c, a.b, w.seq, place0);
   if (!page) return;
   float x[C];
+  bool paired = false;
   if (w.mine) {
-    row_part<DT, C>(a, w, part * C, x);
+    paired = row_part<DT, D>(a, w, part, x);
   } else {
 #pragma unroll
     for (int i = 0; i < C; ++i) x[i] = 0.f;
@@ -562,10 +599,7 @@ __global__ __launch_bounds__(kThreads) void k_append(CacheArgs a) {
   uint8_t* hp = page + (int64_t)w.head * pt * (D + 8);
   if (w.mine && part == 0) reinterpret_cast<uint32_t*>(hp + (int64_t)pt * D)[(w.values ? pt : 0) + slot] = params;
   if (!w.values) {
-    if (w.mine) {
-#pragma unroll
-      for (int i = 0; i < C / 8; ++i) reinterpret_cast<uint32_t*>(hp + slot * (D / 2))[part * (C / 8) + i] = word[i];
-    }
+    if (w.mine) put_key<D>(hp + slot * (D / 2), part, paired, word);
     return;
   }
 #pragma unroll
@@ -749,25 +783,27 @@ struct QueryRows {
 // THREADS threads (whole wavefronts) stage rows r0 .. r0 + R-1 of a sequence; behind the last row, that one again.
 template <int DT, int D, int HQ, int R, int THREADS, RotaryKind KIND>
 __device__ __forceinline__ void stage_queries_of(QueryRows<D, HQ, R>* o, const AttendArgs& a, const Seq& s, int kvh, int r0, int rows, int thread) {
-  constexpr int T = D / 8;  // threads of a row
+  constexpr int G = KIND == kWhole ? 2 : 1, T = D / 8 / G;  // groups of 8 channels of a thread, T * 8 apart; threads of a row
   constexpr int N = (R * T + THREADS - 1) / THREADS;
-  float x[N][8];
+  float x[N][8 * G];
   const int part = thread % T;
 #pragma unroll
   for (int n = 0; n < N; ++n) {  // (threads behind the last row read it along, so that no load waits for a branch)
     const int row = (thread + n * THREADS) / T;
     const int rr = r0 + row < rows ? r0 + row : rows - 1;
     const int t = rr / a.rep, h = kvh * a.rep + rr - t * a.rep, tok = s.first + t;
+    const uint8_t* p = a.q.p + tok * a.q.ts + h * a.q.hs;
     Angles cs{nullptr, 1.f};
     if constexpr (KIND != kPlain) cs = angles_at(a.r, a.b.positions ? a.b.positions[tok] : s.len - s.n + t);
-    rotated8<DT, KIND>(a.q.p + tok * a.q.ts + h * a.q.hs, part * 8, a.r, cs, x[n]);
+    if constexpr (KIND == kWhole) rotated_pair<DT, D>(p, part * 8, cs, x[n], x[n] + 8);
+    else rotated8<DT, KIND>(p, part * 8, a.r, cs, x[n]);
   }
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const int row = (thread + n * THREADS) / T;
     float big = 0.f, sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) big = fmaxf(big, fabsf(x[n][k]));
+    for (int k = 0; k < 8 * G; ++k) big = fmaxf(big, fabsf(x[n][k]));
 #pragma unroll
     for (int d = 1; d < T; d <<= 1) big = fmaxf(big, __shfl_xor(big, d));
     // 2^e with big * 2^e in [2^9, 2^10)
@@ -775,7 +811,7 @@ __device__ __forceinline__ void stage_queries_of(QueryRows<D, HQ, R>* o, const A
     e = e > 120 ? 120 : e;
     const float up = __uint_as_float((uint32_t)(e + 127) << 23);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < 8 * G; ++k) {
       x[n][k] *= up;
       sum += x[n][k];
     }
@@ -784,12 +820,16 @@ __device__ __forceinline__ void stage_queries_of(QueryRows<D, HQ, R>* o, const A
     if (row < R) {
 #pragma unroll
       for (int h2 = 0; h2 < HQ; ++h2) {
-        o->q[h2][row][part] = make_uint4(pack_f16(x[n][0], x[n][4]), pack_f16(x[n][1], x[n][5]), pack_f16(x[n][2], x[n][6]), pack_f16(x[n][3], x[n][7]));
-        if (h2 + 1 < HQ) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            asm("" : "+v"(x[n][k]));
-            x[n][k] -= (float)(_Float16)x[n][k];
+        for (int c = 0; c < G; ++c) {
+          float* y = &x[n][8 * c];
+          o->q[h2][row][part + c * T] = make_uint4(pack_f16(y[0], y[4]), pack_f16(y[1], y[5]), pack_f16(y[2], y[6]), pack_f16(y[3], y[7]));
+          if (h2 + 1 < HQ) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              asm("" : "+v"(y[k]));
+              y[k] -= (float)(_Float16)y[k];
+            }
           }
         }
       }
@@ -802,7 +842,8 @@ __device__ __forceinline__ void stage_queries_of(QueryRows<D, HQ, R>* o, const A
 }
 template <int DT, int D, int HQ, int R, int THREADS>
 __device__ __forceinline__ void stage_queries(QueryRows<D, HQ, R>* o, const AttendArgs& a, const Seq& s, int kvh, int r0, int rows, int thread) {
-  switch (kind_of(a.r)) {
+  switch (kind_of<D>(a.r)) {
+    case kWhole: stage_queries_of<DT, D, HQ, R, THREADS, kWhole>(o, a, s, kvh, r0, rows, thread); break;
     case kPlain: stage_queries_of<DT, D, HQ, R, THREADS, kPlain>(o, a, s, kvh, r0, rows, thread); break;
     case kHalf: stage_queries_of<DT, D, HQ, R, THREADS, kHalf>(o, a, s, kvh, r0, rows, thread); break;
     case kWithin: stage_queries_of<DT, D, HQ, R, THREADS, kWithin>(o, a, s, kvh, r0, rows, thread); break;

@@ -251,10 +251,11 @@ CACHES = [("bf16", 2, 128, 64, [1, 1, 1], [0, 31, 64]), ("fp16", 3, 64, 32, [5, 
 
 
 @pytest.mark.parametrize("dtype,kvh,d,page,new,ctx", CACHES)
-@pytest.mark.parametrize("interleaved,rot", [(False, 0), (False, 32), (True, 64), (False, 20), (True, 6)])
+@pytest.mark.parametrize("interleaved,rot", [(False, 0), (False, 32), (True, 64), (False, 20), (True, 6), (False, "whole"), (True, "whole")])
 def test_append_writes_these_bytes_and_no_others(dtype, kvh, d, page, new, ctx, interleaved, rot):
     import torch
     P = lib()
+    rot = d if rot == "whole" else rot
     s = Setup(dtype, kvh, d, page, new, ctx, seed=d + rot)
     k, k64 = put(s.rng.normal(size=(s.tokens, kvh, d)) * 3 + 1, dtype)
     v, v64 = put(s.rng.normal(size=(s.tokens, kvh, d)), dtype)
@@ -425,6 +426,13 @@ ATTEND = [  # kv heads, heads, d, page, new, ctx
 @pytest.mark.parametrize("causal,window,rot", [(True, 0, 0), (True, 37, 32), (False, 0, 64)])
 def test_attention(dtype, kvh, heads, d, page, new, ctx, causal, window, rot):
     check_attention(Setup(dtype, kvh, d, page, new, ctx, seed=heads + d), heads, causal, window, rot, interleaved=rot == 32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("kvh,heads,d,page,new,ctx", ATTEND[:2] + ATTEND[4:6])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_attention_with_whole_heads_rotated(dtype, kvh, heads, d, page, new, ctx, interleaved):
+    check_attention(Setup(dtype, kvh, d, page, new, ctx, seed=heads + d), heads, rot=d, interleaved=interleaved)
 
 
 @pytest.mark.parametrize("workspace", [0, 1000, 40000, 1 << 24])
