@@ -939,7 +939,7 @@ __device__ __forceinline__ int parts_of(const AttendArgs& a, int lo, int hi) {
 // softmax of its own over its keys (nothing is exchanged between lanes), a lane has 4, 8 or 16 weights to compute instead
 // of 16, and the columns are joined where the wavefronts are.  The weights of keys that are other columns' are zero.
 //
-// The four wavefronts of a workgroup take every fourth 64 keys of the part.  A wavefront asks for the next keys as soon as the
+// The wavefronts of a workgroup (4, or 16 where there are few workgroups) take 64 keys of the part in turn.  A wavefront asks for the next keys as soon as the
 // present ones are used, and for the next values likewise, into the same registers: with three or four wavefronts on a SIMD that
 // hides memory, and a second set of registers would cost one of them.
 template <int D, int R>
@@ -1160,13 +1160,39 @@ __device__ __forceinline__ void add_values64(const uint4 (&v)[2][D / 64], float*
   }
 }
 
+// What the lane 4 or 8 further round among 16 has.
+template <int BY>
+__device__ __forceinline__ float round16(float v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x120 + BY, 0xf, 0xf, true));  // row_ror
+}
+// Joins the columns that one row has: afterwards each of them has all of it.
+template <int D, int R>
+__device__ __forceinline__ void join_columns(Sums<D, 1>* s) {
+  if constexpr (R == 16) return;
+  float ref = fmaxf(s->ref[0], round16<8>(s->ref[0]));
+  if constexpr (R == 4) ref = fmaxf(ref, round16<4>(ref));
+  const float f = __builtin_amdgcn_exp2f(s->ref[0] - ref);
+  s->ref[0] = ref;
+  auto join = [&](float v) {
+    v *= f;
+    v += round16<8>(v);
+    if constexpr (R == 4) v += round16<4>(v);
+    return v;
+  };
+  s->l[0] = join(s->l[0]);
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s->o[0][i][k] = join(s->o[0][i][k]);
+  }
+}
 // Wavefronts of a SIMD that the registers are shared among: as many as the sums and a step's rows leave room for without spills.
 template <int DT, int D, int R> constexpr int few_waves() { return D == 256 ? (R == 16 ? 1 : 2) : R == 4 ? 4 : R == 8 ? 3 : 2; }
-template <int DT, int D, int R>
-__global__ __launch_bounds__(kThreads, (few_waves<DT, D, R>())) void k_attend_few(AttendArgs a) {
-  constexpr int HQ = DT == PLORA_BF16 ? 1 : 2, HW = DT == PLORA_F32 ? 2 : 1, Y = kWaves * (16 / R);
+template <int DT, int D, int R, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, (few_waves<DT, D, R>())) void k_attend_few(AttendArgs a) {
+  constexpr int HQ = DT == PLORA_BF16 ? 1 : 2, HW = DT == PLORA_F32 ? 2 : 1, THREADS = 64 * WAVES;
   __shared__ QueryRows<D, HQ, R> query_rows;
-  __shared__ float so[Y][R][D + 4], sm[Y][R], sl[Y][R];
+  __shared__ float so[WAVES][R][D + 4], sm[WAVES][R], sl[WAVES][R];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int seq = blockIdx.x / a.c.heads, kvh = blockIdx.x - seq * a.c.heads, part = blockIdx.y;
   const Seq sq = seq_at(a.b, seq);
@@ -1179,7 +1205,7 @@ __global__ __launch_bounds__(kThreads, (few_waves<DT, D, R>())) void k_attend_fe
   const int from = lo + part * a.part_keys;
   const int to = part == n_parts - 1 ? hi : from + a.part_keys;
   const int64_t head_at = (int64_t)kvh * a.c.page_tokens * (D + 8);
-  constexpr int kStep = 64 * kWaves;
+  constexpr int kStep = 64 * WAVES;
   int key = from + 64 * wave;
   Place64 here = place64(a, seq, key, to);
   Keys64<D, R> k;
@@ -1187,7 +1213,7 @@ __global__ __launch_bounds__(kThreads, (few_waves<DT, D, R>())) void k_attend_fe
   load_keys(&k, a, here, head_at, key, lane);
   load_values(&v, a, here, head_at, key, lane);
   Place64 next = place64(a, seq, key + kStep, to);
-  stage_queries<DT, D, HQ, R, kThreads>(&query_rows, a, sq, kvh, 0, rows, threadIdx.x);
+  stage_queries<DT, D, HQ, R, THREADS>(&query_rows, a, sq, kvh, 0, rows, threadIdx.x);
   __syncthreads();
   const int own_row = (lane & 15) % R;
   const Column q{query_rows.sum[own_row], (HW == 1 ? -64.f : 8.f) * query_rows.sum[own_row], query_rows.f[own_row], a.causal ? sq.len - sq.n + (own_row < rows ? own_row : rows - 1) / a.rep : 0x7fffffff};
@@ -1209,22 +1235,25 @@ __global__ __launch_bounds__(kThreads, (few_waves<DT, D, R>())) void k_attend_fe
     next = place64(a, seq, key + kStep, to);
   }
   join_lanes(&s);
-  const int r = lane & 15, g = lane >> 4, at = wave * (16 / R) + r / R;
+  join_columns<D, R>(&s);
+  const int r = lane & 15, g = lane >> 4;
+  if (r < R) {
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(&so[at][r % R][g * (D / 4) + 4 * i]) = s.o[0][i];
-  if (g == 0) {
-    sm[at][r % R] = s.ref[0];
-    sl[at][r % R] = s.l[0];
+    for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(&so[wave][r][g * (D / 4) + 4 * i]) = s.o[0][i];
+    if (g == 0) {
+      sm[wave][r] = s.ref[0];
+      sl[wave][r] = s.l[0];
+    }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < rows * (D / 8); i += kThreads) {
+  for (int i = threadIdx.x; i < rows * (D / 8); i += THREADS) {
     const int row = i / (D / 8), c = (i - row * (D / 8)) * 8;
     float ref = sm[0][row];
 #pragma unroll
-    for (int k = 1; k < Y; ++k) ref = fmaxf(ref, sm[k][row]);
+    for (int k = 1; k < WAVES; ++k) ref = fmaxf(ref, sm[k][row]);
     float l = 0.f, o[8] = {};
 #pragma unroll 2
-    for (int k = 0; k < Y; ++k) {
+    for (int k = 0; k < WAVES; ++k) {
       const float f = __builtin_amdgcn_exp2f(sm[k][row] - ref);
       l = __builtin_fmaf(f, sl[k][row], l);
 #pragma unroll
@@ -1602,11 +1631,11 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
 // ---- host side ----------------------------------------------------------------------------------------
 
 template <class A>
-int launch(void (*kernel)(A), uint64_t gx, unsigned gy, unsigned gz, const A& args, plora_stream stream) {
-  if (gx == 0 || gx * kThreads >= ((uint64_t)1 << 32) || gy > 65535) return PLORA_ERR_LIMIT;
+int launch(void (*kernel)(A), uint64_t gx, unsigned gy, unsigned gz, const A& args, plora_stream stream, unsigned threads = kThreads) {
+  if (gx == 0 || gx * threads >= ((uint64_t)1 << 32) || gy > 65535) return PLORA_ERR_LIMIT;
   A copy = args;
   void* p[] = {&copy};
-  const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)gx, gy, gz), dim3(kThreads), p, 0, (hipStream_t)stream);
+  const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)gx, gy, gz), dim3(threads), p, 0, (hipStream_t)stream);
   if (e == hipSuccess) return PLORA_OK;
   plora::g_last_hip = (int)e;
   (void)hipGetLastError();
@@ -1711,8 +1740,11 @@ int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace,
   const uint64_t many = some_many ? groups * a.c.heads : 0;
   const uint64_t fit = workspace ? workspace_bytes / ((uint64_t)rows * (D + 2) * 4) : 0;
   const int64_t keys = a.window ? (a.b.max_len < a.window + (int64_t)max_new + kKeyAlign ? a.b.max_len : a.window + (int64_t)max_new + kKeyAlign) : a.b.max_len;
-  uint64_t want = (some_many ? kFillMany + many - 1 : kFillFew + few - 1) / (some_many ? many : few);
-  const uint64_t most = (uint64_t)keys / kLeastPart;
+  // 16 wavefronts to a part instead of 4 where there would be parts: fewer of them to join, or none
+  const bool wide = D < 256 && !some_many && a.few_rows == 4 && few * 4 <= kFillFew;
+  const uint64_t fill = some_many ? kFillMany : wide ? kFillFew / 4 : kFillFew, given = some_many ? many : few;
+  uint64_t want = (fill + given - 1) / given;
+  const uint64_t most = (uint64_t)keys / (wide ? 4 * kLeastPart : kLeastPart);
   if (want > most) want = most;
   if (want > fit) want = fit;
   if (want > 4096) want = 4096;
@@ -1722,8 +1754,11 @@ int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace,
   a.part_ml = a.part_o + (int64_t)a.parts * rows * D;
   if (!some_few) a.few_rows = 0;
   int rc = PLORA_OK;
-  if (few)
-    rc = launch(a.few_rows == 4 ? k_attend_few<DT, D, 4> : a.few_rows == 8 ? k_attend_few<DT, D, 8> : k_attend_few<DT, D, 16>, few, (unsigned)a.parts, 1, a, stream);
+  if (wide) {
+    if constexpr (D < 256) rc = launch(k_attend_few<DT, D, 4, 16>, few, (unsigned)a.parts, 1, a, stream, 1024);
+  } else if (few) {
+    rc = launch(a.few_rows == 4 ? k_attend_few<DT, D, 4, 4> : a.few_rows == 8 ? k_attend_few<DT, D, 8, 4> : k_attend_few<DT, D, 16, 4>, few, (unsigned)a.parts, 1, a, stream);
+  }
   if (rc == PLORA_OK && many) {
     // a rotated row of 16-bit elements needs more than the 11 bits of one half to be as good as its elements were; the 8 of bf16 do not
     if (DT == PLORA_F32 || (DT == PLORA_F16 && a.r.table)) rc = launch(k_attend_many<DT, D, NQ, 2>, many, (unsigned)a.parts, 1, a, stream);
