@@ -813,6 +813,8 @@ __device__ __forceinline__ void stage_queries_of(QueryRows<D, HQ, R>* o, const A
 #pragma unroll
     for (int k = 0; k < 8 * G; ++k) {
       x[n][k] *= up;
+      // (of what goes into the products: the offset that codes have there is taken off by this sum, times up to 64)
+      if constexpr (HQ == 1) x[n][k] = (float)(_Float16)x[n][k];
       sum += x[n][k];
     }
 #pragma unroll
@@ -1412,7 +1414,7 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
   f16x8 vc[kAhead];
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) vc[i] = __builtin_bit_cast(f16x8, b.values[block * (D / 16) + i][lane]);
-  for (int turn = 0;; ++turn) {  // (as in weights64)
+  auto weights = [&]() {
     float top = 0.f;
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
@@ -1427,7 +1429,9 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
       }
       top = fmaxf(top, l[j] * 0x1p-93f);
     }
-    if (turn || !__any(top > 0x1p15f)) break;
+    return top;
+  };
+  if (__any(weights() > 0x1p15f)) {  // (a NaN is none: it stays where it is)
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
       float best = -INFINITY;
@@ -1445,6 +1449,7 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) s->o[j][i] *= down;
     }
+    weights();
   }
   union { uint32_t u[4]; f16x8 v; } wb[NQ][HW];
 #pragma unroll
@@ -1479,10 +1484,11 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
 template <int DT, int D, int NQ, int HQ>
 __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
   constexpr int HW = DT == PLORA_F32 ? 2 : 1, R = 16 * NQ;
-  // Two workgroups share a CU.  Low halves of 32 rows of 128 channels do not fit the registers beside the rest: they stay in LDS.
-  // A stage is 32 keys (64 channels: 64, a word a lane is too little to fetch): with 64 the same took 1.40 ms instead of 1.34.
+  // Two workgroups share a CU.  Low halves of 32 rows of 128 channels do not fit the registers beside the rest: they stay in LDS,
+  // which then holds stages of 32 keys instead of 64 (fp16 1.64 ms either way; with the halves in registers 2.77; bf16 with 32 keys
+  // 1.44 instead of 1.40).
   constexpr bool LOW_IN_LDS = HQ == 2 && NQ == 2 && D == 128;
-  constexpr int K = D == 64 ? 64 : 32, W = Stage<D, K>::W;
+  constexpr int K = D == 256 || LOW_IN_LDS ? 32 : 64, W = Stage<D, K>::W;
   __shared__ union {
     Stage<D, K> stage[2];
     QueryRows<D, HQ, 16> rows[kWaves];
