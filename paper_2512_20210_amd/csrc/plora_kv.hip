@@ -692,7 +692,7 @@ __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
 // softmax reference per lane serves its column.
 //
 // Codes enter as fp16 numbers code - 8, exactly, and scale and min stay outside in fp32:
-//   q . K[s] = scale_s * (8 sum(q) + q . (code - 8)) + min_s * sum(q),
+//   q . K[s] = scale_s * (q . (code - 8)) + (min_s + 8 scale_s) * sum(q),
 //   sum p_s V[s] = sum (p_s scale_s)(code - 8) + sum p_s (min_s + 8 scale_s).
 // So a row of keys or values costs its codes' unpacking (9 instructions per 8 codes) and no multiplication by its scale, and what
 // lies in places that are not seen cannot hurt: codes are finite whatever the memory holds, and scale and min are dropped
@@ -858,7 +858,6 @@ template <int D, int NQ, int HQ>
 struct Queries {
   f16x8 q[NQ][HQ][D / 32];
   float sum[NQ];
-  float sum8[NQ];  // 8 sums: what code - 8 leaves out
   float f[NQ];
   int place[NQ];   // last place that the column sees
 };
@@ -873,7 +872,6 @@ __device__ __forceinline__ void take_queries(Queries<D, NQ, H>* o, int j, const 
     for (int i = 0; i < D / 32; ++i) o->q[j][h][i] = __builtin_bit_cast(f16x8, from.q[h][r][g * (D / 32) + i]);
   }
   o->sum[j] = from.sum[r];
-  o->sum8[j] = 8.f * from.sum[r];
   o->f[j] = from.f[r];
 }
 
@@ -1024,7 +1022,7 @@ __device__ __forceinline__ void load_values(Values64<D, R>* o, const AttendArgs&
 
 // The row of a lane's column.
 struct Column {
-  float sum, start, f;  // start: times sum, what the keys' offset is too much or too little
+  float sum, start, f;  // start: what takes the keys' offset off
   int place;  // last place that it sees
 };
 
@@ -1059,7 +1057,8 @@ __device__ __forceinline__ void logits64(const Keys64<D, R>& b, const QueryRows<
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t kp = reinterpret_cast<const uint32_t*>(&b.kp[u])[i];
-      x[4 * u + i] = __builtin_fmaf(param_scale(kp), c[u][i], param_min(kp) * q.sum);
+      const float s = param_scale(kp), m = param_min(kp);
+      x[4 * u + i] = __builtin_fmaf(s, c[u][i], (OVER64 ? m : __builtin_fmaf(8.f, s, m)) * q.sum);
     }
   }
 }
@@ -1218,7 +1217,7 @@ __global__ __launch_bounds__(64 * WAVES, (few_waves<DT, D, R>())) void k_attend_
   stage_queries<DT, D, HQ, R, THREADS>(&query_rows, a, sq, kvh, 0, rows, threadIdx.x);
   __syncthreads();
   const int own_row = (lane & 15) % R;
-  const Column q{query_rows.sum[own_row], (HW == 1 ? -64.f : 8.f) * query_rows.sum[own_row], query_rows.f[own_row], a.causal ? sq.len - sq.n + (own_row < rows ? own_row : rows - 1) / a.rep : 0x7fffffff};
+  const Column q{query_rows.sum[own_row], HW == 1 ? -64.f * query_rows.sum[own_row] : 0.f, query_rows.f[own_row], a.causal ? sq.len - sq.n + (own_row < rows ? own_row : rows - 1) / a.rep : 0x7fffffff};
   const CodeBits bits = code_bits();
   Sums<D, 1> s;
   clear(&s);
@@ -1275,7 +1274,7 @@ struct Stage {
   static constexpr int K = KEYS, W = K / 16 * (D / 32) / kWaves;  // keys; words of keys, and of values, of a lane
   uint4 keys[K / 16 * (D / 32)][64];    // [tile of 16 keys][32 channels], then lanes
   uint4 values[K / 32 * (D / 16)][64];  // [32 keys][16 channels]
-  float ks[K], km[K], vs[K], vm[K];     // scale and min of keys; scale and min + 8 scale of values, 0 where there is no row
+  float ks[K], km[K], vs[K], vm[K];     // scale and min + 8 scale of keys and of values, of these 0 where there is no row
 };
 // The pages of a stage's two blocks of 32 keys, read a stage before they are used: -1 behind `to`.
 struct PageIds {
@@ -1349,7 +1348,7 @@ __device__ __forceinline__ void unpack(Stage<D, K>* o, const Fetched<W>& f, cons
     const float s = param_scale(f.vp), m = __builtin_fmaf(8.f, s, param_min(f.vp));
     const bool fine = fabsf(s) < INFINITY && fabsf(m) < INFINITY;
     o->ks[lane] = fine ? param_scale(f.kp) : __builtin_nanf("");
-    o->km[lane] = param_min(f.kp);
+    o->km[lane] = __builtin_fmaf(8.f, param_scale(f.kp), param_min(f.kp));
     o->vs[lane] = fine ? s : 0.f;
     o->vm[lane] = fine ? m : 0.f;
   }
@@ -1363,7 +1362,7 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
   const int g = lane >> 4;
   f32x4 t[NQ][2];
 #pragma unroll
-  for (int j = 0; j < NQ; ++j) t[j][0] = t[j][1] = f32x4{q.sum8[j], q.sum8[j], q.sum8[j], q.sum8[j]};
+  for (int j = 0; j < NQ; ++j) t[j][0] = t[j][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
     const f16x8 k0 = __builtin_bit_cast(f16x8, b.keys[2 * block * (D / 32) + i][lane]), k1 = __builtin_bit_cast(f16x8, b.keys[(2 * block + 1) * (D / 32) + i][lane]);

@@ -402,6 +402,7 @@ def check_attention(s, heads, causal=True, window=0, rot=0, interleaved=False, k
         places = s.places(i) if s.len[i] > 0 else np.full(s.new[i], -1)
         ref, amp, size = O.attend(q64[rows], kk, vv, scale, places, causal, window, holes)
         bound = rounding * np.abs(ref) + (amp * (2 * weight + 2 * logit * size))[..., None] + 1e-30
+        s.exact = ref  # of the last sequence
         far = np.abs(got[rows] - ref)
         assert (far <= bound).all(), "sequence %d: %.3g times its bound" % (i, (far / bound).max())
         if s.len[i] <= 0:
@@ -433,6 +434,22 @@ def test_attention(dtype, kvh, heads, d, page, new, ctx, causal, window, rot):
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_attention_with_whole_heads_rotated(dtype, kvh, heads, d, page, new, ctx, interleaved):
     check_attention(Setup(dtype, kvh, d, page, new, ctx, seed=heads + d), heads, rot=d, interleaved=interleaved)
+
+
+@pytest.mark.parametrize("dtype,most", [("bf16", 2.5e-3), ("fp16", 4e-4), ("fp32", 2e-6)])
+@pytest.mark.parametrize("new,rot", [(1, 0), (1, 128), (3, 128), (40, 128)])
+def test_error_of_long_rows_as_a_norm(dtype, most, new, rot):
+    """2000 keys, some channels of which are loud: the error's 2-norm against the result's.  A result's own rounding is 0.43 units
+    in the last place's half (bf16 1.7e-3, fp16 2.1e-4), weights of 11 bits add 2.1e-4 of it, a rotated bf16 row of 11 bits
+    2.1e-4 times a logit's size of up to 5; fp32: sums of 128 and 2000 terms, and the exponent of a logit of 10, 2^-24 each."""
+    s = Setup(dtype, 1, 128, 64, [new], [2000], seed=5)
+    rng = s.rng
+    loud = np.where(rng.random(128) < 0.06, 4.0, 1.0)
+    keys = [rng.normal(size=(s.len[0], 1, 128)) * loud + 0.5 * rng.normal(size=128)]
+    vals = [rng.normal(size=(s.len[0], 1, 128))]
+    q_in = 1.5 * rng.normal(size=(new, 4, 128))
+    out = host(check_attention(s, 4, rot=rot, keys=keys, vals=vals, q_in=q_in))
+    assert np.linalg.norm(out - s.exact) <= most * np.linalg.norm(s.exact)
 
 
 @pytest.mark.parametrize("workspace", [0, 1000, 40000, 1 << 24])
