@@ -205,9 +205,9 @@ struct RotateArgs {
   uint8_t* y;
   int64_t xt, xh, yt, yh;  // strides in bytes
   int64_t n_units;         // tokens * heads * units
-  int32_t heads, head_dim;
-  int32_t units;           // of a row: pair units, then units of channels that are copied
-  int32_t pair_units;
+  uint32_t heads;
+  uint32_t units;          // of a row: pair units, then units of channels that are copied
+  uint32_t pair_units;
   float sign;
 };
 // One thread, one unit.  VECTOR: a unit is 8 pairs of the half-split layout (two groups of 8 channels), 8 channels of the
@@ -215,14 +215,11 @@ struct RotateArgs {
 // Both members of a pair are read before either is written, so y may be x.
 template <int DT, bool VECTOR>
 __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const uint32_t i = blockIdx.x * (uint32_t)kThreads + threadIdx.x;  // (a launch has fewer than 2^32 threads)
   if (i >= a.n_units) return;
-  const int64_t row = i / a.units;
-  const int u = (int)(i - row * a.units);
-  const int64_t t = row / a.heads;
-  const int h = (int)(row - t * a.heads);
-  const uint8_t* x = a.x + t * a.xt + h * a.xh;
-  uint8_t* y = a.y + t * a.yt + h * a.yh;
+  const uint32_t row = i / a.units, u = i - row * a.units, t = row / a.heads, h = row - t * a.heads;
+  const uint8_t* x = a.x + (int64_t)t * a.xt + (int64_t)h * a.xh;
+  uint8_t* y = a.y + (int64_t)t * a.yt + (int64_t)h * a.yh;
   constexpr int W = VECTOR ? 8 : 1, B = Elt<DT>::B;
   if (u >= a.pair_units) {
     const int c = a.r.rot + (u - a.pair_units) * W;
@@ -1832,7 +1829,6 @@ extern "C" int plora_rotate(const plora_rotary* rotary, int32_t dtype, int32_t n
   a.yt = yr.ts;
   a.yh = yr.hs;
   a.heads = n_heads;
-  a.head_dim = head_dim;
   a.sign = inverse ? -1.f : 1.f;
   // groups of 8 channels where no pair and no copied channel shares a group with another kind
   const bool vector = rotary->rot_dim % (rotary->interleaved ? 8 : 16) == 0;
