@@ -213,6 +213,7 @@ struct RotateArgs {
 // One thread, one unit.  VECTOR: a unit is 8 pairs of the half-split layout (two groups of 8 channels), 8 channels of the
 // interleaved one, or 8 channels to copy; otherwise one pair or one channel.
 // Both members of a pair are read before either is written, so y may be x.
+// Bound by its bytes: 19.4 us for 95.6 MB of fp16 rows (4.9 TB/s; a large copy reaches 5.1), 10 us for 38.6 MB of fp32 rows; one row 2.2.
 template <int DT, bool VECTOR>
 __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
   const uint32_t i = blockIdx.x * (uint32_t)kThreads + threadIdx.x;  // (a launch has fewer than 2^32 threads)
@@ -510,7 +511,8 @@ __device__ __forceinline__ uint32_t quantise(const float* x, uint32_t* word) {
   return fine ? (__float_as_uint(s) >> 16) | (sm & 0xffff0000u) : 0x7fc07fc0u;
 }
 
-// Bound by the latency of its chain (first rows and lengths, page, row and angles, the values' words that it changes one nibble of).
+// Bound by the latency of its chain (first rows and lengths, page, row and angles, the values' words that it changes one nibble of): 4.1 us for 256
+// sequences with 8 heads of 128, bf16, of which an empty launch takes 2.
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void k_append_single(CacheArgs a) {
   constexpr int C = D / 8, RUN = ValueWords<D>::RUN;
@@ -572,6 +574,8 @@ __device__ __forceinline__ void transpose_nibbles(uint32_t* w) {
 
 // Values: codes of 32 rows through LDS, then one thread takes 8 channels of the 8 tokens of a quad and transposes them into 8
 // words.  Words of which only some tokens are the call's are read first.
+// 36.8 us for 5k tokens of 32 heads of 128, bf16 (107 MB, 3.1 TB/s): half of it vector instructions (min and max, the exact quotient, packing),
+// the other half the read.
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void k_append(CacheArgs a) {
   constexpr int C = D / 8;
@@ -630,6 +634,7 @@ __global__ __launch_bounds__(kThreads) void k_append(CacheArgs a) {
   }
 }
 
+// A read thread has the channels that an append thread has of the same row; 26 us for 5k tokens of 32 heads of 128, bf16 (104 MB, 4.0 TB/s).
 template <int DT, int D, bool SINGLE>
 __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
   constexpr int C = D / 8, RUN = ValueWords<D>::RUN;
@@ -935,6 +940,9 @@ __device__ __forceinline__ int parts_of(const AttendArgs& a, int lo, int hi) {
 // each of these takes other keys: of 64 keys in 4 tiles of 16, column c has row c % R and the tiles c / R, c / R + 16 / R, ...  Every column is a
 // softmax of its own over its keys (nothing is exchanged between lanes), a lane has 4, 8 or 16 weights to compute instead
 // of 16, and the columns are joined where the wavefronts are.  The weights of keys that are other columns' are zero.
+// 4 rows in tiles of 4, 8, 16: 116, 126, 158 us (256 sequences of 64 - 4095 keys, 8 heads of 128, bf16: 584 MB, 5.0 - 5.2 TB/s, the probe of a bare
+// read reaches 7.0); by k_attend_many 498.  What bounds it is the read: with 4000 keys in all 512 sequences it is at 6.3 TB/s, the
+// rest is the end of the launch, where the longest run alone.
 //
 // The wavefronts of a workgroup (4, or 16 where there are few workgroups) take 64 keys of the part in turn.  A wavefront asks for the next keys as soon as the
 // present ones are used, and for the next values likewise, into the same registers: with three or four wavefronts on a SIMD that
@@ -1264,8 +1272,11 @@ __global__ __launch_bounds__(64 * WAVES, (few_waves<DT, D, R>())) void k_attend_
 
 // Sequences with more rows: a workgroup has 64 * NQ of them, a wavefront 16 * NQ, and all keys of the part.  What bounds it are the
 // vector instructions of the softmax (11 issue slots a logit, 4 of them the exponential), so the codes' unpacking is shared: of
-// kStage keys each wavefront turns a quarter of the codes into the operands that all four then read from LDS (in operand
-// order: a lane's 16 bytes beside the next lane's), a stage ahead of their use, with one barrier a stage.
+// Stage::K keys each wavefront turns a quarter of the codes into the operands that all four then read from LDS (in operand
+// order: a lane's 16 bytes beside the next lane's), a stage ahead of their use, with one barrier a stage.  2048 tokens with 32 heads over
+// 32k keys: bf16 1.34 - 1.40 ms (740 - 780 TFLOP/s of the 1256 that a large product reaches), fp16 with rotation 1.64 (three products
+// instead of two); matrix units busy 38 % of the time (fp16), vector units 51 %.  Prompts of 5k tokens: 76 us, of which a third is the
+// launch, the search for the rows and the output, a third the rotation of q, a third the keys.
 template <int D, int KEYS>
 struct Stage {
   static constexpr int K = KEYS, W = K / 16 * (D / 32) / kWaves;  // keys; words of keys, and of values, of a lane
@@ -1566,7 +1577,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
   }
 }
 
-// Joins the parts of a row.  D/8 threads have 8 channels each, G times over: group g of them takes the parts g, g + G, ..., and the
+// Joins the parts of a row: 4 to 5 us, a launch and its first loads.  D/8 threads have 8 channels each, G times over: group g of them takes the parts g, g + G, ..., and the
 // groups' sums are joined in their order.  R: rows of a tile of k_attend_many.
 template <int DT, int D, int R, int G>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
@@ -1699,7 +1710,7 @@ int rotate(const RotateArgs& a, bool vector, plora_stream stream) {
 
 template <int DT, int D>
 int append_or_read(const CacheArgs& a, bool single, bool read, plora_stream stream) {
-  if (single) {  // rows one behind the other: 26.6 -> 13 us for append and read of 256 tokens, 8 heads, against blocks of 32 places
+  if (single) {  // rows one behind the other: append and read of 256 tokens with 8 heads 14 us, in blocks of 32 places 23
     const uint64_t rows = (uint64_t)a.b.n_seqs * 2 * a.c.heads;
     return launch(read ? k_read<DT, D, true> : k_append_single<DT, D>, (rows + kThreads / 8 - 1) / (kThreads / 8), 1, 1, a, stream);
   }
@@ -1718,8 +1729,9 @@ int append_or_read(const plora_kv_cache* c, const CacheArgs& a, bool single, boo
                                  : append_or_read<PLORA_F32>(c->head_dim, a, single, read, stream);
 }
 
-// Workgroups that fill the GPU, and keys that are worth a part of their own.
-constexpr int kFillFew = 1024, kFillMany = 512, kLeastPart = 512;
+// Workgroups that fill the GPU (k_attend_few: half as many 57 -> 78 us for 2 sequences of 128k keys, twice as many 63; k_attend_many: 130 -> 204 and
+// 163 us for 512 rows over 8000 keys).
+constexpr int kFillFew = 1024, kFillMany = 512;
 
 // Tiles of 16 columns of a wavefront of k_attend_many.
 template <int DT, int D> constexpr int columns_of() { return DT == PLORA_F32 || D == 256 ? 1 : 2; }
@@ -1732,7 +1744,7 @@ int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace,
   const int64_t most_rows = (int64_t)max_new * a.rep;
   const bool some_many = most_rows > kMostFew;
   // Sequences of few rows among ones of many are left to k_attend_many where they are rare and their keys not many: a launch
-  // that finds nothing to do costs 4.6 us, 1024 keys in one workgroup of the other kernel 15.
+  // that finds nothing to do costs 2 to 5 us (prompts of 5k tokens 74 -> 76 us; 64 sequences of up to 64 rows and 900 keys 73 -> 86).
   const bool some_few = !some_many || (a.b.n_seqs > 1 && (a.b.max_len > 1024 || a.b.n_tokens < 16 * (int64_t)a.b.n_seqs));
   // rows of a tile of k_attend_few: all that a sequence can have, or those of a single token next to sequences with many
   const int64_t tile_rows = some_many ? a.rep : most_rows;
@@ -1740,13 +1752,20 @@ int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace,
   const uint64_t few = some_few ? (uint64_t)a.b.n_seqs * a.c.heads : 0;
   const uint64_t groups = (uint64_t)a.b.n_tokens * a.rep / R + a.b.n_seqs;
   const uint64_t many = some_many ? groups * a.c.heads : 0;
+  const uint64_t likely = ((uint64_t)a.b.n_tokens * a.rep + R - 1) / R + (a.b.n_seqs - 1) / 2;  // groups that have rows
   const uint64_t fit = workspace ? workspace_bytes / ((uint64_t)rows * (D + 2) * 4) : 0;
   const int64_t keys = a.window ? (a.b.max_len < a.window + (int64_t)max_new + kKeyAlign ? a.b.max_len : a.window + (int64_t)max_new + kKeyAlign) : a.b.max_len;
-  // 16 wavefronts to a part instead of 4 where there would be parts: fewer of them to join, or none
-  const bool wide = D < 256 && !some_many && a.few_rows == 4 && few * 4 <= kFillFew;
-  const uint64_t fill = some_many ? kFillMany : wide ? kFillFew / 4 : kFillFew, given = some_many ? many : few;
-  uint64_t want = (fill + given - 1) / given;
-  const uint64_t most = (uint64_t)keys / (wide ? 4 * kLeastPart : kLeastPart);
+  // 16 wavefronts to a workgroup instead of parts, and no join, where that takes few steps.  8 heads; 1 sequence of 500 / 1500 / 2000 / 3000
+  // keys: 10.4 / 14.1 / 15.7 / 19.6 us, as parts 11.5 / 16.0 / 16.4 / 16.4; 24 of 2600 / 4000 / 8000: 20 / 26 / 44, as parts 23 / 29 / 44.
+  const bool wide = D < 256 && !some_many && a.few_rows == 4 && few * 4 <= kFillFew && keys <= (few * 8 <= kFillFew ? 2048 : 4096);
+  const uint64_t fill = some_many ? kFillMany : kFillFew, given = some_many ? likely * a.c.heads : few;
+  // As many parts as the GPU holds at once, where their lengths are alike (one sequence) or there are many of a sequence: some more of them
+  // would run alone at the end (12 sequences of 30000 keys 85 us, these 76; 300 rows over 30000 keys 348, these 256).  Otherwise one more, for
+  // lengths differ (70 sequences of 1000 - 12000 keys: 106 us against 132).
+  uint64_t want = wide ? 1 : given * (a.b.n_seqs == 1 ? 2 : 8) <= fill ? fill / given : (fill + given - 1) / given;
+  // Keys that are worth a part of their own: 256, or 512 where few rows have many workgroups anyway (8 sequences of 8000 keys, 64 workgroups: 23
+  // us, with 512 26; 8 tokens over 1000 keys 26, with 512 43; 24 sequences with 12 heads and a window of 1000 keys 19, with 512 16).
+  const uint64_t most = (uint64_t)keys / (some_many || given * 8 <= fill ? 256 : 512);
   if (want > most) want = most;
   if (want > fit) want = fit;
   if (want > 4096) want = 4096;
@@ -1767,7 +1786,7 @@ int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace,
     else rc = launch(k_attend_many<DT, D, NQ, DT == PLORA_F32 ? 2 : 1>, many, (unsigned)a.parts, 1, a, stream);
   }
   if (rc == PLORA_OK && a.parts > 1) {
-    // threads of a row, times D/8: as many as there are parts, up to a workgroup's
+    // threads of a row, times D/8: as many as there are parts, up to a workgroup's (64 parts 57 us, with one each 63)
     constexpr int MOST = kThreads / (D / 8);
     const int g = a.parts <= 4 ? 1 : a.parts <= 16 ? 4 : MOST;
     rc = launch(g == 1 ? k_attend_join<DT, D, R, 1> : g == 4 ? k_attend_join<DT, D, R, 4> : k_attend_join<DT, D, R, MOST>,
