@@ -3,6 +3,7 @@ without a GPU; the pointers are never followed."""
 import ctypes as C
 
 import pytest
+import torch  # noqa: F401  (ahead of the package: both then share the HIP runtime that torch brings)
 
 import paper_2512_20210_amd as P
 
