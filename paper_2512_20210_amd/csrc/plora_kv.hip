@@ -574,8 +574,8 @@ __device__ __forceinline__ void transpose_nibbles(uint32_t* w) {
 
 // Values: codes of 32 rows through LDS, then one thread takes 8 channels of the 8 tokens of a quad and transposes them into 8
 // words.  Words of which only some tokens are the call's are read first.
-// 36.8 us for 5k tokens of 32 heads of 128, bf16 (107 MB, 3.1 TB/s): half of it vector instructions (min and max, the exact quotient, packing),
-// the other half the read.
+// 36.8 us for 5k tokens of 32 heads of 128, bf16 (107 MB, 2.9 TB/s): vector instructions are two thirds of the time (min and max, the exact
+// quotient, packing).
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void k_append(CacheArgs a) {
   constexpr int C = D / 8;
@@ -1577,7 +1577,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
   }
 }
 
-// Joins the parts of a row: 4 to 5 us, a launch and its first loads.  D/8 threads have 8 channels each, G times over: group g of them takes the parts g, g + G, ..., and the
+// Joins the parts of a row: 4 to 7 us, a launch and its loads.  D/8 threads have 8 channels each, G times over: group g of them takes the parts g, g + G, ..., and the
 // groups' sums are joined in their order.  R: rows of a tile of k_attend_many.
 template <int DT, int D, int R, int G>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
