@@ -1491,7 +1491,8 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
 template <int DT, int D, int NQ, int HQ>
 __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
   constexpr int HW = DT == PLORA_F32 ? 2 : 1, R = 16 * NQ;
-  // Two workgroups share a CU.  Low halves of 32 rows of 128 channels do not fit the registers beside the rest: they stay in LDS,
+  // Two workgroups share a CU, also where 29 registers go to scratch for it (fp32, heads of 256: 2048 tokens with 8 heads 103 us; with one
+  // workgroup and none in scratch 144).  Low halves of 32 rows of 128 channels do not fit the registers beside the rest: they stay in LDS,
   // which then holds stages of 32 keys instead of 64 (fp16 1.64 ms either way; with the halves in registers 2.77; bf16 with 32 keys
   // 1.44 instead of 1.40).
   constexpr bool LOW_IN_LDS = HQ == 2 && NQ == 2 && D == 128;
