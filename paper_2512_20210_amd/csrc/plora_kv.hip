@@ -703,9 +703,14 @@ __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
 //
 // Softmax in one pass: weights are p = 2^(x - ref), x = scale * log2(e) * q.K.  w = p * scale_s has to fit fp16 without loss, so ref
 // is chosen for the largest x + log2(max(scale_s, |min_s| / 8)): that product is brought to 2^8 and may grow to 2^15
-// before ref is moved (and the sums are multiplied), which after a row's first keys hardly ever happens.
+// before ref is moved (and the sums are multiplied), which after a row's first keys hardly ever happens.  A value of scale 0 has no w, and
+// one with a small scale a small w, but their min weighs p * min all the same: ref is also moved before a step's sum of these passes
+// 2^100 (or is inf - inf), so that the sums stay far from fp32's limit whatever the values are.
 
 constexpr float kNoRef = -3e38f;  // ref before the first key: the weight of any x is over its limit
+// Whether a step's weights ask for another ref.  top: their largest w; l, z: their sums.  (A w or l that is NaN asks for none; a z
+// that is asks in vain if a key or value is, which changes nothing.)
+__device__ __forceinline__ bool outgrown(float top, float l, float z) { return fmaxf(top, l * 0x1p-93f) > 0x1p15f || !(fabsf(z) < 0x1p100f); }
 
 struct AttendArgs {
   Cache c;
@@ -1101,7 +1106,7 @@ __device__ __forceinline__ void weights64(const uint4* vparams, const Column& q,
       z = __builtin_fmaf(p, __builtin_fmaf(8.f, param_scale(vp[n]), param_min(vp[n])), z);
       top = fmaxf(top, w[n]);
     }
-    if (turn || !__any(fmaxf(top, l * 0x1p-93f) > 0x1p15f)) break;  // (a NaN is none: it stays where it is)
+    if (turn || !__any(outgrown(top, l, z))) break;
     float best = -INFINITY;
 #pragma unroll
     for (int n = 0; n < R; ++n) {
@@ -1422,9 +1427,10 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) vc[i] = __builtin_bit_cast(f16x8, b.values[block * (D / 16) + i][lane]);
   auto weights = [&]() {
-    float top = 0.f;
+    bool more = false;
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
+      float top = 0.f;
       l[j] = z[j] = 0.f;
 #pragma unroll
       for (int n = 0; n < 8; ++n) {
@@ -1434,11 +1440,11 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
         z[j] = __builtin_fmaf(p, vm[n >> 2][n & 3], z[j]);
         top = fmaxf(top, w[j][n]);
       }
-      top = fmaxf(top, l[j] * 0x1p-93f);
+      more |= outgrown(top, l[j], z[j]);
     }
-    return top;
+    return more;
   };
-  if (__any(weights() > 0x1p15f)) {  // (a NaN is none: it stays where it is)
+  if (__any(weights())) {
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
       float best = -INFINITY;

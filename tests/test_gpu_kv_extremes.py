@@ -1,0 +1,31 @@
+"""Attention over the KV cache where sizes, lengths and settings are far apart or at their limits, against the oracle's 64 bits.  The bounds
+are those of test_gpu_kv.py, from the arithmetic, where an input gives no other reason."""
+import numpy as np
+import pytest
+
+from test_gpu_kv import Setup, check_attention
+
+pytestmark = pytest.mark.gpu
+
+# One sequence in every kernel and form of it: tokens, tokens ahead of them, query heads, workspace.
+FORMS = {"few, 4 rows, 16 wavefronts": (1, 1100, 2, 0), "few, 4 rows, 4 wavefronts": (1, 2300, 2, 0), "few, 8 rows": (2, 700, 4, 0),
+         "few, 16 rows": (4, 700, 4, 0), "few, parts": (1, 4500, 2, 1 << 22), "many": (40, 500, 2, 0), "many, parts": (40, 3000, 2, 1 << 24)}
+
+
+def one(form, dtype, d=64, seed=0):
+    """(Setup of one sequence, query heads, workspace, places)"""
+    new, ctx, heads, workspace = FORMS[form]
+    return Setup(dtype, 1, d, 64, [new], [ctx], seed=seed), heads, workspace, new + ctx
+
+
+# ---- values of very different size ------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("signs", ["one", "both"])
+def test_constant_rows_behind_rows_of_zeros(form, dtype, signs):
+    """Values of scale 0: their weights meet their min only.  All logits are about the same."""
+    s, heads, workspace, n = one(form, dtype)
+    c = 1e9 * np.where((np.arange(n) % 2 == 0) | (signs == "one"), 1.0, -0.75)
+    c[:n // 2] = 0
+    check_attention(s, heads, vals=[np.broadcast_to(c[:, None, None], (n, 1, 64))], q_std=0.1, workspace=workspace)
