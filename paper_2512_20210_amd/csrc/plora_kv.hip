@@ -719,21 +719,26 @@ struct AttendArgs {
   Rotary r;
   int32_t heads, rep;          // query heads; query heads per kv head
   float scale;                 // * log2(e)
-  int32_t causal, window;
+  int32_t causal, window;      // window: 0 (none), or below the batch's max_len
   int32_t part_keys, parts;    // keys of a part (a multiple of kKeyAlign), parts at most; 1: results go to out
   int32_t few_rows;            // k_attend_few has the sequences with at most so many rows, k_attend_many the others
   float *part_o, *part_ml;     // [part][token][head][head_dim], [part][token][head][2]: sums, (ref, weights)
 };
 constexpr int kMostFew = 16;
 
+// Place of a sequence's token t; -1 for all that lie ahead of the first one: they see no key, and a window taken off stays within 32 bits.
+__device__ __forceinline__ int place_of(const Seq& s, int t) {
+  const int p = s.len - s.n + t;
+  return p < -1 ? -1 : p;
+}
 // Keys [lo, hi) that rows r0 .. r1-1 of a sequence see, lo on a boundary of kKeyAlign.
 __device__ __forceinline__ void keys_of_rows(const Seq& s, const AttendArgs& a, int r0, int r1, int* lo, int* hi) {
   *lo = 0;
   *hi = s.len;
   if (a.causal) {
-    const int p0 = s.len - s.n + r0 / a.rep, p1 = s.len - s.n + (r1 - 1) / a.rep;
-    *hi = p1 + 1 < 0 ? 0 : p1 + 1;
-    if (a.window) *lo = (p0 - a.window + 1 < 0 ? 0 : p0 - a.window + 1) & ~(kKeyAlign - 1);
+    const int p0 = place_of(s, r0 / a.rep), p1 = place_of(s, (r1 - 1) / a.rep);
+    *hi = p1 + 1;
+    if (a.window && p0 >= a.window) *lo = (p0 - a.window + 1) & ~(kKeyAlign - 1);
   }
 }
 
@@ -872,7 +877,7 @@ template <int D, int NQ, int H, int HQ>
 __device__ __forceinline__ void take_queries(Queries<D, NQ, H>* o, int j, const QueryRows<D, HQ, 16>& from, const AttendArgs& a, const Seq& s, int r0, int rows, int lane) {
   const int r = lane & 15, g = lane >> 4;
   const int row = r0 + r < rows ? r0 + r : rows - 1;
-  o->place[j] = a.causal ? s.len - s.n + row / a.rep : 0x7fffffff;
+  o->place[j] = a.causal ? place_of(s, row / a.rep) : 0x7fffffff;
 #pragma unroll
   for (int h = 0; h < H; ++h) {
 #pragma unroll
@@ -1227,16 +1232,16 @@ __global__ __launch_bounds__(64 * WAVES, (few_waves<DT, D, R>())) void k_attend_
   stage_queries<DT, D, HQ, R, THREADS>(&query_rows, a, sq, kvh, 0, rows, threadIdx.x);
   __syncthreads();
   const int own_row = (lane & 15) % R;
-  const Column q{query_rows.sum[own_row], HW == 1 ? -64.f * query_rows.sum[own_row] : 0.f, query_rows.f[own_row], a.causal ? sq.len - sq.n + (own_row < rows ? own_row : rows - 1) / a.rep : 0x7fffffff};
+  const Column q{query_rows.sum[own_row], HW == 1 ? -64.f * query_rows.sum[own_row] : 0.f, query_rows.f[own_row], a.causal ? place_of(sq, (own_row < rows ? own_row : rows - 1) / a.rep) : 0x7fffffff};
   const CodeBits bits = code_bits();
   Sums<D, 1> s;
   clear(&s);
-  const int first_place = sq.len - sq.n;
+  const int first_place = place_of(sq, 0);
   while (key < to) {
     float x[R], w[R];
     logits64<D, R, HQ, HW == 1>(k, query_rows, q, bits, x, lane);
     load_keys(&k, a, next, head_at, key + kStep, lane);
-    const bool whole = here.page0 && here.page1 && key + 64 <= to && (!a.causal || (key + 63 <= first_place && (!a.window || key > first_place + sq.n - 1 - a.window)));
+    const bool whole = here.page0 && here.page1 && key + 64 <= to && (!a.causal || (key + 63 <= first_place && (!a.window || key > sq.len - 1 - a.window)));
     if (!whole) mask64<D, R>(x, v.vp, q, here, key, to, a.window, lane);
     weights64<D, R>(v.vp, q, &s, x, w);
     add_values64<D, R, HW>(v.v, w, &s, bits, lane);
@@ -1551,7 +1556,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
   Sums<D, NQ> s;
   clear(&s);
   // places of the wavefront's first and last row, if what a row sees goes by its place
-  const int first = a.causal ? sq.len - sq.n + r0 / a.rep : 0x7fffffff, last = a.causal ? sq.len - sq.n + (r1 - 1) / a.rep : 0x7fffffff;
+  const int first = a.causal ? place_of(sq, r0 / a.rep) : 0x7fffffff, last = a.causal ? place_of(sq, (r1 - 1) / a.rep) : 0x7fffffff;
   int at = 0;
   for (int key = from; key < to; key += K) {
 #pragma unroll 1
@@ -1911,7 +1916,7 @@ extern "C" int plora_kv_attend(const plora_kv_cache* cache, const plora_kv_batch
   a.rep = n_heads / cache->n_kv_heads;
   a.scale = scale * 1.44269504088896341f;
   a.causal = causal != 0;
-  a.window = window;
+  a.window = window < a.b.max_len ? window : 0;  // a window that holds every sequence is none
   return cache->dtype == PLORA_BF16  ? attend<PLORA_BF16>(cache->head_dim, a, batch->max_new, workspace_bytes, workspace, stream)
          : cache->dtype == PLORA_F16 ? attend<PLORA_F16>(cache->head_dim, a, batch->max_new, workspace_bytes, workspace, stream)
                                      : attend<PLORA_F32>(cache->head_dim, a, batch->max_new, workspace_bytes, workspace, stream);

@@ -29,3 +29,12 @@ def test_constant_rows_behind_rows_of_zeros(form, dtype, signs):
     c = 1e9 * np.where((np.arange(n) % 2 == 0) | (signs == "one"), 1.0, -0.75)
     c[:n // 2] = 0
     check_attention(s, heads, vals=[np.broadcast_to(c[:, None, None], (n, 1, 64))], q_std=0.1, workspace=workspace)
+
+
+# ---- settings at their limits -------------------------------------------------------------------------
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 4, 2 ** 30, 50])
+@pytest.mark.parametrize("new,length,heads", [([9, 1], [4, 60], 1), ([40, 3], [31, 70], 2), ([200, 1], [150, 1], 1)])
+def test_wide_windows_and_negative_places(window, new, length, heads):
+    """The window's first place lies before 0, by up to 2^31 and a few."""
+    check_attention(Setup("bf16", 1, 64, 32, new, [l - n for l, n in zip(length, new)]), heads, window=window)
