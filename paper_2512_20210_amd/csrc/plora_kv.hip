@@ -725,6 +725,7 @@ struct AttendArgs {
   float *part_o, *part_ml;     // [part][token][head][head_dim], [part][token][head][2]: sums, (ref, weights)
 };
 constexpr int kMostFew = 16;
+constexpr int kMostKeys = 1 << 30;  // of a sequence: the steps and parts behind the last key, and a window ahead of it, stay within 32 bits
 
 // Place of a sequence's token t; -1 for all that lie ahead of the first one: they see no key, and a window taken off stays within 32 bits.
 __device__ __forceinline__ int place_of(const Seq& s, int t) {
@@ -1906,6 +1907,7 @@ extern "C" int plora_kv_attend(const plora_kv_cache* cache, const plora_kv_batch
   if (batch->n_tokens == 0 || batch->n_seqs == 0) return PLORA_OK;
   if (!good_rows(q, cache->dtype) || !good_output(out, cache->dtype, batch->n_tokens, n_heads, cache->head_dim)) return PLORA_ERR_INVAL;
   if ((int64_t)batch->n_tokens * (n_heads / cache->n_kv_heads) > 0x7fffffff) return PLORA_ERR_LIMIT;
+  if (device_batch(cache, batch).max_len > kMostKeys) return PLORA_ERR_LIMIT;
   AttendArgs a;
   a.c = device_cache(cache);
   a.b = device_batch(cache, batch);

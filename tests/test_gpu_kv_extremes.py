@@ -38,3 +38,12 @@ def test_constant_rows_behind_rows_of_zeros(form, dtype, signs):
 def test_wide_windows_and_negative_places(window, new, length, heads):
     """The window's first place lies before 0, by up to 2^31 and a few."""
     check_attention(Setup("bf16", 1, 64, 32, new, [l - n for l, n in zip(length, new)]), heads, window=window)
+
+
+@pytest.mark.parametrize("new,ctx", [([1, 1], [4000, 9]), ([40, 1], [300, 77])])
+def test_a_max_len_far_above_the_table(new, ctx):
+    """max_len is a bound: the table holds 64 or 5 pages."""
+    s = Setup("bf16", 1, 64, 64, new, ctx)
+    plain = s.batch
+    s.batch = lambda positions=None: plain(positions, max_len=2 ** 31 - 1)
+    check_attention(s, 2)
