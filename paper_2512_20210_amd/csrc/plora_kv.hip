@@ -706,8 +706,15 @@ __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
 // before ref is moved (and the sums are multiplied), which after a row's first keys hardly ever happens.  A value of scale 0 has no w, and
 // one with a small scale a small w, but their min weighs p * min all the same: ref is also moved before a step's sum of these passes
 // 2^100 (or is inf - inf), so that the sums stay far from fp32's limit whatever the values are.
+//
+// Two refs may be further apart than fp32 reaches although the weights behind them are alike (values of 0, held against 2^-90, and of
+// 1e25: 2^171).  Then 2^(old - new) is 0, which is right for the sums over values, whose size is in it, but not for the sum of the weights: that
+// product is a number again.  So refs are whole numbers, and the sum's exponent is moved.  Weights below 2^-126 are 0; the
+// largest is at least 2^(7 - e) with e = floor(log2(max(scale, |min| / 8))) of some value that is seen: 96 for values of 1e30, 124 at most.
 
 constexpr float kNoRef = -3e38f;  // ref before the first key: the weight of any x is over its limit
+// A sum of weights as ref moves up by -by, a whole number (or less than all refs are apart).
+__device__ __forceinline__ float moved(float sum, float by) { return __builtin_ldexpf(sum, (int)fmaxf(by, -1000.f)); }
 // Whether a step's weights ask for another ref.  top: their largest w; l, z: their sums.  (A w or l that is NaN asks for none; a z
 // that is asks in vain if a key or value is, which changes nothing.)
 __device__ __forceinline__ bool outgrown(float top, float l, float z) { return fmaxf(top, l * 0x1p-93f) > 0x1p15f || !(fabsf(z) < 0x1p100f); }
@@ -1121,9 +1128,9 @@ __device__ __forceinline__ void weights64(const uint4* vparams, const Column& q,
     }
     best = fmaxf(best, __shfl_xor(best, 16));
     best = fmaxf(best, __shfl_xor(best, 32));
-    const float ref = fmaxf(s->ref[0], best - 8.f), down = __builtin_amdgcn_exp2f(s->ref[0] - ref);
+    const float ref = fmaxf(s->ref[0], ceilf(best - 8.f)), by = s->ref[0] - ref, down = __builtin_amdgcn_exp2f(by);
     s->ref[0] = ref;
-    s->l[0] *= down;
+    s->l[0] = moved(s->l[0], by);
     s->z[0] *= down;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) s->o[0][i] *= down;
@@ -1188,19 +1195,18 @@ __device__ __forceinline__ void join_columns(Sums<D, 1>* s) {
   if constexpr (R == 16) return;
   float ref = fmaxf(s->ref[0], round16<8>(s->ref[0]));
   if constexpr (R == 4) ref = fmaxf(ref, round16<4>(ref));
-  const float f = __builtin_amdgcn_exp2f(s->ref[0] - ref);
+  const float by = s->ref[0] - ref, f = __builtin_amdgcn_exp2f(by);
   s->ref[0] = ref;
   auto join = [&](float v) {
-    v *= f;
     v += round16<8>(v);
     if constexpr (R == 4) v += round16<4>(v);
     return v;
   };
-  s->l[0] = join(s->l[0]);
+  s->l[0] = join(moved(s->l[0], by));
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) s->o[0][i][k] = join(s->o[0][i][k]);
+    for (int k = 0; k < 4; ++k) s->o[0][i][k] = join(s->o[0][i][k] * f);
   }
 }
 // Wavefronts of a SIMD that the registers are shared among: as many as the sums and a step's rows leave room for without spills.
@@ -1271,8 +1277,8 @@ __global__ __launch_bounds__(64 * WAVES, (few_waves<DT, D, R>())) void k_attend_
     float l = 0.f, o[8] = {};
 #pragma unroll 2
     for (int k = 0; k < WAVES; ++k) {
-      const float f = __builtin_amdgcn_exp2f(sm[k][row] - ref);
-      l = __builtin_fmaf(f, sl[k][row], l);
+      const float by = sm[k][row] - ref, f = __builtin_amdgcn_exp2f(by);
+      l += moved(sl[k][row], by);
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = __builtin_fmaf(f, so[k][row][c + e], o[e]);
     }
@@ -1461,9 +1467,9 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
       }
       best = fmaxf(best, __shfl_xor(best, 16));
       best = fmaxf(best, __shfl_xor(best, 32));
-      const float ref = fmaxf(s->ref[j], best - 8.f), down = __builtin_amdgcn_exp2f(s->ref[j] - ref);
+      const float ref = fmaxf(s->ref[j], ceilf(best - 8.f)), by = s->ref[j] - ref, down = __builtin_amdgcn_exp2f(by);
       s->ref[j] = ref;
-      s->l[j] *= down;
+      s->l[j] = moved(s->l[j], by);
       s->z[j] *= down;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) s->o[j][i] *= down;
@@ -1620,11 +1626,11 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
 #pragma unroll 4
     for (int k = g; k < n; k += G) {
       const float2 m = ml[k * all + row];
-      const float f = __builtin_amdgcn_exp2f(m.x - ref);
+      const float by = m.x - ref, f = __builtin_amdgcn_exp2f(by);
       const float4* p = reinterpret_cast<const float4*>(a.part_o + (k * all + row) * D + c);
       const float4 u = p[0], v = p[1];
       const float e[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-      l = __builtin_fmaf(f, m.y, l);
+      l += moved(m.y, by);
 #pragma unroll
       for (int i = 0; i < 8; ++i) o[i] = __builtin_fmaf(f, e[i], o[i]);
     }
@@ -1645,8 +1651,8 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
     for (int i = 0; i < 8; ++i) o[i] = 0.f;
 #pragma unroll
     for (int k = 0; k < G; ++k) {
-      const float f = __builtin_amdgcn_exp2f(sm[k][mine] - ref);
-      l = __builtin_fmaf(f, sl[k][mine], l);
+      const float by = sm[k][mine] - ref, f = __builtin_amdgcn_exp2f(by);
+      l += moved(sl[k][mine], by);
 #pragma unroll
       for (int i = 0; i < 8; ++i) o[i] = __builtin_fmaf(f, so[k][mine][c + i], o[i]);
     }

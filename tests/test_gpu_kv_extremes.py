@@ -47,3 +47,17 @@ def test_a_max_len_far_above_the_table(new, ctx):
     plain = s.batch
     s.batch = lambda positions=None: plain(positions, max_len=2 ** 31 - 1)
     check_attention(s, 2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("light", [0.0, 1e-25])
+@pytest.mark.parametrize("stripe", [16, 32, 64, "light first", "heavy first"])
+def test_light_and_heavy_values_of_the_same_weight(form, dtype, light, stripe):
+    """Values of 1e25 and next to nothing, in steps, columns, wavefronts and parts of their own: what the sums are held against differs by
+    up to 2^180, the weights do not."""
+    s, heads, workspace, n = one(form, dtype)
+    at = np.arange(n)
+    heavy = at >= n // 2 if stripe == "light first" else at < n // 2 if stripe == "heavy first" else at // stripe % 2 == 1
+    v = (2 + 0.3 * s.rng.normal(size=(n, 1, 64))) * np.where(heavy, 1e25, light)[:, None, None]
+    check_attention(s, heads, vals=[v], q_std=0.1, workspace=workspace)
