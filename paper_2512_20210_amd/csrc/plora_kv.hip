@@ -715,9 +715,11 @@ __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
 constexpr float kNoRef = -3e38f;  // ref before the first key: the weight of any x is over its limit
 // A sum of weights as ref moves up by -by, a whole number (or less than all refs are apart).
 __device__ __forceinline__ float moved(float sum, float by) { return __builtin_ldexpf(sum, (int)fmaxf(by, -1000.f)); }
-// Whether a step's weights ask for another ref.  top: their largest w; l, z: their sums.  (A w or l that is NaN asks for none; a z
-// that is asks in vain if a key or value is, which changes nothing.)
-__device__ __forceinline__ bool outgrown(float top, float l, float z) { return fmaxf(top, l * 0x1p-93f) > 0x1p15f || !(fabsf(z) < 0x1p100f); }
+// Whether a step's weights ask for another ref.  top: their largest w; l: the lane's sum of weights with them; z: their sum with min.  A lane's l
+// may grow to 2^109: the 2^8 lanes and wavefronts that share a row, and 2^10 parts, do not bring it past fp32.  (Weights next to values of 0 are
+// 2^98 after a move, so a lane with thousands of these asks every time, in vain.  A w or l that is NaN asks for none; a z that is asks
+// in vain if a key or value is, which changes nothing.)
+__device__ __forceinline__ bool outgrown(float top, float l, float z) { return fmaxf(top, l * 0x1p-94f) > 0x1p15f || !(fabsf(z) < 0x1p100f); }
 
 struct AttendArgs {
   Cache c;
@@ -1119,7 +1121,7 @@ __device__ __forceinline__ void weights64(const uint4* vparams, const Column& q,
       z = __builtin_fmaf(p, __builtin_fmaf(8.f, param_scale(vp[n]), param_min(vp[n])), z);
       top = fmaxf(top, w[n]);
     }
-    if (turn || !__any(outgrown(top, l, z))) break;
+    if (turn || !__any(outgrown(top, s->l[0] + l, z))) break;
     float best = -INFINITY;
 #pragma unroll
     for (int n = 0; n < R; ++n) {
@@ -1452,7 +1454,7 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
         z[j] = __builtin_fmaf(p, vm[n >> 2][n & 3], z[j]);
         top = fmaxf(top, w[j][n]);
       }
-      more |= outgrown(top, l[j], z[j]);
+      more |= outgrown(top, s->l[j] + l[j], z[j]);
     }
     return more;
   };

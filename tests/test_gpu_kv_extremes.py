@@ -3,7 +3,7 @@ are those of test_gpu_kv.py, from the arithmetic, where an input gives no other 
 import numpy as np
 import pytest
 
-from test_gpu_kv import Setup, check_attention
+from test_gpu_kv import Setup, check_attention, host, ints, stream
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +61,31 @@ def test_light_and_heavy_values_of_the_same_weight(form, dtype, light, stripe):
     heavy = at >= n // 2 if stripe == "light first" else at < n // 2 if stripe == "heavy first" else at // stripe % 2 == 1
     v = (2 + 0.3 * s.rng.normal(size=(n, 1, 64))) * np.where(heavy, 1e25, light)[:, None, None]
     check_attention(s, heads, vals=[v], q_std=0.1, workspace=workspace)
+
+
+def test_weights_of_millions_of_keys_without_values():
+    """Keys whose values are 0 leave the reference far below, so their weights are large numbers: 2^23 of them, then 256 values of 1.  The pages
+    in between are the same one.  Bound: a lane's sum has 2^15 additions, each rounded by 2^-24 of it at most."""
+    import torch
+    import paper_2512_20210_amd as P
+    from oracle import kv as O
+    columns = (1 << 15) + 2
+    pages = np.zeros((3, P.PagedKvCache.page_bytes(1, 64, 256)), np.uint8)
+    o = O.KvOracle(pages, 1, 64, 256)
+    key = 7.5 * np.log(2) / (64 * 0.125)  # logit of 7.5 to base 2 with a q of ones
+    for page, (k, v) in enumerate(((0, 0), (key, 0), (key, 1))):
+        for values, x in ((0, k), (1, v)):
+            c, sc, m = O.chosen(np.full((1, 64), x), 32)
+            for slot in range(256):
+                o.write(page, slot, 0, values, c[0], sc[0], m[0])
+            if page == 1 and not values:
+                held = float(m[0])
+    table = torch.ones(1, columns, dtype=torch.int32, device="cuda")
+    table[0, 0], table[0, -1] = 0, 2
+    cache = P.PagedKvCache(P.PLORA_F32, 1, 64, 256, torch.from_numpy(pages).cuda())
+    length = columns * 256
+    batch = P.KvBatch(ints([0, 1]), ints([length]), table, 1, 1, length)
+    q, out = torch.ones(1, 1, 64, device="cuda"), torch.zeros(1, 1, 64, device="cuda")
+    cache.attend(batch, q, out, 0.125, None, stream=stream())
+    ref = 256 / (256 * np.exp(-8 * held) + 256 * (columns - 1))
+    assert np.abs(host(out) / ref - 1).max() <= 2.0 ** -9 + 2.0 ** -18
