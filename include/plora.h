@@ -466,7 +466,7 @@ uint64_t plora_kv_page_bytes(const plora_kv_cache* cache);
  * Out of range: tok_start is held to [0, n_tokens] and kv_len to [0, min(max_len, table_stride * page_tokens)]; a page outside
  * [0, n_pages) is a hole: nothing is appended there, it reads as NaN, and attention passes over its tokens; tokens at
  * negative places are not appended, read as NaN and see no key (unless attention is not causal).  More than max_new tokens
- * of a sequence: those beyond may be left out.  Rows of no sequence are left alone.  Sequences may share pages that are
+ * of a sequence: those beyond may be left out, the first max_new are not.  Rows of no sequence are left alone.  Sequences may share pages that are
  * only read; two that append to one page race. */
 typedef struct {
   int32_t n_seqs, n_tokens;

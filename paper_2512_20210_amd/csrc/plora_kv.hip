@@ -727,6 +727,7 @@ struct AttendArgs {
   Rows q, out;
   Rotary r;
   int32_t heads, rep;          // query heads; query heads per kv head
+  int32_t max_new;             // tokens of a sequence that have a result, at most
   float scale;                 // * log2(e)
   int32_t causal, window;      // window: 0 (none), or below the batch's max_len
   int32_t part_keys, parts;    // keys of a part (a multiple of kKeyAlign), parts at most; 1: results go to out
@@ -736,6 +737,8 @@ struct AttendArgs {
 constexpr int kMostFew = 16;
 constexpr int kMostKeys = 1 << 30;  // of a sequence: the steps and parts behind the last key, and a window ahead of it, stay within 32 bits
 
+// Rows of a sequence and kv head.  Every kernel of a call counts the same ones: the join must not meet a row that nobody had.
+__device__ __forceinline__ int rows_of(const Seq& s, const AttendArgs& a) { return (s.n < a.max_new ? s.n : a.max_new) * a.rep; }
 // Place of a sequence's token t; -1 for all that lie ahead of the first one: they see no key, and a window taken off stays within 32 bits.
 __device__ __forceinline__ int place_of(const Seq& s, int t) {
   const int p = s.len - s.n + t;
@@ -1221,7 +1224,7 @@ __global__ __launch_bounds__(64 * WAVES, (few_waves<DT, D, R>())) void k_attend_
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int seq = blockIdx.x / a.c.heads, kvh = blockIdx.x - seq * a.c.heads, part = blockIdx.y;
   const Seq sq = seq_at(a.b, seq);
-  const int rows = sq.n * a.rep;
+  const int rows = rows_of(sq, a);
   if (rows == 0 || rows > R) return;
   int lo, hi;
   keys_of_rows(sq, a, 0, rows, &lo, &hi);
@@ -1527,7 +1530,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
   const int kvh = (int)(blockIdx.x - number * a.c.heads), part = blockIdx.y;
   const int seq = find_seq(a.b, number, a.rep, R * kWaves, 1);
   const Seq sq = seq_at(a.b, seq);
-  const int rows = sq.n * a.rep;
+  const int rows = rows_of(sq, a);
   if (rows <= a.few_rows) return;
   const int64_t tile = number - first_number(a.b, seq, a.rep, R * kWaves, 1);
   if (tile < 0 || tile * (R * kWaves) >= rows) return;
@@ -1612,9 +1615,9 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
   int seq = find_seq(a.b, first_row / a.heads, 1, 1, 0);
   while (seq + 1 < a.b.n_seqs && hold(a.b.tok_start[seq + 1], a.b.n_tokens) <= tok) ++seq;
   const Seq sq = seq_at(a.b, seq);
-  const int t = tok - sq.first, rows = sq.n * a.rep;
+  const int t = tok - sq.first, rows = rows_of(sq, a);
   int n = 1;
-  if (t >= 0 && t < sq.n) {
+  if (t >= 0 && t * a.rep < rows) {
     const int r0 = (t * a.rep + h % a.rep) / R * R, r1 = r0 + R < rows ? r0 + R : rows;  // (a tile of k_attend_few is one of these too: R >= 16)
     int lo, hi;
     keys_of_rows(sq, a, r0, r1, &lo, &hi);
@@ -1762,6 +1765,7 @@ int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace,
   constexpr int NQ = columns_of<DT, D>(), R = 16 * NQ * kWaves;
   const int64_t rows = (int64_t)a.b.n_tokens * a.heads;
   if (max_new > a.b.n_tokens) max_new = a.b.n_tokens;
+  a.max_new = max_new;
   const int64_t most_rows = (int64_t)max_new * a.rep;
   const bool some_many = most_rows > kMostFew;
   // Sequences of few rows among ones of many are left to k_attend_many where they are rare and their keys not many: a launch

@@ -3,7 +3,7 @@ are those of test_gpu_kv.py, from the arithmetic, where an input gives no other 
 import numpy as np
 import pytest
 
-from test_gpu_kv import Setup, check_attention, host, ints, stream
+from test_gpu_kv import DT, Setup, check_attention, host, ints, put, stream
 
 pytestmark = pytest.mark.gpu
 
@@ -89,3 +89,30 @@ def test_weights_of_millions_of_keys_without_values():
     cache.attend(batch, q, out, 0.125, None, stream=stream())
     ref = 256 / (256 * np.exp(-8 * held) + 256 * (columns - 1))
     assert np.abs(host(out) / ref - 1).max() <= 2.0 ** -9 + 2.0 ** -18
+
+
+# ---- more rows than the call says --------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("max_new,new,ctx,heads,kvh", [(1, [2, 1, 5, 1], [4000, 300, 3000, 0], 4, 1), (1, [3, 1], [30, 100], 8, 8), (2, [2, 7, 1], [2000, 900, 90], 8, 2),
+                                                       (3, [1, 3, 4, 90], [900, 5000, 40, 4000], 8, 1), (30, [31, 1, 500], [3000, 7, 20], 2, 1)])
+@pytest.mark.parametrize("workspace", [0, 1 << 24])
+def test_more_tokens_than_max_new(dtype, max_new, new, ctx, heads, kvh, workspace):
+    """The first max_new tokens of a sequence have their results, the others may be left out; nothing of the workspace's contents shows."""
+    import torch
+    from oracle import kv as O
+    s = Setup(dtype, kvh, 64, 64, new, ctx, seed=max_new)
+    s.fill(*([s.rng.normal(size=(l, kvh, 64)) for l in s.len] for _ in range(2)))
+    s.to_gpu()
+    q, q64 = put(s.rng.normal(size=(s.tokens, heads, 64)), dtype)
+    out = torch.full_like(q, 9.0)
+    ws = torch.full((workspace // 4,), float("nan"), device="cuda") if workspace else None
+    s.cache.attend(s.batch(max_new=max_new), q, out, 0.125, ws, stream=stream())
+    got = host(out)
+    for i in range(len(new)):
+        rows = slice(s.start[i], s.start[i + 1])
+        ref, amp, size = O.attend(q64[rows], *s.rows(i), 0.125, s.places(i))
+        bound = DT[dtype][0] * np.abs(ref) + (amp * (2.0 ** -10 + 2.0 ** -15 * size))[..., None]
+        right, alone = np.abs(got[rows] - ref) <= bound, got[rows] == 9
+        assert right[:max_new].all()
+        assert (right[max_new:].all(-1) | alone[max_new:].all(-1)).all()
