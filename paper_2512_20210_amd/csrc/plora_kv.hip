@@ -698,8 +698,11 @@ __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
 //   sum p_s V[s] = sum (p_s scale_s)(code - 8) + sum p_s (min_s + 8 scale_s).
 // So a row of keys or values costs its codes' unpacking (9 instructions per 8 codes) and no multiplication by its scale, and what
 // lies in places that are not seen cannot hurt: codes are finite whatever the memory holds, and scale and min are dropped
-// where a key is masked.  q is multiplied by a power of two per row that brings it into fp16's range (undone in the softmax's
-// factor); fp32 rows, and their weights, go as a high and a low half.
+// where a key is masked.  q is multiplied by a power of two per row that brings it into fp16's range; fp32 rows, and their weights, go as a
+// high and a low half.  The power is undone where large keys do not meet it alone (keys of 1e34 and a q of 1e-34, times 2^122, have a logit of
+// the order of 1, but their products would pass fp32): with few rows half of it ahead of the key's scale and half in the softmax's
+// factor; with many rows, which have no instruction to spare, all of it in the factor, and 32 keys of which one is large are brought
+// down by 2^40.
 //
 // Softmax in one pass: weights are p = 2^(x - ref), x = scale * log2(e) * q.K.  w = p * scale_s has to fit fp16 without loss, so ref
 // is chosen for the largest x + log2(max(scale_s, |min_s| / 8)): that product is brought to 2^8 and may grow to 2^15
@@ -802,8 +805,8 @@ __device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __buil
 template <int D, int HQ, int R>
 struct QueryRows {
   uint4 q[HQ][R][D / 8 + 1];
-  float sum[R];  // of the scaled row
-  float f[R];    // scale * log2(e) / the row's power of two
+  float sum[R];        // of the scaled row
+  float f1[R], f2[R];  // a power of two, and scale * log2(e) / the row's power of two / f1
 };
 // THREADS threads (whole wavefronts) stage rows r0 .. r0 + R-1 of a sequence; behind the last row, that one again.
 template <int DT, int D, int HQ, int R, int THREADS, RotaryKind KIND>
@@ -862,7 +865,10 @@ __device__ __forceinline__ void stage_queries_of(QueryRows<D, HQ, R>* o, const A
       }
       if (part == 0) {
         o->sum[row] = sum;
-        o->f[row] = a.scale * __uint_as_float((uint32_t)(127 - e) << 23);
+        // (2^-12: products of a row near 1 are up to 2^22, so with half of the power alone keys past 2^106 would be too large)
+        const int e1 = e / 2 + 12;
+        o->f1[row] = __uint_as_float((uint32_t)(127 - e1) << 23);
+        o->f2[row] = a.scale * __uint_as_float((uint32_t)(127 - e + e1) << 23);
       }
     }
   }
@@ -897,7 +903,7 @@ __device__ __forceinline__ void take_queries(Queries<D, NQ, H>* o, int j, const 
     for (int i = 0; i < D / 32; ++i) o->q[j][h][i] = __builtin_bit_cast(f16x8, from.q[h][r][g * (D / 32) + i]);
   }
   o->sum[j] = from.sum[r];
-  o->f[j] = from.f[r];
+  o->f[j] = from.f1[r] * from.f2[r];
 }
 
 // Running sums of a column, per lane.
@@ -1050,11 +1056,11 @@ __device__ __forceinline__ void load_values(Values64<D, R>* o, const AttendArgs&
 
 // The row of a lane's column.
 struct Column {
-  float sum, start, f;  // start: what takes the keys' offset off
+  float sum, start, f1, f;  // the row's sum times f1; what takes the keys' offset off; the row's f1 and f2
   int place;  // last place that it sees
 };
 
-// Logits of a lane's keys, less what q.f multiplies them with.
+// Logits of a lane's keys, less q.f.
 template <int D, int R, int HQ, bool OVER64>
 __device__ __forceinline__ void logits64(const Keys64<D, R>& b, const QueryRows<D, HQ, R>& rows, const Column& q, const CodeBits& bits, float* x, int lane) {
   constexpr int U = R / 4, P = 16 / R;
@@ -1086,7 +1092,7 @@ __device__ __forceinline__ void logits64(const Keys64<D, R>& b, const QueryRows<
     for (int i = 0; i < 4; ++i) {
       const uint32_t kp = reinterpret_cast<const uint32_t*>(&b.kp[u])[i];
       const float s = param_scale(kp), m = param_min(kp);
-      x[4 * u + i] = __builtin_fmaf(s, c[u][i], (OVER64 ? m : __builtin_fmaf(8.f, s, m)) * q.sum);
+      x[4 * u + i] = __builtin_fmaf(s, c[u][i] * q.f1, (OVER64 ? m : __builtin_fmaf(8.f, s, m)) * q.sum);
     }
   }
 }
@@ -1244,7 +1250,8 @@ __global__ __launch_bounds__(64 * WAVES, (few_waves<DT, D, R>())) void k_attend_
   stage_queries<DT, D, HQ, R, THREADS>(&query_rows, a, sq, kvh, 0, rows, threadIdx.x);
   __syncthreads();
   const int own_row = (lane & 15) % R;
-  const Column q{query_rows.sum[own_row], HW == 1 ? -64.f * query_rows.sum[own_row] : 0.f, query_rows.f[own_row], a.causal ? place_of(sq, (own_row < rows ? own_row : rows - 1) / a.rep) : 0x7fffffff};
+  const float f1 = query_rows.f1[own_row];
+  const Column q{query_rows.sum[own_row] * f1, HW == 1 ? -64.f * query_rows.sum[own_row] : 0.f, f1, query_rows.f2[own_row], a.causal ? place_of(sq, (own_row < rows ? own_row : rows - 1) / a.rep) : 0x7fffffff};
   const CodeBits bits = code_bits();
   Sums<D, 1> s;
   clear(&s);
@@ -1305,7 +1312,9 @@ struct Stage {
   uint4 keys[K / 16 * (D / 32)][64];    // [tile of 16 keys][32 channels], then lanes
   uint4 values[K / 32 * (D / 16)][64];  // [32 keys][16 channels]
   float ks[K], km[K], vs[K], vm[K];     // scale and min + 8 scale of keys and of values, of these 0 where there is no row
+  float up[K / 32];                     // what the 32 keys' ks and km are short of: 1, or 2^40 where one of them is large
 };
+constexpr float kLargeKey = 0x1p90f;
 // The pages of a stage's two blocks of 32 keys, read a stage before they are used: -1 behind `to`.
 struct PageIds {
   int32_t p0, p1;
@@ -1377,8 +1386,12 @@ __device__ __forceinline__ void unpack(Stage<D, K>* o, const Fetched<W>& f, cons
     // not has a weight of 0 that meets nothing but numbers.
     const float s = param_scale(f.vp), m = __builtin_fmaf(8.f, s, param_min(f.vp));
     const bool fine = fabsf(s) < INFINITY && fabsf(m) < INFINITY;
-    o->ks[lane] = fine ? param_scale(f.kp) : __builtin_nanf("");
-    o->km[lane] = __builtin_fmaf(8.f, param_scale(f.kp), param_min(f.kp));
+    const float ks = param_scale(f.kp), km = __builtin_fmaf(8.f, ks, param_min(f.kp));
+    const bool large = (uint32_t)(__ballot(fmaxf(fabsf(ks), fabsf(km)) > kLargeKey) >> (lane & 32)) != 0;
+    const float down = large ? 0x1p-40f : 1.f;
+    o->ks[lane] = fine ? ks * down : __builtin_nanf("");
+    o->km[lane] = km * down;
+    if ((lane & 31) == 0) o->up[lane >> 5] = large ? 0x1p40f : 1.f;
     o->vs[lane] = fine ? s : 0.f;
     o->vm[lane] = fine ? m : 0.f;
   }
@@ -1408,7 +1421,9 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
       }
     }
   }
-  float x[NQ][8], w[NQ][8], l[NQ], z[NQ];
+  float x[NQ][8], w[NQ][8], l[NQ], z[NQ], f[NQ];
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) f[j] = q.f[j] * b.up[block];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int at = block * kBlockTok + 16 * u + 4 * g;
@@ -1451,7 +1466,7 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
       l[j] = z[j] = 0.f;
 #pragma unroll
       for (int n = 0; n < 8; ++n) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][n], q.f[j], -s->ref[j]));
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][n], f[j], -s->ref[j]));
         w[j][n] = p * vs[n >> 2][n & 3];
         l[j] += p;
         z[j] = __builtin_fmaf(p, vm[n >> 2][n & 3], z[j]);
@@ -1468,7 +1483,7 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
 #pragma unroll
       for (int n = 0; n < 8; ++n) {
         const float sc = vs[n >> 2][n & 3], m = fmaxf(fmaxf(sc, fabsf(__builtin_fmaf(-8.f, sc, vm[n >> 2][n & 3])) * 0.125f), 0x1p-90f);
-        best = fmaxf(best, x[j][n] * q.f[j] + (float)((int)(__float_as_uint(m) >> 23) - 127));
+        best = fmaxf(best, x[j][n] * f[j] + (float)((int)(__float_as_uint(m) >> 23) - 127));
       }
       best = fmaxf(best, __shfl_xor(best, 16));
       best = fmaxf(best, __shfl_xor(best, 32));

@@ -116,3 +116,20 @@ def test_more_tokens_than_max_new(dtype, max_new, new, ctx, heads, kvh, workspac
         right, alone = np.abs(got[rows] - ref) <= bound, got[rows] == 9
         assert right[:max_new].all()
         assert (right[max_new:].all(-1) | alone[max_new:].all(-1)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("q_std,k_std", [(1e-34, 1e34), (1e-34, 1e36), (3e-35, 3e36), (1e-30, 1e30), (1e28, 1e-28)])
+def test_large_keys_and_small_queries(form, dtype, q_std, k_std):
+    """Logits of the order of 1 to 100: sizes of one side that fp32's sums of codes could not take meet the other side first."""
+    s, heads, workspace, n = one(form, dtype, d=128)
+    check_attention(s, heads, q_std=q_std, k_std=k_std, workspace=workspace)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("form", FORMS)
+def test_large_keys_among_ordinary_ones(form, dtype):
+    s, heads, workspace, n = one(form, dtype, d=128)
+    keys = s.rng.normal(size=(n, 1, 128)) * np.where(s.rng.random((n, 1, 1)) < 0.1, 1e36, 1e3)
+    check_attention(s, heads, q_std=1e-34, keys=[keys], workspace=workspace)
