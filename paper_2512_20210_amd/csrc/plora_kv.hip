@@ -715,6 +715,8 @@ __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
 // product is a number again.  So refs are whole numbers, and the sum's exponent is moved.  Weights below 2^-126 are 0; the
 // largest is at least 2^(7 - e) with e = floor(log2(max(scale, |min| / 8))) of some value that is seen: 96 for values of 1e30, 124 at most.
 
+// The least factor of a logit: with 0 in its place a masked key's minus infinity would become NaN.
+constexpr float kLeastFactor = 0x1p-149f;
 constexpr float kNoRef = -3e38f;  // ref before the first key: the weight of any x is over its limit
 // A sum of weights as ref moves up by -by, a whole number (or less than all refs are apart).
 __device__ __forceinline__ float moved(float sum, float by) { return __builtin_ldexpf(sum, (int)fmaxf(by, -1000.f)); }
@@ -868,7 +870,7 @@ __device__ __forceinline__ void stage_queries_of(QueryRows<D, HQ, R>* o, const A
         // (2^-12: products of a row near 1 are up to 2^22, so with half of the power alone keys past 2^106 would be too large)
         const int e1 = e / 2 + 12;
         o->f1[row] = __uint_as_float((uint32_t)(127 - e1) << 23);
-        o->f2[row] = a.scale * __uint_as_float((uint32_t)(127 - e + e1) << 23);
+        o->f2[row] = fmaxf(a.scale * __uint_as_float((uint32_t)(127 - e + e1) << 23), kLeastFactor);
       }
     }
   }
@@ -903,7 +905,7 @@ __device__ __forceinline__ void take_queries(Queries<D, NQ, H>* o, int j, const 
     for (int i = 0; i < D / 32; ++i) o->q[j][h][i] = __builtin_bit_cast(f16x8, from.q[h][r][g * (D / 32) + i]);
   }
   o->sum[j] = from.sum[r];
-  o->f[j] = from.f1[r] * from.f2[r];
+  o->f[j] = fmaxf(from.f1[r] * from.f2[r], kLeastFactor);
 }
 
 // Running sums of a column, per lane.

@@ -133,3 +133,12 @@ def test_large_keys_among_ordinary_ones(form, dtype):
     s, heads, workspace, n = one(form, dtype, d=128)
     keys = s.rng.normal(size=(n, 1, 128)) * np.where(s.rng.random((n, 1, 1)) < 0.1, 1e36, 1e3)
     check_attention(s, heads, q_std=1e-34, keys=[keys], workspace=workspace)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("scale,q_std", [(1e-40, 1e-3), (1e-12, 1e-36), (1e-38, 60.0)])
+def test_scales_that_leave_equal_weights(form, dtype, scale, q_std):
+    """Keys that are not seen stay out of a mean over the others."""
+    s, heads, workspace, n = one(form, dtype)
+    check_attention(s, heads, q_std=q_std if dtype != "fp16" else max(q_std, 1e-3), scale=scale, workspace=workspace, window=n - 7)
