@@ -701,8 +701,9 @@ __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
 // where a key is masked.  q is multiplied by a power of two per row that brings it into fp16's range; fp32 rows, and their weights, go as a
 // high and a low half.  The power is undone where large keys do not meet it alone (keys of 1e34 and a q of 1e-34, times 2^122, have a logit of
 // the order of 1, but their products would pass fp32): with few rows half of it ahead of the key's scale and half in the softmax's
-// factor; with many rows, which have no instruction to spare, all of it in the factor, and 32 keys of which one is large are brought
-// down by 2^40.
+// factor; with many rows, which have no instruction to spare, all of it in the factor, and every key's scale and min are held times 2^-14,
+// which is as much as the factor of the largest rows has room for: keys of 1e37 fit whatever their signs are.  (A flag per 32 keys and
+// 2^-40 where one of them passes 2^90: 3 % of a long chunk's time.)
 //
 // Softmax in one pass: weights are p = 2^(x - ref), x = scale * log2(e) * q.K.  w = p * scale_s has to fit fp16 without loss, so ref
 // is chosen for the largest x + log2(max(scale_s, |min_s| / 8)): that product is brought to 2^8 and may grow to 2^15
@@ -715,6 +716,7 @@ __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
 // product is a number again.  So refs are whole numbers, and the sum's exponent is moved.  Weights below 2^-126 are 0; the
 // largest is at least 2^(7 - e) with e = floor(log2(max(scale, |min| / 8))) of some value that is seen: 96 for values of 1e30, 124 at most.
 
+constexpr float kKeyUnit = 0x1p-14f;  // k_attend_many: what keys' scale and min are held times
 // The least factor of a logit: with 0 in its place a masked key's minus infinity would become NaN.
 constexpr float kLeastFactor = 0x1p-149f;
 constexpr float kNoRef = -3e38f;  // ref before the first key: the weight of any x is over its limit
@@ -836,9 +838,9 @@ __device__ __forceinline__ void stage_queries_of(QueryRows<D, HQ, R>* o, const A
     for (int k = 0; k < 8 * G; ++k) big = fmaxf(big, fabsf(x[n][k]));
 #pragma unroll
     for (int d = 1; d < T; d <<= 1) big = fmaxf(big, __shfl_xor(big, d));
-    // 2^e with big * 2^e in [2^9, 2^10)
+    // 2^e with big * 2^e in [2^9, 2^10); for the largest rows in [2^14, 2^15), so that 2^-e / kKeyUnit times a scale of 1 is a number
     int e = big > 0.f ? 9 - (int)((__float_as_uint(big) >> 23) & 255) + 127 : 0;
-    e = e > 120 ? 120 : e;
+    e = e > 120 ? 120 : e < -113 ? -113 : e;
     const float up = __uint_as_float((uint32_t)(e + 127) << 23);
 #pragma unroll
     for (int k = 0; k < 8 * G; ++k) {
@@ -905,7 +907,7 @@ __device__ __forceinline__ void take_queries(Queries<D, NQ, H>* o, int j, const 
     for (int i = 0; i < D / 32; ++i) o->q[j][h][i] = __builtin_bit_cast(f16x8, from.q[h][r][g * (D / 32) + i]);
   }
   o->sum[j] = from.sum[r];
-  o->f[j] = fmaxf(from.f1[r] * from.f2[r], kLeastFactor);
+  o->f[j] = fmaxf(from.f1[r] * (1 / kKeyUnit) * from.f2[r], kLeastFactor);
 }
 
 // Running sums of a column, per lane.
@@ -1313,10 +1315,8 @@ struct Stage {
   static constexpr int K = KEYS, W = K / 16 * (D / 32) / kWaves;  // keys; words of keys, and of values, of a lane
   uint4 keys[K / 16 * (D / 32)][64];    // [tile of 16 keys][32 channels], then lanes
   uint4 values[K / 32 * (D / 16)][64];  // [32 keys][16 channels]
-  float ks[K], km[K], vs[K], vm[K];     // scale and min + 8 scale of keys and of values, of these 0 where there is no row
-  float up[K / 32];                     // what the 32 keys' ks and km are short of: 1, or 2^40 where one of them is large
+  float ks[K], km[K], vs[K], vm[K];     // scale and min + 8 scale of keys (times kKeyUnit) and of values, of these 0 where there is no row
 };
-constexpr float kLargeKey = 0x1p90f;
 // The pages of a stage's two blocks of 32 keys, read a stage before they are used: -1 behind `to`.
 struct PageIds {
   int32_t p0, p1;
@@ -1388,12 +1388,9 @@ __device__ __forceinline__ void unpack(Stage<D, K>* o, const Fetched<W>& f, cons
     // not has a weight of 0 that meets nothing but numbers.
     const float s = param_scale(f.vp), m = __builtin_fmaf(8.f, s, param_min(f.vp));
     const bool fine = fabsf(s) < INFINITY && fabsf(m) < INFINITY;
-    const float ks = param_scale(f.kp), km = __builtin_fmaf(8.f, ks, param_min(f.kp));
-    const bool large = (uint32_t)(__ballot(fmaxf(fabsf(ks), fabsf(km)) > kLargeKey) >> (lane & 32)) != 0;
-    const float down = large ? 0x1p-40f : 1.f;
-    o->ks[lane] = fine ? ks * down : __builtin_nanf("");
-    o->km[lane] = km * down;
-    if ((lane & 31) == 0) o->up[lane >> 5] = large ? 0x1p40f : 1.f;
+    const float ks = param_scale(f.kp) * kKeyUnit;
+    o->ks[lane] = fine ? ks : __builtin_nanf("");
+    o->km[lane] = __builtin_fmaf(8.f, ks, param_min(f.kp) * kKeyUnit);
     o->vs[lane] = fine ? s : 0.f;
     o->vm[lane] = fine ? m : 0.f;
   }
@@ -1423,9 +1420,7 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
       }
     }
   }
-  float x[NQ][8], w[NQ][8], l[NQ], z[NQ], f[NQ];
-#pragma unroll
-  for (int j = 0; j < NQ; ++j) f[j] = q.f[j] * b.up[block];
+  float x[NQ][8], w[NQ][8], l[NQ], z[NQ];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int at = block * kBlockTok + 16 * u + 4 * g;
@@ -1468,7 +1463,7 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
       l[j] = z[j] = 0.f;
 #pragma unroll
       for (int n = 0; n < 8; ++n) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][n], f[j], -s->ref[j]));
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][n], q.f[j], -s->ref[j]));
         w[j][n] = p * vs[n >> 2][n & 3];
         l[j] += p;
         z[j] = __builtin_fmaf(p, vm[n >> 2][n & 3], z[j]);
@@ -1485,7 +1480,7 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
 #pragma unroll
       for (int n = 0; n < 8; ++n) {
         const float sc = vs[n >> 2][n & 3], m = fmaxf(fmaxf(sc, fabsf(__builtin_fmaf(-8.f, sc, vm[n >> 2][n & 3])) * 0.125f), 0x1p-90f);
-        best = fmaxf(best, x[j][n] * f[j] + (float)((int)(__float_as_uint(m) >> 23) - 127));
+        best = fmaxf(best, x[j][n] * q.f[j] + (float)((int)(__float_as_uint(m) >> 23) - 127));
       }
       best = fmaxf(best, __shfl_xor(best, 16));
       best = fmaxf(best, __shfl_xor(best, 32));
