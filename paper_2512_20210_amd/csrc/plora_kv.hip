@@ -1456,10 +1456,9 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) vc[i] = __builtin_bit_cast(f16x8, b.values[block * (D / 16) + i][lane]);
   auto weights = [&]() {
-    bool more = false;
+    float top = 0.f, all_l = 0.f, all_z = 0.f;
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
-      float top = 0.f;
       l[j] = z[j] = 0.f;
 #pragma unroll
       for (int n = 0; n < 8; ++n) {
@@ -1469,9 +1468,10 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
         z[j] = __builtin_fmaf(p, vm[n >> 2][n & 3], z[j]);
         top = fmaxf(top, w[j][n]);
       }
-      more |= outgrown(top, s->l[j] + l[j], z[j]);
+      all_l += s->l[j] + l[j];
+      all_z += fabsf(z[j]);
     }
-    return more;
+    return outgrown(top, all_l, all_z);
   };
   if (__any(weights())) {
 #pragma unroll
