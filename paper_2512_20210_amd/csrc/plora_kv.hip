@@ -488,8 +488,10 @@ __device__ __forceinline__ uint32_t quantise(const float* x, uint32_t* word) {
   const float m = __uint_as_float(sm & 0xffff0000u);
   const bool fine = none == 0.f && fabsf(s) < INFINITY && fabsf(m) < INFINITY;
   if (s < 0x1p-100f) s = 0.f;
-  // (x - min) / scale rounded as by a division: the quotient by the reciprocal, and one correction by its remainder
-  const float inv = s > 0.f ? 1.0f / s : 0.f;
+  // (x - min) / scale rounded as by a division: the quotient by the reciprocal, and one correction by its remainder.  Half of both where the
+  // kept min is so far below lo that x - min would not be finite.
+  const float by = hi - m < INFINITY ? 1.f : 0.5f, sb = s * by, mb = m * by;
+  const float inv = s > 0.f ? 1.0f / sb : 0.f;
 #pragma unroll
   for (int i = 0; i < C / 8; ++i) {
     float half[2];
@@ -498,9 +500,9 @@ __device__ __forceinline__ uint32_t quantise(const float* x, uint32_t* word) {
       float sum = 0.f;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float d = x[8 * i + 4 * h + k] - m;
+        const float d = __builtin_fmaf(x[8 * i + 4 * h + k], by, -mb);  // by 1: x - m
         float q = d * inv;
-        q = __builtin_fmaf(__builtin_fmaf(-q, s, d), inv, q);
+        q = __builtin_fmaf(__builtin_fmaf(-q, sb, d), inv, q);
         q = __builtin_amdgcn_fmed3f(__builtin_rintf(q), 0.f, 15.f);
         sum = __builtin_fmaf(q, (float)(1 << (4 * k)), sum);  // whole numbers below 2^16: exact
       }
@@ -670,7 +672,7 @@ __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
       for (int i = 0; i < C / 8; ++i) {
         const uint32_t q = kw[i];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[8 * i + k] = m + s * (float)(q >> (4 * k) & 15u);  // the product is exact: 12 bits at most
+        for (int k = 0; k < 8; ++k) x[8 * i + k] = __builtin_fmaf(s, (float)(q >> (4 * k) & 15u), m);  // (15 s alone may pass fp32)
       }
     } else {
       const uint32_t* vw = reinterpret_cast<const uint32_t*>(hp + (int64_t)pt * (D / 2) + (slot / kBlockTok) * (16 * D));
@@ -679,7 +681,7 @@ __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
         uint32_t q[RUN];
         ld_run<RUN>(q, vw + at);
 #pragma unroll
-        for (int i = 0; i < RUN; ++i) x[c + 4 * i] = m + s * (float)(q[i] >> shift & 15u);
+        for (int i = 0; i < RUN; ++i) x[c + 4 * i] = __builtin_fmaf(s, (float)(q[i] >> shift & 15u), m);
       });
     }
   }

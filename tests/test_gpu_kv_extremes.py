@@ -142,3 +142,32 @@ def test_scales_that_leave_equal_weights(form, dtype, scale, q_std):
     """Keys that are not seen stay out of a mean over the others."""
     s, heads, workspace, n = one(form, dtype)
     check_attention(s, heads, q_std=q_std if dtype != "fp16" else max(q_std, 1e-3), scale=scale, workspace=workspace, window=n - 7)
+
+
+# ---- rows of the cache at the limit of fp32 -----------------------------------------------------------
+
+def test_rows_whose_spread_just_fits():
+    """hi - lo is finite, hi less the rounded lo is not."""
+    import torch
+    from oracle import kv as O
+    x = np.random.default_rng(1).uniform(-1.69e38, 1.69e38, size=(40, 1, 64)).astype(np.float32)
+    top, lo = np.float32(3.4028235e38), np.float32(-1.6955e38)
+    x[:, 0, 3] = lo * np.linspace(1, 1.003, 40, dtype=np.float32)
+    x[:, 0, 60] = top * np.float32(1 - 2.0 ** -13) + x[:, 0, 3]
+    x[1::2, 0, 60] *= np.float32(0.99)
+    with np.errstate(all="ignore"):
+        lo16 = O.to_bf16(x.min(-1))
+        assert np.isfinite(x.max(-1) - x.min(-1)).all() and (~np.isfinite(x.max(-1) - lo16)).sum() >= 5
+    s = Setup("fp32", 1, 64, 32, [40], [3])
+    t, x64 = put(x, "fp32")
+    s.cache.append(s.batch(), t, t.clone(), None, stream())
+    for j, place in enumerate(s.places(0)):
+        with np.errstate(all="ignore"):
+            c, sc, mn = O.chosen(x64[j].astype(np.float32), 32)
+        for values in (0, 1):
+            s.oracle.write(*s.slot(0, place), 0, values, c[0], sc[0], mn[0])
+    assert torch.equal(s.pages.cpu(), torch.from_numpy(s.oracle.p))
+    kb, vb = torch.zeros_like(t), torch.zeros_like(t)
+    s.cache.read(s.batch(), kb, vb, stream())
+    for got, ref in zip((kb, vb), s.rows(0)[:, 3:]):
+        assert torch.equal(got.cpu(), torch.from_numpy(ref.astype(np.float32)))
