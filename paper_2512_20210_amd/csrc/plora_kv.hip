@@ -1784,7 +1784,8 @@ int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace,
   const bool some_many = most_rows > kMostFew;
   // Sequences of few rows among ones of many are left to k_attend_many where they are rare and their keys not many: a launch
   // that finds nothing to do costs 2 to 5 us (prompts of 5k tokens 74 -> 76 us; 64 sequences of up to 64 rows and 900 keys 73 -> 86).
-  const bool some_few = !some_many || (a.b.n_seqs > 1 && (a.b.max_len > 1024 || a.b.n_tokens < 16 * (int64_t)a.b.n_seqs));
+  // With more than 16 query heads a kv head there is no sequence of few rows.
+  const bool some_few = !some_many || (a.rep <= kMostFew && a.b.n_seqs > 1 && (a.b.max_len > 1024 || a.b.n_tokens < 16 * (int64_t)a.b.n_seqs));
   // rows of a tile of k_attend_few: all that a sequence can have, or those of a single token next to sequences with many
   const int64_t tile_rows = some_many ? a.rep : most_rows;
   a.few_rows = tile_rows <= 4 ? 4 : tile_rows <= 8 ? 8 : 16;
