@@ -25,8 +25,8 @@ constexpr int kKeyAlign = 64;       // parts of a sequence's keys start at multi
 
 // ---- element types ------------------------------------------------------------------------------------
 
-template <int DT> struct Elt { static constexpr int B = 2, V = 8; };  // bytes, elements per 16 bytes
-template <> struct Elt<PLORA_F32> { static constexpr int B = 4, V = 4; };
+template <int DT> struct Elt { static constexpr int B = 2; };  // bytes
+template <> struct Elt<PLORA_F32> { static constexpr int B = 4; };
 
 template <int DT>
 __device__ __forceinline__ float ld1(const uint8_t* p, int64_t i) {
@@ -1822,8 +1822,10 @@ int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace,
   }
   if (rc == PLORA_OK && many) {
     // a rotated row of 16-bit elements needs more than the 11 bits of one half to be as good as its elements were; the 8 of bf16 do not
-    if (DT == PLORA_F32 || (DT == PLORA_F16 && a.r.table)) rc = launch(k_attend_many<DT, D, NQ, 2>, many, (unsigned)a.parts, 1, a, stream);
-    else rc = launch(k_attend_many<DT, D, NQ, DT == PLORA_F32 ? 2 : 1>, many, (unsigned)a.parts, 1, a, stream);
+    void (*kernel)(AttendArgs);
+    if constexpr (DT == PLORA_F16) kernel = a.r.table ? k_attend_many<DT, D, NQ, 2> : k_attend_many<DT, D, NQ, 1>;
+    else kernel = k_attend_many<DT, D, NQ, DT == PLORA_F32 ? 2 : 1>;
+    rc = launch(kernel, many, (unsigned)a.parts, 1, a, stream);
   }
   if (rc == PLORA_OK && a.parts > 1) {
     // threads of a row, times D/8: as many as there are parts, up to a workgroup's (64 parts 57 us, with one each 63)

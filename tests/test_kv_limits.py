@@ -12,3 +12,12 @@ def test_attention_over_more_than_two_to_the_30_keys():
         b = batch(stride=stride, max_len=max_len)
         assert P.plora_kv_attend(cache(page=64), b, 8, rows(), rows(), 0.1) == P.PLORA_ERR_LIMIT
         assert P.plora_kv_attend(cache(page=64), b, 8, rows(), rows(), 0.1, 0) == P.PLORA_ERR_LIMIT
+
+
+def test_the_library_holds_the_attention_kernels_that_calls_reach():
+    """k_attend_many<dtype, head_dim, tiles of a wavefront, halves of q>: fp16 with both numbers of halves (rotated, or not), bf16 with 1, fp32 with 2."""
+    import re
+    names = set(re.findall(rb"k_attend_manyILi(\d)ELi(\d+)ELi(\d)ELi(\d)E", open(P.LIB_PATH, "rb").read()))
+    built = {(int(dt), int(d), int(h)) for dt, d, _, h in names}
+    assert built == {(dt, d, h) for d in (64, 128, 256) for dt, h in ((P.PLORA_F16, 1), (P.PLORA_F16, 2), (P.PLORA_BF16, 1), (P.PLORA_F32, 2))}
+    assert len(names) == len(built)
