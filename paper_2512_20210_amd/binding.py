@@ -7,6 +7,7 @@ PloraError on a negative status and keeps the objects it must keep alive.
 """
 import ctypes as C
 import os
+import sys
 
 import numpy as np
 
@@ -728,17 +729,24 @@ def _dtype_of(t):
     return code
 
 
-def _rows_of(call, t, n_tokens, heads, head_dim, dtype):
+def _device():
+    """The GPU that this thread's kernels run on: these calls have no pool that would know theirs."""
+    global _device
+    _device = sys.modules["torch"].cuda.current_device  # (from now on; torch is there, for its tensors are)
+    return _device()
+
+
+def _rows_of(call, t, n_tokens, heads, head_dim, dtype, device):
     """plora_rows of a torch tensor [tokens, heads, head_dim] (any strides the library takes, the last one 1)."""
     st = t.stride()
-    if t.shape != (n_tokens, heads, head_dim) or st[2] != 1 or _dtype_of(t) != dtype or not t.is_cuda:
+    if t.shape != (n_tokens, heads, head_dim) or st[2] != 1 or _dtype_of(t) != dtype or t.get_device() != device:
         raise PloraError(call, PLORA_ERR_INVAL)
     return RowsStruct(t.data_ptr(), st[0], st[1])
 
 
-def _ints_of(call, t, least):
+def _ints_of(call, t, least, device):
     """Device pointer of a contiguous int32 torch tensor of at least that many entries."""
-    if _dtype_of(t) != _INT32 or not t.is_contiguous() or t.numel() < least or not t.is_cuda:
+    if _dtype_of(t) != _INT32 or not t.is_contiguous() or t.numel() < least or t.get_device() != device:
         raise PloraError(call, PLORA_ERR_INVAL)
     return t.data_ptr()
 
@@ -749,6 +757,9 @@ def _three(call, t):
     return t.shape
 
 
+# Rotary, KvBatch and PagedKvCache take torch tensors, all of the GPU that is torch's current one at the call (others are refused: the
+# kernels would run elsewhere).  stream: a hipStream_t as a number; None is the null stream, not torch's current one, so a program
+# that works on a stream of its own passes torch.cuda.current_stream().cuda_stream.
 class Rotary:
     """A table of angles (torch float32 tensor [positions, rot_dim/2, 2] on the GPU) and how a head is rotated by it."""
 
@@ -757,22 +768,29 @@ class Rotary:
                 table.shape[2] != 2 or not table.is_cuda:
             raise PloraError("Rotary", PLORA_ERR_INVAL)
         self.table = table  # kept alive
+        self.device = table.get_device()
         self.c = RotaryStruct(table.data_ptr(), table.shape[0], rot_dim, int(interleaved))
 
     @classmethod
     def make(cls, table, config=None, interleaved=False, stream=None):
         """Fills `table` by `config` (a RotaryConfig) first."""
         out = cls(table, table.shape[1] * 2, interleaved)
+        if out.device != _device():
+            raise PloraError("plora_rotary_table", PLORA_ERR_INVAL)
         _check("plora_rotary_table", plora_rotary_table(config or RotaryConfig(), out.c.rot_dim, out.c.max_pos, table.data_ptr(), stream))
         return out
 
     def rotate(self, positions, x, out, inverse=False, stream=None):
         """out = x [tokens, heads, head_dim] rotated by positions (int32 [tokens]); out may be x."""
-        n, heads, d = _three("plora_rotate", x)
+        call = "plora_rotate"
+        device = _device()
+        if self.device != device:
+            raise PloraError(call, PLORA_ERR_INVAL)
+        n, heads, d = _three(call, x)
         dtype = _dtype_of(x)
-        rows = _rows_of("plora_rotate", x, n, heads, d, dtype)
-        rc = lib.plora_rotate(self.c, dtype, n, heads, d, _ints_of("plora_rotate", positions, n), rows, rows if out is x else _rows_of("plora_rotate", out, n, heads, d, dtype),
-                              inverse, stream)
+        rows = _rows_of(call, x, n, heads, d, dtype, device)
+        rc = lib.plora_rotate(self.c, dtype, n, heads, d, _ints_of(call, positions, n, device), rows,
+                              rows if out is x else _rows_of(call, out, n, heads, d, dtype, device), inverse, stream)
         if rc:
             _check("plora_rotate", rc)
         return out
@@ -789,8 +807,11 @@ class KvBatch:
             raise PloraError(call, PLORA_ERR_INVAL)
         self.kept = (tok_start, kv_len, page_table, positions)
         self.n_tokens = n_tokens
-        self.c = KvBatchStruct(n, n_tokens, max_new, max_len, page_table.shape[1], _ints_of(call, tok_start, n + 1), _ints_of(call, kv_len, n),
-                               _ints_of(call, page_table, n), None if positions is None else _ints_of(call, positions, n_tokens))
+        self.device = dev = kv_len.get_device()
+        if dev < 0:  # not on a GPU
+            raise PloraError(call, PLORA_ERR_INVAL)
+        self.c = KvBatchStruct(n, n_tokens, max_new, max_len, page_table.shape[1], _ints_of(call, tok_start, n + 1, dev), _ints_of(call, kv_len, n, dev),
+                               _ints_of(call, page_table, n, dev), None if positions is None else _ints_of(call, positions, n_tokens, dev))
 
 
 class PagedKvCache:
@@ -798,6 +819,7 @@ class PagedKvCache:
 
     def __init__(self, dtype, n_kv_heads, head_dim, page_tokens, pages):
         self.pages = pages  # kept alive
+        self.device = pages.get_device()
         self.dtype, self.heads, self.head_dim = dtype, n_kv_heads, head_dim
         self.c = KvCacheStruct(dtype, n_kv_heads, head_dim, page_tokens, pages.shape[0], pages.data_ptr())
         page = plora_kv_page_bytes(self.c)
@@ -808,34 +830,46 @@ class PagedKvCache:
     def page_bytes(n_kv_heads, head_dim, page_tokens):
         return plora_kv_page_bytes(KvCacheStruct(PLORA_F16, n_kv_heads, head_dim, page_tokens, 1, None))
 
-    def _rows(self, call, batch, t):
-        return _rows_of(call, t, batch.n_tokens, self.heads, self.head_dim, self.dtype)
+    def _rows(self, call, batch, t, device):
+        return _rows_of(call, t, batch.n_tokens, self.heads, self.head_dim, self.dtype, device)
 
     def append(self, batch, k, v, rotary=None, stream=None):
         """k, v: [tokens, kv heads, head_dim]; rotary: applied to k."""
-        rc = lib.plora_kv_append(self.c, batch.c, self._rows("plora_kv_append", batch, k), self._rows("plora_kv_append", batch, v),
+        call = "plora_kv_append"
+        device = _device()
+        if self.device != device or batch.device != device or (rotary is not None and rotary.device != device):
+            raise PloraError(call, PLORA_ERR_INVAL)
+        rc = lib.plora_kv_append(self.c, batch.c, self._rows(call, batch, k, device), self._rows(call, batch, v, device),
                                  None if rotary is None else rotary.c, stream)
         if rc:
-            _check("plora_kv_append", rc)
+            _check(call, rc)
 
     def read(self, batch, k, v, stream=None):
-        rc = lib.plora_kv_read(self.c, batch.c, self._rows("plora_kv_read", batch, k), self._rows("plora_kv_read", batch, v), stream)
+        call = "plora_kv_read"
+        device = _device()
+        if self.device != device or batch.device != device:
+            raise PloraError(call, PLORA_ERR_INVAL)
+        rc = lib.plora_kv_read(self.c, batch.c, self._rows(call, batch, k, device), self._rows(call, batch, v, device), stream)
         if rc:
-            _check("plora_kv_read", rc)
+            _check(call, rc)
 
     def attend(self, batch, q, out, scale, workspace=None, causal=True, window=0, rotary=None, stream=None):
         """q, out: [tokens, heads, head_dim]; workspace: any contiguous tensor on the GPU, or None; rotary: applied to q."""
         call = "plora_kv_attend"
+        device = _device()
+        if self.device != device or batch.device != device or (rotary is not None and rotary.device != device):
+            raise PloraError(call, PLORA_ERR_INVAL)
         n, heads, d = _three(call, q)
         if d != self.head_dim or n != batch.n_tokens:
             raise PloraError(call, PLORA_ERR_INVAL)
         ws, size = None, 0
         if workspace is not None:
-            if not workspace.is_contiguous() or not workspace.is_cuda:
+            if not workspace.is_contiguous() or workspace.get_device() != device:
                 raise PloraError(call, PLORA_ERR_INVAL)
             size = workspace.nbytes
             ws = workspace.data_ptr() if size else None
-        rc = lib.plora_kv_attend(self.c, batch.c, heads, _rows_of(call, q, n, heads, d, self.dtype), _rows_of(call, out, n, heads, d, self.dtype), scale,
+        rc = lib.plora_kv_attend(self.c, batch.c, heads, _rows_of(call, q, n, heads, d, self.dtype, device),
+                                 _rows_of(call, out, n, heads, d, self.dtype, device), scale,
                                  causal, window, None if rotary is None else rotary.c, ws, size, stream)
         if rc:
             _check(call, rc)
