@@ -774,6 +774,8 @@ class Rotary:
     @classmethod
     def make(cls, table, config=None, interleaved=False, stream=None):
         """Fills `table` by `config` (a RotaryConfig) first."""
+        if table.dim() != 3:
+            raise PloraError("Rotary", PLORA_ERR_INVAL)
         out = cls(table, table.shape[1] * 2, interleaved)
         if out.device != _device():
             raise PloraError("plora_rotary_table", PLORA_ERR_INVAL)
@@ -818,12 +820,14 @@ class PagedKvCache:
     """One layer's keys and values in 4 bits, on pages of a caller's tensor (uint8 [pages, page bytes] on the GPU)."""
 
     def __init__(self, dtype, n_kv_heads, head_dim, page_tokens, pages):
+        if pages.dim() != 2:
+            raise PloraError("PagedKvCache", PLORA_ERR_INVAL)
         self.pages = pages  # kept alive
         self.device = pages.get_device()
         self.dtype, self.heads, self.head_dim = dtype, n_kv_heads, head_dim
         self.c = KvCacheStruct(dtype, n_kv_heads, head_dim, page_tokens, pages.shape[0], pages.data_ptr())
         page = plora_kv_page_bytes(self.c)
-        if not page or pages.dim() != 2 or pages.shape[1] != page or not pages.is_contiguous() or str(pages.dtype) != "torch.uint8" or not pages.is_cuda:
+        if not page or pages.shape[1] != page or not pages.is_contiguous() or str(pages.dtype) != "torch.uint8" or not pages.is_cuda:
             raise PloraError("PagedKvCache", PLORA_ERR_INVAL)
 
     @staticmethod

@@ -78,3 +78,10 @@ def test_tensors_of_another_gpu_are_refused(monkeypatch):
         P.KvBatch(*[OnGpu(-1, torch.int32, *t.shape) for t in mixed], 0, 1, 100)
     with pytest.raises(P.PloraError, match="INVAL"):
         P.Rotary.make(OnGpu(1, torch.float32, 16, 32, 2))
+
+
+def test_tensors_with_other_dimensions_are_refused():
+    for make in (lambda: P.Rotary.make(OnGpu(0, torch.float32, 64)), lambda: P.Rotary(OnGpu(0, torch.float32, 64), 64),
+                 lambda: P.PagedKvCache(P.PLORA_BF16, 1, 64, 32, OnGpu(0, torch.uint8)), lambda: P.PagedKvCache(P.PLORA_BF16, 1, 64, 32, OnGpu(0, torch.uint8, 32 * 72))):
+        with pytest.raises(P.PloraError, match="INVAL"):
+            make()
