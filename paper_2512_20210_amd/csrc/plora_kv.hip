@@ -715,15 +715,14 @@ __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
 //
 // Two refs may be further apart than fp32 reaches although the weights behind them are alike (values of 0, held against 2^-90, and of
 // 1e25: 2^171).  Then 2^(old - new) is 0, which is right for the sums over values, whose size is in it, but not for the sum of the weights: that
-// product is a number again.  So refs are whole numbers, and the sum's exponent is moved.  Weights below 2^-126 are 0; the
-// largest is at least 2^(7 - e) with e = floor(log2(max(scale, |min| / 8))) of some value that is seen: 96 for values of 1e30, 124 at most.
+// product is a number again, so it is multiplied by the root of 2^(old - new) twice.  (Refs rounded up to whole numbers, and exponents
+// moved, give up that the weight that sets a ref is a power of two and its w exact: the error of a long chunk goes from 2.78e-4 to
+// 3.03e-4.)  Weights below 2^-126 are 0; the largest is at least 2^(8 - e) with e = floor(log2(max(scale, |min| / 8))) of some value that is seen: 96 for values of 1e30, 124 at most.
 
 constexpr float kKeyUnit = 0x1p-14f;  // k_attend_many: what keys' scale and min are held times
 // The least factor of a logit: with 0 in its place a masked key's minus infinity would become NaN.
 constexpr float kLeastFactor = 0x1p-149f;
 constexpr float kNoRef = -3e38f;  // ref before the first key: the weight of any x is over its limit
-// A sum of weights as ref moves up by -by, a whole number (or less than all refs are apart).
-__device__ __forceinline__ float moved(float sum, float by) { return __builtin_ldexpf(sum, (int)fmaxf(by, -1000.f)); }
 // Whether a step's weights ask for another ref.  top: their largest w; l: the lane's sum of weights with them; z: their sum with min.  A lane's l
 // may grow to 2^109: the 2^8 lanes and wavefronts that share a row, and 2^10 parts, do not bring it past fp32.  (Weights next to values of 0 are
 // 2^98 after a move, so a lane with thousands of these asks every time, in vain.  A w or l that is NaN asks for none; a z that is asks
@@ -1145,9 +1144,9 @@ __device__ __forceinline__ void weights64(const uint4* vparams, const Column& q,
     }
     best = fmaxf(best, __shfl_xor(best, 16));
     best = fmaxf(best, __shfl_xor(best, 32));
-    const float ref = fmaxf(s->ref[0], ceilf(best - 8.f)), by = s->ref[0] - ref, down = __builtin_amdgcn_exp2f(by);
+    const float ref = fmaxf(s->ref[0], best - 8.f), root = __builtin_amdgcn_exp2f(0.5f * (s->ref[0] - ref)), down = root * root;
     s->ref[0] = ref;
-    s->l[0] = moved(s->l[0], by);
+    s->l[0] = s->l[0] * root * root;
     s->z[0] *= down;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) s->o[0][i] *= down;
@@ -1212,14 +1211,14 @@ __device__ __forceinline__ void join_columns(Sums<D, 1>* s) {
   if constexpr (R == 16) return;
   float ref = fmaxf(s->ref[0], round16<8>(s->ref[0]));
   if constexpr (R == 4) ref = fmaxf(ref, round16<4>(ref));
-  const float by = s->ref[0] - ref, f = __builtin_amdgcn_exp2f(by);
+  const float root = __builtin_amdgcn_exp2f(0.5f * (s->ref[0] - ref)), f = root * root;
   s->ref[0] = ref;
   auto join = [&](float v) {
     v += round16<8>(v);
     if constexpr (R == 4) v += round16<4>(v);
     return v;
   };
-  s->l[0] = join(moved(s->l[0], by));
+  s->l[0] = join(s->l[0] * root * root);
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
 #pragma unroll
@@ -1295,8 +1294,8 @@ __global__ __launch_bounds__(64 * WAVES, (few_waves<DT, D, R>())) void k_attend_
     float l = 0.f, o[8] = {};
 #pragma unroll 2
     for (int k = 0; k < WAVES; ++k) {
-      const float by = sm[k][row] - ref, f = __builtin_amdgcn_exp2f(by);
-      l += moved(sl[k][row], by);
+      const float root = __builtin_amdgcn_exp2f(0.5f * (sm[k][row] - ref)), f = root * root;
+      l = __builtin_fmaf(sl[k][row] * root, root, l);
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = __builtin_fmaf(f, so[k][row][c + e], o[e]);
     }
@@ -1486,9 +1485,9 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
       }
       best = fmaxf(best, __shfl_xor(best, 16));
       best = fmaxf(best, __shfl_xor(best, 32));
-      const float ref = fmaxf(s->ref[j], ceilf(best - 8.f)), by = s->ref[j] - ref, down = __builtin_amdgcn_exp2f(by);
+      const float ref = fmaxf(s->ref[j], best - 8.f), root = __builtin_amdgcn_exp2f(0.5f * (s->ref[j] - ref)), down = root * root;
       s->ref[j] = ref;
-      s->l[j] = moved(s->l[j], by);
+      s->l[j] = s->l[j] * root * root;
       s->z[j] *= down;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) s->o[j][i] *= down;
@@ -1645,11 +1644,11 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
 #pragma unroll 4
     for (int k = g; k < n; k += G) {
       const float2 m = ml[k * all + row];
-      const float by = m.x - ref, f = __builtin_amdgcn_exp2f(by);
+      const float root = __builtin_amdgcn_exp2f(0.5f * (m.x - ref)), f = root * root;
       const float4* p = reinterpret_cast<const float4*>(a.part_o + (k * all + row) * D + c);
       const float4 u = p[0], v = p[1];
       const float e[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-      l += moved(m.y, by);
+      l = __builtin_fmaf(m.y * root, root, l);
 #pragma unroll
       for (int i = 0; i < 8; ++i) o[i] = __builtin_fmaf(f, e[i], o[i]);
     }
@@ -1670,8 +1669,8 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
     for (int i = 0; i < 8; ++i) o[i] = 0.f;
 #pragma unroll
     for (int k = 0; k < G; ++k) {
-      const float by = sm[k][mine] - ref, f = __builtin_amdgcn_exp2f(by);
-      l += moved(sl[k][mine], by);
+      const float root = __builtin_amdgcn_exp2f(0.5f * (sm[k][mine] - ref)), f = root * root;
+      l = __builtin_fmaf(sl[k][mine] * root, root, l);
 #pragma unroll
       for (int i = 0; i < 8; ++i) o[i] = __builtin_fmaf(f, so[k][mine][c + i], o[i]);
     }
