@@ -466,8 +466,8 @@ uint64_t plora_kv_page_bytes(const plora_kv_cache* cache);
  * Out of range: tok_start is held to [0, n_tokens] and kv_len to [0, min(max_len, table_stride * page_tokens)]; a page outside
  * [0, n_pages) is a hole: nothing is appended there, it reads as NaN, and attention passes over its tokens; tokens at
  * negative places are not appended, read as NaN and see no key (unless attention is not causal).  More than max_new tokens
- * of a sequence: those beyond may be left out, the first max_new are not.  Rows of no sequence are left alone.  Sequences may share pages that are
- * only read; two that append to one page race. */
+ * of a sequence: those beyond may be left out, the first max_new are not.  Rows of no sequence are left alone.  Sequences
+ * may share pages that are only read; two that append to one page race. */
 typedef struct {
   int32_t n_seqs, n_tokens;
   int32_t max_new;           /* most tokens of one sequence in this call, >= 1 */
@@ -492,11 +492,13 @@ int plora_kv_read(const plora_kv_cache* cache, const plora_kv_batch* batch, cons
  *   out[t, h] = sum_s p_s V[s] ,  p = softmax over the keys s that t sees of  scale * (q[t, h] . K[s]) ,
  * K, V of kv head h / (n_heads / n_kv_heads), as the values the codes stand for.  Sums are held in 32 bits; codes and q enter exactly
  * (a q that is rotated on the way, and fp32's, with 22 bits; bf16's rotated one with 11), the weights p with 11 bits for the
- * 16-bit types and 22 for fp32.  causal != 0: a token at place s sees the
- * places up to s, with window > 0 the last `window` of them only; causal = 0 (window 0): every place of its sequence, as
- * for queries that look at an encoder's states.  A token that sees no key gets 0.  NaN in rows that a token does not see
- * do not reach it.  q and values may be of any size, and keys up to 1e37, with products q . K that 32 bits hold (scale up to 1); beside values
- * above 1e30 small weights are dropped (below 2^-38 of the largest one for 1e30, below 2^-10 for 3e38).  rotary (or NULL): applied to q on the way.  n_heads: a multiple of n_kv_heads; scale > 0 and finite.
+ * 16-bit types and 22 for fp32.  16-bit types, up to 16 rows (token, query head) of a kv head: the sums q . codes run with an
+ * offset of 64 to the codes, which takes 6 of their 24 bits.  causal != 0: a token at place s sees the places up to s, with
+ * window > 0 the last `window` of them only; causal = 0 (window 0): every place of its sequence, as for queries that look
+ * at an encoder's states.  A token that sees no key gets 0.  NaN in rows that a token does not see do not reach it.
+ * q and values may be of any size, and keys up to 1e37, with products q . K that 32 bits hold (scale up to 1); beside values
+ * above 1e30 small weights are dropped (below 2^-38 of the largest one for 1e30, below 2^-10 for 3e38).
+ * rotary (or NULL): applied to q on the way.  n_heads: a multiple of n_kv_heads; scale > 0 and finite.
  * A sequence may have 2^30 keys: LIMIT if min(max_len, table_stride * page_tokens) is more.
  * workspace: device, 16-byte aligned, of any size (0 and NULL too): room for partial results.  With few tokens and many
  * keys the keys are split among workgroups as far as it reaches: n_tokens * n_heads * (head_dim + 2) * 4 bytes per part.

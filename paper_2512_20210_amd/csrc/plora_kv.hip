@@ -213,7 +213,7 @@ struct RotateArgs {
 // One thread, one unit.  VECTOR: a unit is 8 pairs of the half-split layout (two groups of 8 channels), 8 channels of the
 // interleaved one, or 8 channels to copy; otherwise one pair or one channel.
 // Both members of a pair are read before either is written, so y may be x.
-// Bound by its bytes: 19.4 us for 95.6 MB of fp16 rows (4.9 TB/s; a large copy reaches 5.1), 10 us for 38.6 MB of fp32 rows; one row 2.2.
+// Bound by its bytes: 19.5 us for 95.6 MB of fp16 rows (4.9 TB/s; a large copy reaches 5.2), 10 us for 38.6 MB of fp32 rows; one row 2.0.
 template <int DT, bool VECTOR>
 __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
   const uint32_t i = blockIdx.x * (uint32_t)kThreads + threadIdx.x;  // (a launch has fewer than 2^32 threads)
@@ -513,7 +513,7 @@ __device__ __forceinline__ uint32_t quantise(const float* x, uint32_t* word) {
   return fine ? (__float_as_uint(s) >> 16) | (sm & 0xffff0000u) : 0x7fc07fc0u;
 }
 
-// Bound by the latency of its chain (first rows and lengths, page, row and angles, the values' words that it changes one nibble of): 4.1 us for 256
+// Bound by the latency of its chain (first rows and lengths, page, row and angles, the values' words that it changes one nibble of): 4.3 us for 256
 // sequences with 8 heads of 128, bf16, of which an empty launch takes 2.
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void k_append_single(CacheArgs a) {
@@ -576,8 +576,8 @@ __device__ __forceinline__ void transpose_nibbles(uint32_t* w) {
 
 // Values: codes of 32 rows through LDS, then one thread takes 8 channels of the 8 tokens of a quad and transposes them into 8
 // words.  Words of which only some tokens are the call's are read first.
-// 36.8 us for 5k tokens of 32 heads of 128, bf16 (107 MB, 2.9 TB/s): vector instructions are two thirds of the time (min and max, the exact
-// quotient, packing).
+// 37.5 us for 5k tokens of 32 heads of 128, bf16 (107 MB, 2.9 TB/s): vector instructions are two thirds of the time (min and max, the exact
+// quotient, packing), and the 14080 workgroups, of which some 2000 fit at once, are seven rounds of the chain that bounds single rows.
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void k_append(CacheArgs a) {
   constexpr int C = D / 8;
@@ -707,9 +707,12 @@ __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
 // which is as much as the factor of the largest rows has room for: keys of 1e37 fit whatever their signs are.  (A flag per 32 keys and
 // 2^-40 where one of them passes 2^90: 3 % of a long chunk's time.)
 //
-// Softmax in one pass: weights are p = 2^(x - ref), x = scale * log2(e) * q.K.  w = p * scale_s has to fit fp16 without loss, so ref
+// Softmax in one pass: weights are p = 2^(x - ref), x = scale * log2(e) * q.K.  w = p * scale_s has to fit fp16's range, so ref
 // is chosen for the largest x + log2(max(scale_s, |min_s| / 8)): that product is brought to 2^8 and may grow to 2^15
-// before ref is moved (and the sums are multiplied), which after a row's first keys hardly ever happens.  A value of scale 0 has no w, and
+// before ref is moved (and the sums are multiplied), which after a row's first keys hardly ever happens.  For the 16-bit types w is rounded
+// to its 11 bits (p, its sum and p * min stay in fp32): an fp16 result's error is 2.78e-4 in place of the 2.07e-4 of its own rounding, a bf16
+// result's 1.680e-3 in place of 1.674e-3.  Low halves of w in a second product, as fp32 has them, would take 120 us in place of 114 (256
+// sequences, few rows), and 2.03 ms in place of 1.65 and 1.71 in place of 1.36 (2k rows over 32k keys, fp16 and bf16).  A value of scale 0 has no w, and
 // one with a small scale a small w, but their min weighs p * min all the same: ref is also moved before a step's sum of these passes
 // 2^100 (or is inf - inf), so that the sums stay far from fp32's limit whatever the values are.
 //
@@ -717,7 +720,8 @@ __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
 // 1e25: 2^171).  Then 2^(old - new) is 0, which is right for the sums over values, whose size is in it, but not for the sum of the weights: that
 // product is a number again, so it is multiplied by the root of 2^(old - new) twice.  (Refs rounded up to whole numbers, and exponents
 // moved, give up that the weight that sets a ref is a power of two and its w exact: the error of a long chunk goes from 2.78e-4 to
-// 3.03e-4.)  Weights below 2^-126 are 0; the largest is at least 2^(8 - e) with e = floor(log2(max(scale, |min| / 8))) of some value that is seen: 96 for values of 1e30, 124 at most.
+// 3.03e-4.)  Weights below 2^-126 are 0; the largest is at least 2^(8 - e) with e = floor(log2(max(scale, |min| / 8))) of some value that is
+// seen: 96 for values of 1e30, 124 at most.
 
 constexpr float kKeyUnit = 0x1p-14f;  // k_attend_many: what keys' scale and min are held times
 // The least factor of a logit: with 0 in its place a masked key's minus infinity would become NaN.
@@ -790,8 +794,9 @@ __device__ __forceinline__ f16x8 codes8(uint32_t w, const CodeBits& c) {
   r.p[3] = code_pair(h, 0x00f000f0u, c.high, high);
   return r.v;
 }
-// The same as 64 + code, in 7 instructions instead of 9: good for keys in the 16-bit types, where -64 sum(q) in the accumulator
-// takes the offset off again at the price of 6 of its 24 bits.  (With values it would cost bits of the weights.)
+// The same as 64 + code, in 7 instructions instead of 9 (few rows, 16-bit types, keys: 256 sequences 114 us in place of 121, with 3 tokens
+// each 91 in place of 98): -64 sum(q) in the accumulator takes the offset off again at the price of 6 of its 24 bits.  (With values it
+// would cost bits of the weights.)
 __device__ __forceinline__ f16x8 codes8_over64(uint32_t w, const CodeBits& c) {
   union { f16x2 p[4]; f16x8 v; } r;
   const uint32_t s[4] = {w << 4, w, w >> 4, w >> 8};
@@ -974,8 +979,8 @@ __device__ __forceinline__ int parts_of(const AttendArgs& a, int lo, int hi) {
 // each of these takes other keys: of 64 keys in 4 tiles of 16, column c has row c % R and the tiles c / R, c / R + 16 / R, ...  Every column is a
 // softmax of its own over its keys (nothing is exchanged between lanes), a lane has 4, 8 or 16 weights to compute instead
 // of 16, and the columns are joined where the wavefronts are.  The weights of keys that are other columns' are zero.
-// 4 rows in tiles of 4, 8, 16: 116, 126, 158 us (256 sequences of 64 - 4095 keys, 8 heads of 128, bf16: 584 MB, 5.0 - 5.2 TB/s, the probe of a bare
-// read reaches 7.0); by k_attend_many 498.  What bounds it is the read: with 4000 keys in all 512 sequences it is at 6.3 TB/s, the
+// 4 rows in tiles of 4, 8, 16: 114, 126, 159 us (256 sequences of 64 - 4095 keys, 8 heads of 128, bf16: 584 MB, 5.1 TB/s, the probe of a bare
+// read reaches 7.0); by k_attend_many 504.  What bounds it is the read: with 4000 keys in all 512 sequences it is at 6.3 TB/s, the
 // rest is the end of the launch, where the longest run alone.
 //
 // The wavefronts of a workgroup (4, or 16 where there are few workgroups) take 64 keys of the part in turn.  A wavefront asks for the next keys as soon as the
@@ -1004,7 +1009,7 @@ __device__ __forceinline__ Place64 place64(const AttendArgs& a, int seq, int key
   return p;
 }
 // Codes are read once a call (a prefix that sequences share: once a sequence): streaming loads leave the caches to what is read
-// again.  256 sequences 124 -> 113 us, 5.8 and for longer ones 6.3 TB/s.
+// again.  256 sequences 124 -> 115 us (5.1 TB/s), longer ones of one length 6.3 TB/s.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint4 ldnt(const uint8_t* p) {
   const u32x4 q = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
@@ -1308,8 +1313,8 @@ __global__ __launch_bounds__(64 * WAVES, (few_waves<DT, D, R>())) void k_attend_
 // vector instructions of the softmax (11 issue slots a logit, 4 of them the exponential), so the codes' unpacking is shared: of
 // Stage::K keys each wavefront turns a quarter of the codes into the operands that all four then read from LDS (in operand
 // order: a lane's 16 bytes beside the next lane's), a stage ahead of their use, with one barrier a stage.  2048 tokens with 32 heads over
-// 32k keys: bf16 1.34 - 1.40 ms (740 - 780 TFLOP/s of the 1256 that a large product reaches), fp16 with rotation 1.64 (three products
-// instead of two); matrix units busy 38 % of the time (fp16), vector units 51 %.  Prompts of 5k tokens: 76 us, of which a third is the
+// 32k keys: bf16 1.36 - 1.38 ms (750 - 765 TFLOP/s of the 1210 that a large product reaches), fp16 with rotation 1.65 - 1.68 (three products
+// instead of two); matrix units busy 37 % of the time (fp16), vector units 51 %.  Prompts of 5k tokens: 78 us, of which a third is the
 // launch, the search for the rows and the output, a third the rotation of q, a third the keys.
 template <int D, int KEYS>
 struct Stage {
@@ -1527,9 +1532,9 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
 template <int DT, int D, int NQ, int HQ>
 __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
   constexpr int HW = DT == PLORA_F32 ? 2 : 1, R = 16 * NQ;
-  // Two workgroups share a CU, also where 29 registers go to scratch for it (fp32, heads of 256: 2048 tokens with 8 heads 103 us; with one
-  // workgroup and none in scratch 144).  Low halves of 32 rows of 128 channels do not fit the registers beside the rest: they stay in LDS,
-  // which then holds stages of 32 keys instead of 64 (fp16 1.64 ms either way; with the halves in registers 2.77; bf16 with 32 keys
+  // Two workgroups share a CU, also where 34 registers go to scratch for it (fp32, heads of 256: 2048 tokens with 8 heads 96 us; with one
+  // workgroup and none in scratch 133).  Low halves of 32 rows of 128 channels do not fit the registers beside the rest: they stay in LDS,
+  // which then holds stages of 32 keys instead of 64 (fp16 1.65 ms either way; with the halves in registers 2.77; bf16 with 32 keys
   // 1.44 instead of 1.40).
   constexpr bool LOW_IN_LDS = HQ == 2 && NQ == 2 && D == 128;
   constexpr int K = D == 256 || LOW_IN_LDS ? 32 : 64, W = Stage<D, K>::W;
@@ -1614,7 +1619,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a) {
   }
 }
 
-// Joins the parts of a row: 4 to 7 us, a launch and its loads.  D/8 threads have 8 channels each, G times over: group g of them takes the parts g, g + G, ..., and the
+// Joins the parts of a row: 4 to 5 us, a launch and its loads.  D/8 threads have 8 channels each, G times over: group g of them takes the parts g, g + G, ..., and the
 // groups' sums are joined in their order.  R: rows of a tile of k_attend_many.
 template <int DT, int D, int R, int G>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
@@ -1783,7 +1788,7 @@ int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace,
   const bool some_many = most_rows > kMostFew;
   // Sequences of few rows among ones of many are left to k_attend_many where they are rare and their keys not many: a launch
   // that finds nothing to do costs 2 to 5 us (prompts of 5k tokens 74 -> 76 us; 64 sequences of up to 64 rows and 900 keys 73 -> 86).
-  // With more than 16 query heads a kv head there is no sequence of few rows.
+  // With more than 16 query heads a kv head there is no sequence of few rows (256 sequences with 32 heads on one kv head: 114 us, with that launch 117).
   const bool some_few = !some_many || (a.rep <= kMostFew && a.b.n_seqs > 1 && (a.b.max_len > 1024 || a.b.n_tokens < 16 * (int64_t)a.b.n_seqs));
   // rows of a tile of k_attend_few: all that a sequence can have, or those of a single token next to sequences with many
   const int64_t tile_rows = some_many ? a.rep : most_rows;
@@ -1800,7 +1805,8 @@ int attend(AttendArgs a, int max_new, uint64_t workspace_bytes, void* workspace,
   const uint64_t fill = some_many ? kFillMany : kFillFew, given = some_many ? likely * a.c.heads : few;
   // As many parts as the GPU holds at once, where their lengths are alike (one sequence) or there are many of a sequence: some more of them
   // would run alone at the end (12 sequences of 30000 keys 85 us, these 76; 300 rows over 30000 keys 348, these 256).  Otherwise one more, for
-  // lengths differ (70 sequences of 1000 - 12000 keys: 106 us against 132).
+  // lengths differ (70 sequences of 1000 - 12000 keys: 106 us against 132).  None where the workgroups fill the GPU by themselves (256 sequences
+  // of 64 - 4095 keys 115 us, in 2 parts 118, in 4 127; 512 of 4000: 357, 391, 436).
   uint64_t want = wide ? 1 : given * (a.b.n_seqs == 1 ? 2 : 8) <= fill ? fill / given : (fill + given - 1) / given;
   // Keys that are worth a part of their own: 256, or 512 where few rows have many workgroups anyway (8 sequences of 8000 keys, 64 workgroups: 23
   // us, with 512 26; 8 tokens over 1000 keys 26, with 512 43; 24 sequences with 12 heads and a window of 1000 keys 19, with 512 16).
