@@ -1474,7 +1474,7 @@ __device__ __forceinline__ void step32(const Stage<D, K>& b, int block, const Qu
         z[j] = __builtin_fmaf(p, vm[n >> 2][n & 3], z[j]);
         top = fmaxf(top, w[j][n]);
       }
-      all_l += s->l[j] + l[j];
+      all_l = fmaxf(all_l, s->l[j] + l[j]);  // (no sum: one that is NaN must not hide the others)
       all_z += fabsf(z[j]);
     }
     return outgrown(top, all_l, all_z);

@@ -171,3 +171,33 @@ def test_rows_whose_spread_just_fits():
     s.cache.read(s.batch(), kb, vb, stream())
     for got, ref in zip((kb, vb), s.rows(0)[:, 3:]):
         assert torch.equal(got.cpu(), torch.from_numpy(ref.astype(np.float32)))
+
+
+# ---- rows beside rows that are NaN --------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_growing_weights_beside_a_row_that_is_nan(dtype):
+    """Tokens 0 to 15 see a key that is NaN, the others do not, and share their lanes: the others' weights grow by 2^28 while the values are 0,
+    then the values are 1."""
+    import torch
+    from oracle import kv as O
+    new, ctx, window = 64, 200, 150
+    s = Setup(dtype, 1, 64, 64, [new], [ctx])
+    n = new + ctx
+    first = ctx + 15 - window + 1  # the last token's of the first 16 first key
+    k, v = np.zeros((n, 1, 64)), np.zeros((n, 1, 64))
+    k[first] = np.nan
+    grown = (np.arange(n) >= first + 65) & (np.arange(n) % 16 < 4)  # keys of the lanes that have the one that is NaN
+    k[grown] = 28 * np.log(2) / (64 * 0.125)  # a logit of 28 to base 2 with a q of ones
+    v[ctx - 10:] = 1
+    s.fill([k], [v])
+    s.to_gpu()
+    q, q64 = put(np.ones((new, 1, 64)), dtype)
+    out = torch.zeros_like(q)
+    s.cache.attend(s.batch(), q, out, 0.125, None, True, window, stream=stream())
+    got = host(out)
+    kk, vv = s.rows(0)
+    ref, amp, size = O.attend(q64, np.nan_to_num(kk), vv, 0.125, s.places(0), window=window)
+    assert np.isnan(got[:16]).all()
+    bound = DT[dtype][0] * np.abs(ref) + (amp * (2.0 ** -10 + 2.0 ** -15 * size))[..., None]
+    assert (np.abs(got - ref) <= bound)[16:].all()
