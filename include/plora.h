@@ -496,8 +496,8 @@ int plora_kv_read(const plora_kv_cache* cache, const plora_kv_batch* batch, cons
  * offset of 64 to the codes, which takes 6 of their 24 bits.  causal != 0: a token at place s sees the places up to s, with
  * window > 0 the last `window` of them only; causal = 0 (window 0): every place of its sequence, as for queries that look
  * at an encoder's states.  A token that sees no key gets 0.  NaN in rows that a token does not see do not reach it.
- * q and values may be of any size, and keys up to 1e37, with products q . K that 32 bits hold (scale up to 1); beside values
- * above 1e30 small weights are dropped (below 2^-38 of the largest one for 1e30, below 2^-10 for 3e38).
+ * q and values may be of any size and keys up to 1e37, with scale up to 1 and scale * q . K up to 1e7 in size; beside values above
+ * 1e30 small weights are dropped (below 2^-38 of the largest one for 1e30, below 2^-10 for 3e38).
  * rotary (or NULL): applied to q on the way.  n_heads: a multiple of n_kv_heads; scale > 0 and finite.
  * A sequence may have 2^30 keys: LIMIT if min(max_len, table_stride * page_tokens) is more.
  * workspace: device, 16-byte aligned, of any size (0 and NULL too): room for partial results.  With few tokens and many

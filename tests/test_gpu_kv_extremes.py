@@ -201,3 +201,15 @@ def test_growing_weights_beside_a_row_that_is_nan(dtype):
     assert np.isnan(got[:16]).all()
     bound = DT[dtype][0] * np.abs(ref) + (amp * (2.0 ** -10 + 2.0 ** -15 * size))[..., None]
     assert (np.abs(got - ref) <= bound)[16:].all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("q_std,v_std", [(3e2, 1.0), (1e5, 1e9), (1e6, 1e-9), (1e6, 1.0)])
+def test_large_logits(form, dtype, q_std, v_std):
+    """Logits up to 1e7 leave one key's values, or a few, which are a mean of values all the same: no further out than the outermost one."""
+    s, heads, workspace, n = one(form, dtype)
+    out = host(check_attention(s, heads, q_std=q_std, v_std=v_std, workspace=workspace))
+    low, high = s.rows(0)[1].min((0, 1)), s.rows(0)[1].max((0, 1))
+    slack = (DT[dtype][0] + 2 * 2.0 ** (-22 if dtype == "fp32" else -11)) * np.maximum(np.abs(low), np.abs(high))  # the result's rounding, the weights' bits
+    assert (out >= low - slack).all() and (out <= high + slack).all()
