@@ -701,8 +701,8 @@ __global__ __launch_bounds__(kThreads) void k_read(CacheArgs a) {
 // So a row of keys or values costs its codes' unpacking (9 instructions per 8 codes) and no multiplication by its scale, and what
 // lies in places that are not seen cannot hurt: codes are finite whatever the memory holds, and scale and min are dropped
 // where a key is masked.  q is multiplied by a power of two per row that brings it into fp16's range; fp32 rows, and their weights, go as a
-// high and a low half.  The power is undone where large keys do not meet it alone (keys of 1e34 and a q of 1e-34, times 2^122, have a logit of
-// the order of 1, but their products would pass fp32): with few rows half of it ahead of the key's scale and half in the softmax's
+// high and a low half.  The power is undone where large keys do not meet it alone (keys of 1e36 and a q of 1e-34, times 2^120, have a logit of
+// the order of 100, but their products would pass fp32): with few rows half of it ahead of the key's scale and half in the softmax's
 // factor; with many rows, which have no instruction to spare, all of it in the factor, and every key's scale and min are held times 2^-14,
 // which is as much as the factor of the largest rows has room for: keys of 1e37 fit whatever their signs are.  (A flag per 32 keys and
 // 2^-40 where one of them passes 2^90: 3 % of a long chunk's time.)
