@@ -508,6 +508,115 @@ int plora_kv_attend(const plora_kv_cache* cache, const plora_kv_batch* batch, in
                     uint64_t workspace_bytes, plora_stream stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * The base layer that the adapters belong to: norms between its blocks, base weights and activations in 8 bits, their
+ * products, and layers of experts.  As above: no pool, no allocation, no synchronisation, kernels only on `stream`, every buffer the
+ * caller's, and what device arrays hold is defined below for every value.
+ *
+ * Matrices.  plora_matrix: rows of contiguous elements, row r at data + r * stride (in elements; outputs: at least a row).  data
+ * is 16-byte aligned and the stride a multiple of 16 bytes (routing's logits: any).  Inputs may have stride 0 (one row for all). */
+typedef struct {
+  void* data; /* device; read only where the call takes a const plora_matrix that it does not write */
+  int64_t stride;
+} plora_matrix;
+
+/* Rows in 8 bits: k values as e4m3 codes (4 exponent and 3 mantissa bits, largest value 448, no infinities), and for each block of 128 of them
+ * (the last one may be short) a scale; a code c stands for scale * c.  Made from values x of a block with amax = max |x|, in 32 bits:
+ *   scale = amax / 448,  code = e4m3(x * (448 / amax)), to nearest, ties to even;  amax < 2^-100: scale and codes 0;
+ *   a value that is not finite: scale NaN, codes 0 (every value of the block stands for NaN).
+ * Scale of block b of row r at scales[b * scale_stride + r].  codes 16-byte aligned, code_stride (bytes) a multiple of 8, at least k. */
+typedef struct {
+  void* codes;          /* device */
+  float* scales;        /* device */
+  int64_t code_stride;  /* bytes from row to row */
+  int64_t scale_stride; /* floats from block to block, at least the number of rows */
+} plora_fp8_rows;
+
+/* Weights in 8 bits: n_experts matrices (1 for a plain one) of n rows of k codes, [n_experts][n][k], 16-byte aligned; one scale for every
+ * block of 128 rows x 128 values, [n_experts][ceil(n / 128)][ceil(k / 128)].  Row j has the weights of output channel j. */
+typedef struct {
+  int32_t n_experts; /* 1 .. 1024 */
+  int32_t n;         /* output channels, a multiple of 8, up to 2^20 */
+  int32_t k;         /* input channels, a multiple of 16, up to 2^20 */
+  void* codes;       /* device */
+  float* scales;     /* device */
+} plora_fp8_weights;
+
+typedef enum { PLORA_ACT_NONE = 0, PLORA_ACT_SILU = 1, PLORA_ACT_GELU = 2 } plora_activation;
+
+/* Rows of x in 8 bits; k a multiple of 8, up to 2^20.  activation NONE: x has k values a row.  SILU, GELU: x has 2k, and what is taken is
+ *   act(x[r, j]) * x[r, k + j],  silu(a) = a / (1 + exp(-a)),  gelu(a) = a / 2 * (1 + tanh(sqrt(2/pi) (a + 0.044715 a^3))),
+ * in 32 bits, without a rounding before the codes are chosen. */
+int plora_fp8_quantise(int32_t dtype, int32_t n_rows, int32_t k, const plora_matrix* x, int32_t activation, const plora_fp8_rows* out, plora_stream stream);
+
+/* Weights in 8 bits from w: n_experts * n rows of k values, expert after expert (codes and scales by the rule of rows, for blocks of 128 x 128). */
+int plora_fp8_quantise_weights(int32_t dtype, const plora_matrix* w, const plora_fp8_weights* out, plora_stream stream);
+
+/* out[r, j] = sum over blocks b of  (x scale[b, r] * w scale[j / 128, b]) * sum over the block of (x code * w code),
+ * n_rows x n values of dtype; w->n_experts must be 1, x's code_stride a multiple of 16.  Sums in 32 bits, one rounding at the end.  The two
+ * scales are multiplied first, in 32 bits: where their product is below 2^-126 bits of it are lost.  The order of the sums depends on
+ * the sizes only, not on the other rows' contents. */
+int plora_fp8_matmul(const plora_fp8_rows* x, const plora_fp8_weights* w, int32_t dtype, int32_t n_rows, const plora_matrix* out, plora_stream stream);
+
+/* The same with a matrix for each group of rows: out rows offsets[e] .. offsets[e+1] - 1 are products with expert e's weights.  offsets: device,
+ * n_experts + 1 entries, ascending, as plora_route makes them; each is held to [0, n_rows], and a group that ends ahead of its
+ * start is empty.  Rows of no group are left alone; where groups overlap (offsets that are not ascending) their rows are undefined.
+ * rows: device, n_rows entries, or NULL: the x row of every out row (one x row may be read for several); an entry outside
+ * [0, n_x_rows) gives a row of NaN.  NULL: x row r for out row r (n_x_rows >= n_rows). */
+int plora_fp8_grouped(const plora_fp8_rows* x, int32_t n_x_rows, const plora_fp8_weights* w, const int32_t* offsets, const int32_t* rows,
+                      int32_t dtype, int32_t n_rows, const plora_matrix* out, plora_stream stream);
+
+/* Tokens to experts.  logits: n_tokens rows of n_experts (1 .. 1024) values; of each the top_k (1 .. 32, at most n_experts) largest are chosen, largest first,
+ * ties to the lowest index.  A logit of -inf or NaN is never chosen (padding: a row of -inf), and where fewer than top_k are left
+ * the rest have expert -1, weight 0, place -1.  In 32 bits:
+ *   weights[t, j] = scale * p_j / (renormalise ? sum of the chosen p : 1),  p = softmax of the token's logits;
+ * all weights of a token that has a logit of NaN or +inf are NaN.
+ * Behind the choice the chosen (token, j) are sorted by expert, then by token: offsets[n_experts + 1] is where each expert's rows start
+ * and end, rows[n_tokens * top_k] the token of every sorted row (-1 behind the last one), places[t, j] where (t, j) went.
+ * All outputs: device, int32 (weights: float), contiguous.  workspace: device, 16-byte aligned, at least
+ * plora_route_workspace_bytes (0 up to 64 tokens); its contents do not matter; calls that may overlap need one each. */
+uint64_t plora_route_workspace_bytes(int32_t n_tokens, int32_t n_experts);
+int plora_route(int32_t dtype, int32_t n_tokens, int32_t n_experts, int32_t top_k, const plora_matrix* logits, int32_t renormalise, float scale,
+                int32_t* experts, float* weights, int32_t* offsets, int32_t* rows, int32_t* places, void* workspace, uint64_t workspace_bytes,
+                plora_stream stream);
+
+/* A norm's parameters:  norm(v) = (v - m) / sqrt(mean((v - m)^2) + eps) * (offset + weight) + bias,  m = mean(v) if center, else 0. */
+typedef struct {
+  const void* weight; /* device, dim values of the call's dtype, 16-byte aligned; NULL: 0 with offset 1 */
+  const void* bias;   /* the same, or NULL: none */
+  float eps;          /* >= 0 and finite */
+  float offset;       /* finite; 0, or 1 for weights that are held as their distance from 1 */
+  int32_t center;     /* 0 or 1 */
+} plora_norm_weights;
+
+/* What lies between two blocks of a layer:
+ *   u = block[t],  or with places  sum over j < top_k of place_weights[t, j] * block[places[t, j]]   (the experts' rows of the token)
+ *   hidden = residual + scale * gate * post(u),      y = pre(hidden)
+ * in 32 bits, each result rounded once: y comes from hidden as it is ahead of its rounding.  Parts that are NULL are left out: residual (0), gate (1), post and
+ * pre (the value itself), hidden and out (not written).  y goes to out (rows of dtype) or out8 (8 bits), not both; at least one of hidden, out, out8.
+ * Squares are summed in 32 bits.  Entries of places outside [0, n_block_rows) add nothing, whatever their weight.
+ * hidden and out may each be block (without places), residual or gate (same data and stride, a gate or residual of one row for all apart);
+ * otherwise outputs overlap nothing. */
+typedef struct {
+  int32_t dtype;    /* of every matrix and of the norms' weights */
+  int32_t n_tokens;
+  int32_t dim;      /* a multiple of 8, up to 16384 */
+  float scale;      /* finite */
+  const plora_matrix* block;
+  const int32_t* places;      /* device, n_tokens x top_k entries, or NULL */
+  const float* place_weights; /* device, as places */
+  int32_t top_k;              /* with places: 1 .. 32 */
+  int32_t n_block_rows;       /* with places: rows of block, >= 0 */
+  const plora_norm_weights* post;
+  const plora_matrix* gate;
+  const plora_matrix* residual;
+  const plora_matrix* hidden;
+  const plora_norm_weights* pre;
+  const plora_matrix* out;
+  const plora_fp8_rows* out8;
+} plora_block_norm;
+int plora_norm(const plora_block_norm* args, plora_stream stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Traffic predictor (Sec. III-A), host only: every pointer below is a host pointer and no call
  * touches the GPU.  A stack of `layers` LSTM layers of `hidden` units over a sliding window of
  * `window` prediction intervals, followed by a fully connected layer that gives one access

@@ -27,13 +27,18 @@ __all__ = ["PLORA_OK", "PLORA_ERR_INVAL", "PLORA_ERR_NOMEM", "PLORA_ERR_EXISTS",
            "plora_suggest_page_bytes",
            "PLORA_ROTARY_NONE", "PLORA_ROTARY_LINEAR", "PLORA_ROTARY_NTK", "PLORA_ROTARY_TURNS",
            "plora_rotary_table", "plora_rotate", "plora_kv_page_bytes", "plora_kv_append", "plora_kv_read", "plora_kv_attend",
-           "RotaryConfig", "RotaryStruct", "RowsStruct", "KvCacheStruct", "KvBatchStruct", "Rotary", "KvBatch", "PagedKvCache"]
+           "RotaryConfig", "RotaryStruct", "RowsStruct", "KvCacheStruct", "KvBatchStruct", "Rotary", "KvBatch", "PagedKvCache",
+           "PLORA_ACT_NONE", "PLORA_ACT_SILU", "PLORA_ACT_GELU",
+           "plora_norm", "plora_fp8_quantise", "plora_fp8_quantise_weights", "plora_fp8_matmul", "plora_fp8_grouped", "plora_route",
+           "plora_route_workspace_bytes", "MatrixStruct", "Fp8RowsStruct", "Fp8WeightsStruct", "NormWeightsStruct", "BlockNormStruct",
+           "Fp8Rows", "Fp8Weights", "Routing", "NormWeights", "BlockNorm"]
 
 PLORA_OK, PLORA_ERR_INVAL, PLORA_ERR_NOMEM, PLORA_ERR_EXISTS = 0, -1, -2, -3
 PLORA_ERR_NOTFOUND, PLORA_ERR_BUSY, PLORA_ERR_HIP, PLORA_ERR_LIMIT = -4, -5, -6, -7
 PLORA_F16, PLORA_BF16, PLORA_F32 = 0, 1, 2
 PLORA_POOL_PLACEMENT_ONLY = 1
 PLORA_ROTARY_NONE, PLORA_ROTARY_LINEAR, PLORA_ROTARY_NTK, PLORA_ROTARY_TURNS = 0, 1, 2, 3
+PLORA_ACT_NONE, PLORA_ACT_SILU, PLORA_ACT_GELU = 0, 1, 2
 _STATUS = {0: "OK", -1: "INVAL", -2: "NOMEM", -3: "EXISTS", -4: "NOTFOUND", -5: "BUSY", -6: "HIP", -7: "LIMIT"}
 
 LIB_PATH = os.environ.get("PLORA_LIB") or os.path.join(os.path.dirname(os.path.abspath(__file__)), "libplora.so")
@@ -878,3 +883,276 @@ class PagedKvCache:
         if rc:
             _check(call, rc)
         return out
+
+
+# ---------------------------------------------------------------------------------------------
+# the base layer: norms between blocks, rows and weights in 8 bits, their products, routing
+# ---------------------------------------------------------------------------------------------
+class MatrixStruct(C.Structure):
+    """plora_matrix; stride in elements."""
+    _fields_ = [("data", _vp), ("stride", C.c_int64)]
+
+
+class Fp8RowsStruct(C.Structure):
+    _fields_ = [("codes", _vp), ("scales", _vp), ("code_stride", C.c_int64), ("scale_stride", C.c_int64)]
+
+
+class Fp8WeightsStruct(C.Structure):
+    _fields_ = [("n_experts", _i32), ("n", _i32), ("k", _i32), ("codes", _vp), ("scales", _vp)]
+
+
+class NormWeightsStruct(C.Structure):
+    _fields_ = [("weight", _vp), ("bias", _vp), ("eps", _f32), ("offset", _f32), ("center", _i32)]
+
+
+_matrix_p, _fp8_rows_p, _fp8_weights_p, _norm_p = (C.POINTER(t) for t in (MatrixStruct, Fp8RowsStruct, Fp8WeightsStruct, NormWeightsStruct))
+
+
+class BlockNormStruct(C.Structure):
+    _fields_ = [("dtype", _i32), ("n_tokens", _i32), ("dim", _i32), ("scale", _f32), ("block", _matrix_p), ("places", _vp), ("place_weights", _vp),
+                ("top_k", _i32), ("n_block_rows", _i32), ("post", _norm_p), ("gate", _matrix_p), ("residual", _matrix_p), ("hidden", _matrix_p),
+                ("pre", _norm_p), ("out", _matrix_p), ("out8", _fp8_rows_p)]
+
+
+lib.plora_norm.argtypes = [C.POINTER(BlockNormStruct), _vp]
+lib.plora_fp8_quantise.argtypes = [_i32, _i32, _i32, _matrix_p, _i32, _fp8_rows_p, _vp]
+lib.plora_fp8_quantise_weights.argtypes = [_i32, _matrix_p, _fp8_weights_p, _vp]
+lib.plora_fp8_matmul.argtypes = [_fp8_rows_p, _fp8_weights_p, _i32, _i32, _matrix_p, _vp]
+lib.plora_fp8_grouped.argtypes = [_fp8_rows_p, _i32, _fp8_weights_p, _vp, _vp, _i32, _i32, _matrix_p, _vp]
+lib.plora_route.argtypes = [_i32, _i32, _i32, _i32, _matrix_p, _i32, _f32, _vp, _vp, _vp, _vp, _vp, _vp, _u64, _vp]
+lib.plora_route_workspace_bytes.argtypes = [_i32, _i32]
+lib.plora_route_workspace_bytes.restype = _u64
+
+
+def plora_norm(args, stream=None):
+    """args: BlockNormStruct."""
+    return lib.plora_norm(args, stream)
+
+
+def plora_fp8_quantise(dtype, n_rows, k, x, activation, out, stream=None):
+    """x: MatrixStruct, out: Fp8RowsStruct."""
+    return lib.plora_fp8_quantise(dtype, n_rows, k, x, activation, out, stream)
+
+
+def plora_fp8_quantise_weights(dtype, w, out, stream=None):
+    """w: MatrixStruct, out: Fp8WeightsStruct."""
+    return lib.plora_fp8_quantise_weights(dtype, w, out, stream)
+
+
+def plora_fp8_matmul(x, w, dtype, n_rows, out, stream=None):
+    """x: Fp8RowsStruct, w: Fp8WeightsStruct, out: MatrixStruct."""
+    return lib.plora_fp8_matmul(x, w, dtype, n_rows, out, stream)
+
+
+def plora_fp8_grouped(x, n_x_rows, w, offsets_ptr, rows_ptr, dtype, n_rows, out, stream=None):
+    return lib.plora_fp8_grouped(x, n_x_rows, w, offsets_ptr, rows_ptr, dtype, n_rows, out, stream)
+
+
+def plora_route_workspace_bytes(n_tokens, n_experts):
+    return lib.plora_route_workspace_bytes(n_tokens, n_experts)
+
+
+def plora_route(dtype, n_tokens, n_experts, top_k, logits, renormalise, scale, experts_ptr, weights_ptr, offsets_ptr, rows_ptr, places_ptr,
+                workspace_ptr=None, workspace_bytes=0, stream=None):
+    """logits: MatrixStruct."""
+    return lib.plora_route(dtype, n_tokens, n_experts, top_k, logits, int(renormalise), scale, experts_ptr, weights_ptr, offsets_ptr, rows_ptr, places_ptr,
+                           workspace_ptr, workspace_bytes, stream)
+
+
+_ELEMENTS = (PLORA_F16, PLORA_BF16, PLORA_F32)
+_EIGHT = ("torch.float8_e4m3fn", "torch.uint8")
+
+
+def _matrix_of(call, t, n_rows, width, dtype, device):
+    """plora_matrix of a torch tensor [rows, width] (a row's elements one behind the other)."""
+    st = t.stride()
+    if t.shape != (n_rows, width) or (width > 1 and st[1] != 1) or _dtype_of(t) != dtype or t.get_device() != device:
+        raise PloraError(call, PLORA_ERR_INVAL)
+    return MatrixStruct(t.data_ptr(), st[0])
+
+
+def _two(call, t):
+    if t.dim() != 2:
+        raise PloraError(call, PLORA_ERR_INVAL)
+    return t.shape
+
+
+# The classes below take torch tensors as those above do: all of the GPU that is torch's current one at the call; stream None is the null stream.
+class Fp8Rows:
+    """Rows of k values in 8 bits: codes [rows, k] (float8_e4m3fn, or uint8 with the same bytes) and scales [ceil(k / 128), rows] (float32)."""
+
+    def __init__(self, codes, scales):
+        call = "Fp8Rows"
+        n, k = _two(call, codes)
+        blocks, rows = _two(call, scales)
+        self.device = codes.get_device()
+        if self.device < 0 or scales.get_device() != self.device or str(codes.dtype) not in _EIGHT or str(scales.dtype) != "torch.float32" or rows != n or \
+                blocks != -(-k // 128) or (k > 1 and codes.stride(1) != 1) or (n > 1 and scales.stride(1) != 1):
+            raise PloraError(call, PLORA_ERR_INVAL)
+        self.codes, self.scales = codes, scales  # kept alive
+        self.n, self.k = n, k
+        # (a tensor of one row or one block may have any stride there)
+        self.c = Fp8RowsStruct(codes.data_ptr(), scales.data_ptr(), codes.stride(0) if n > 1 else -(-k // 16) * 16, scales.stride(0) if blocks > 1 else n)
+
+    def quantise(self, x, activation=PLORA_ACT_NONE, stream=None):
+        """Becomes x [rows, k]; with an activation x is [rows, 2k], the gate's half first."""
+        call = "plora_fp8_quantise"
+        device = _device()
+        dtype = _dtype_of(x)
+        if self.device != device or dtype not in _ELEMENTS:
+            raise PloraError(call, PLORA_ERR_INVAL)
+        rc = lib.plora_fp8_quantise(dtype, self.n, self.k, _matrix_of(call, x, self.n, self.k if activation == PLORA_ACT_NONE else 2 * self.k, dtype, device),
+                                    activation, self.c, stream)
+        if rc:
+            _check(call, rc)
+        return self
+
+
+class Fp8Weights:
+    """Weights in 8 bits: codes [n, k], or [experts, n, k] for grouped products, and scales [.., ceil(n / 128), ceil(k / 128)], contiguous."""
+
+    def __init__(self, codes, scales):
+        call = "Fp8Weights"
+        if codes.dim() not in (2, 3) or scales.dim() != codes.dim():
+            raise PloraError(call, PLORA_ERR_INVAL)
+        n, k = codes.shape[-2:]
+        experts = codes.shape[0] if codes.dim() == 3 else 1
+        self.device = codes.get_device()
+        if self.device < 0 or scales.get_device() != self.device or str(codes.dtype) not in _EIGHT or str(scales.dtype) != "torch.float32" or \
+                scales.shape != (*codes.shape[:-2], -(-n // 128), -(-k // 128)) or not codes.is_contiguous() or not scales.is_contiguous():
+            raise PloraError(call, PLORA_ERR_INVAL)
+        self.codes, self.scales = codes, scales  # kept alive
+        self.n, self.k = n, k
+        self.c = Fp8WeightsStruct(experts, n, k, codes.data_ptr(), scales.data_ptr())
+
+    def quantise(self, w, stream=None):
+        """Becomes w, of the codes' shape and contiguous."""
+        call = "plora_fp8_quantise_weights"
+        dtype = _dtype_of(w)
+        if self.device != _device() or w.get_device() != self.device or dtype not in _ELEMENTS or w.shape != self.codes.shape or not w.is_contiguous():
+            raise PloraError(call, PLORA_ERR_INVAL)
+        rc = lib.plora_fp8_quantise_weights(dtype, MatrixStruct(w.data_ptr(), self.k), self.c, stream)
+        if rc:
+            _check(call, rc)
+        return self
+
+    def matmul(self, x, out, stream=None):
+        """out [rows, n] = x (Fp8Rows) times the weights."""
+        call = "plora_fp8_matmul"
+        device = _device()
+        dtype = _dtype_of(out)
+        if self.device != device or x.device != device or x.k != self.k or dtype not in _ELEMENTS:
+            raise PloraError(call, PLORA_ERR_INVAL)
+        rc = lib.plora_fp8_matmul(x.c, self.c, dtype, x.n, _matrix_of(call, out, x.n, self.n, dtype, device), stream)
+        if rc:
+            _check(call, rc)
+        return out
+
+    def grouped(self, x, offsets, out, rows=None, stream=None):
+        """Out rows offsets[e] .. offsets[e + 1] - 1 = their x rows times expert e's weights; rows (int32): the x row of every out row."""
+        call = "plora_fp8_grouped"
+        device = _device()
+        dtype = _dtype_of(out)
+        if self.device != device or x.device != device or x.k != self.k or dtype not in _ELEMENTS:
+            raise PloraError(call, PLORA_ERR_INVAL)
+        n = _two(call, out)[0]
+        rc = lib.plora_fp8_grouped(x.c, x.n, self.c, _ints_of(call, offsets, self.c.n_experts + 1, device),
+                                   None if rows is None else _ints_of(call, rows, n, device), dtype, n,
+                                   _matrix_of(call, out, n, self.n, dtype, device), stream)
+        if rc:
+            _check(call, rc)
+        return out
+
+
+class Routing:
+    """What routing writes (int32 tensors but for weights, float32; contiguous, on the GPU): experts, weights and places [tokens, top_k],
+    offsets [n_experts + 1], rows [tokens * top_k]; workspace: a contiguous tensor of at least workspace_bytes(tokens, n_experts), or None."""
+
+    def __init__(self, experts, weights, offsets, rows, places, workspace=None):
+        call = "Routing"
+        n, k = _two(call, experts)
+        self.device = dev = offsets.get_device()
+        if dev < 0 or str(weights.dtype) != "torch.float32" or not weights.is_contiguous() or weights.get_device() != dev or weights.shape != (n, k) or \
+                places.shape != (n, k) or (workspace is not None and (not workspace.is_contiguous() or workspace.get_device() != dev)):
+            raise PloraError(call, PLORA_ERR_INVAL)
+        self.experts, self.weights, self.offsets, self.rows, self.places, self.workspace = experts, weights, offsets, rows, places, workspace
+        self.n, self.k, self.n_experts = n, k, offsets.numel() - 1
+        size = 0 if workspace is None else workspace.nbytes
+        self.at = (_ints_of(call, experts, n * k, dev), weights.data_ptr(), _ints_of(call, offsets, 2, dev), _ints_of(call, rows, n * k, dev),
+                   _ints_of(call, places, n * k, dev), workspace.data_ptr() if size else None, size)
+
+    @staticmethod
+    def workspace_bytes(n_tokens, n_experts):
+        return plora_route_workspace_bytes(n_tokens, n_experts)
+
+    def route(self, logits, renormalise=True, scale=1.0, stream=None):
+        """Chooses by logits [tokens, n_experts] and sorts."""
+        call = "plora_route"
+        device = _device()
+        dtype = _dtype_of(logits)
+        if self.device != device or dtype not in _ELEMENTS:
+            raise PloraError(call, PLORA_ERR_INVAL)
+        rc = lib.plora_route(dtype, self.n, self.n_experts, self.k, _matrix_of(call, logits, self.n, self.n_experts, dtype, device), int(renormalise), scale,
+                             *self.at, stream)
+        if rc:
+            _check(call, rc)
+        return self
+
+
+class NormWeights:
+    """A norm's parameters: weight and bias [dim] (or None), eps; center: the mean is taken off first; offset: added to the weight."""
+
+    def __init__(self, weight=None, bias=None, eps=1e-6, center=False, offset=0.0):
+        call = "NormWeights"
+        self.kept = [t for t in (weight, bias) if t is not None]
+        for t in self.kept:
+            if t.dim() != 1 or not t.is_contiguous() or t.get_device() < 0 or t.shape != self.kept[0].shape or t.dtype != self.kept[0].dtype or \
+                    t.get_device() != self.kept[0].get_device():
+                raise PloraError(call, PLORA_ERR_INVAL)
+        self.c = NormWeightsStruct(None if weight is None else weight.data_ptr(), None if bias is None else bias.data_ptr(), eps, offset, int(center))
+
+    def fits(self, dim, dtype, device):
+        return not self.kept or (self.kept[0].numel() == dim and _dtype_of(self.kept[0]) == dtype and self.kept[0].get_device() == device)
+
+
+class BlockNorm:
+    """What lies between two blocks: hidden = residual + scale * gate * post(block), result = pre(hidden); pre, post: NormWeights or None."""
+
+    def __init__(self, pre=None, post=None, scale=1.0):
+        self.pre, self.post, self.scale = pre, post, scale
+
+    def run(self, block, residual=None, hidden=None, out=None, out8=None, gate=None, places=None, place_weights=None, stream=None):
+        """block, residual, hidden, out, gate: [tokens, dim]; gate may be [dim], one for all tokens; out8: Fp8Rows in place of out.
+        places (int32 [tokens, top_k], as Routing has them) and place_weights: block's rows are the experts', and a token takes the weighted sum of its own."""
+        call = "plora_norm"
+        device = _device()
+        dtype = _dtype_of(block)
+        n, dim = _two(call, block)
+        if dtype not in _ELEMENTS:
+            raise PloraError(call, PLORA_ERR_INVAL)
+        top_k, block_rows = 0, n
+        if places is not None:
+            n, top_k = _two(call, places)
+            if place_weights is None or place_weights.shape != (n, top_k) or str(place_weights.dtype) != "torch.float32" or \
+                    not place_weights.is_contiguous() or place_weights.get_device() != device:
+                raise PloraError(call, PLORA_ERR_INVAL)
+        elif place_weights is not None:
+            raise PloraError(call, PLORA_ERR_INVAL)
+        for p in (self.pre, self.post):
+            if p is not None and not p.fits(dim, dtype, device):
+                raise PloraError(call, PLORA_ERR_INVAL)
+        if out8 is not None and (out8.device != device or out8.n != n or out8.k != dim):
+            raise PloraError(call, PLORA_ERR_INVAL)
+
+        def of(t, rows=n):
+            return None if t is None else C.pointer(_matrix_of(call, t, rows, dim, dtype, device))
+
+        if gate is not None and gate.dim() == 1:
+            gate = gate.expand(n, dim)
+        args = BlockNormStruct(dtype, n, dim, self.scale, of(block, block_rows), None if places is None else _ints_of(call, places, n * top_k, device),
+                               None if places is None else place_weights.data_ptr(), top_k, block_rows if places is not None else 0,
+                               None if self.post is None else C.pointer(self.post.c), of(gate), of(residual), of(hidden),
+                               None if self.pre is None else C.pointer(self.pre.c), of(out), None if out8 is None else C.pointer(out8.c))
+        rc = lib.plora_norm(args, stream)
+        if rc:
+            _check(call, rc)
