@@ -14,8 +14,6 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kBlock = 128;
 
-__device__ const uint4 g_zeros = {0, 0, 0, 0};  // what codes behind the last one of a row are taken from
-
 struct ProductArgs {
   const uint8_t* x;
   const float* xs;
@@ -30,13 +28,27 @@ struct ProductArgs {
 typedef __attribute__((address_space(3))) void lds_void;
 __device__ __forceinline__ uint32_t lds_addr(const void* p) { return (uint32_t)(uintptr_t)(const lds_void*)p; }
 // 16 bytes per lane from memory into LDS at dst + 16 * lane (dst: a uniform LDS address), in assembly because the compiler
-// makes every later LDS read wait for all such loads.  (No output registers: nothing is in flight but LDS bytes.)
+// makes every later LDS read wait for all such loads.  (No output registers: nothing is in flight but LDS bytes.)  Memory is named by
+// a base in scalar registers, a lane's offset and a uniform one; an offset of kNowhere is out of the buffer's range: zeros.
+constexpr uint32_t kNowhere = 0x80000000u, kReach = 0x7fffffffu;
+__device__ __forceinline__ i32x4 buffer_at(const uint8_t* p) {
+  const uint64_t a = (uint64_t)(uintptr_t)p;
+  return i32x4{__builtin_amdgcn_readfirstlane((int)a), __builtin_amdgcn_readfirstlane((int)(a >> 32) & 0xffff), (int)kReach, 0x00020000};
+}
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"  // (m0 is a reserved register; naming it orders other writers of it)
-__device__ __forceinline__ void load_to_lds(const uint8_t* src, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(dst) : "memory", "m0");
+__device__ __forceinline__ void load_to_lds(i32x4 buffer, uint32_t offset, uint32_t uniform, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" : : "v"(offset), "s"(buffer), "s"(uniform), "s"(dst) : "memory", "m0");
+}
+__device__ __forceinline__ void load_word_to_lds(i32x4 buffer, uint32_t offset, uint32_t dst) {  // 4 bytes per lane
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" : : "v"(offset), "s"(buffer), "s"(dst) : "memory", "m0");
 }
 #pragma clang diagnostic pop
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // until at most N of the wavefront's vector memory accesses, and none of its LDS reads, are in flight
+  static_assert(N >= 0 && N < 64, "six bits");
+  __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14));
+}
 
 __device__ __forceinline__ f32x4 dot128(i32x8 w, i32x8 x) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
@@ -52,23 +64,32 @@ __device__ __forceinline__ int32_t clamped(int32_t v, int32_t hi) { return v < 0
 // bands of kBand row tiles, so that what runs on it at once shares rows and weights in its L2.
 template <int TT, int TN, bool GROUPED>
 __device__ __forceinline__ Tile tile_of(const ProductArgs& a) {
-  constexpr uint32_t kBand = 8;
+  constexpr uint32_t kBand = 4;
   Tile t = {0, 0, 0, 0, false};
   const uint32_t columns = (uint32_t)(a.n + TN - 1) / TN;
   const int lane = threadIdx.x & 63;
-  uint32_t row_tiles;
-  if constexpr (!GROUPED) {
-    row_tiles = (uint32_t)(a.n_rows + TT - 1) / TT;
-  } else {
-    uint32_t s = 0;
-    for (int e = lane; e < a.n_experts; e += 64) {
-      const int32_t n = clamped(a.offsets[e + 1], a.n_rows) - clamped(a.offsets[e], a.n_rows);
-      s += n > 0 ? (uint32_t)(n + TT - 1) / TT : 0;
+  // experts e0 .. e0 + 63, one a lane: their rows, their row tiles, and the sum of these up to the lane's
+  int32_t from = 0, to = 0;
+  uint32_t n = 0, sum = 0;
+  const auto look = [&](int e0) {
+    const int e = e0 + lane;
+    from = to = 0;
+    if (e < a.n_experts) {
+      from = clamped(a.offsets[e], a.n_rows);
+      to = clamped(a.offsets[e + 1], a.n_rows);
     }
+    sum = n = to > from ? (uint32_t)(to - from + TT - 1) / TT : 0;
 #pragma unroll
-    for (int i = 1; i < 64; i *= 2) s += __shfl_xor(s, i);
-    row_tiles = __builtin_amdgcn_readfirstlane(s);
-  }
+    for (int i = 1; i < 64; i *= 2) {
+      const uint32_t o = __shfl_up(sum, i);
+      if (lane >= i) sum += o;
+    }
+    return (uint32_t)__builtin_amdgcn_readlane(sum, 63);
+  };
+  uint32_t row_tiles = 0;
+  if constexpr (!GROUPED) row_tiles = (uint32_t)(a.n_rows + TT - 1) / TT;
+  else
+    for (int e0 = 0; e0 < a.n_experts; e0 += 64) row_tiles += look(e0);
   const uint64_t tiles = (uint64_t)row_tiles * columns;
   const uint32_t xcd = blockIdx.x & 7, at = blockIdx.x >> 3, per = (uint32_t)(tiles >> 3), more = (uint32_t)(tiles & 7);
   if (at >= per + (xcd < more ? 1 : 0)) return t;
@@ -84,30 +105,18 @@ __device__ __forceinline__ Tile tile_of(const ProductArgs& a) {
   } else {
     uint32_t before = 0;  // row tiles of the experts ahead
     for (int e0 = 0; e0 < a.n_experts; e0 += 64) {
-      const int e = e0 + lane;
-      int32_t from = 0, to = 0;
-      if (e < a.n_experts) {
-        from = clamped(a.offsets[e], a.n_rows);
-        to = clamped(a.offsets[e + 1], a.n_rows);
-      }
-      const uint32_t n = to > from ? (uint32_t)(to - from + TT - 1) / TT : 0;
-      uint32_t s = n;
-#pragma unroll
-      for (int i = 1; i < 64; i *= 2) {
-        const uint32_t o = __shfl_up(s, i);
-        if (lane >= i) s += o;
-      }
-      const uint64_t here = __ballot(before + s > q);
+      const uint32_t all = a.n_experts <= 64 ? row_tiles : look(e0);
+      const uint64_t here = __ballot(before + sum > q);
       if (here) {
         const int l = __builtin_ctzll(here);
         t.expert = e0 + l;
-        const int32_t skip = (int32_t)(q - before - (__builtin_amdgcn_readlane(s, l) - __builtin_amdgcn_readlane(n, l)));
+        const int32_t skip = (int32_t)(q - before - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(n, l)));
         const int32_t end = __builtin_amdgcn_readlane(to, l);
         t.first = __builtin_amdgcn_readlane(from, l) + skip * TT;
         t.last = end - t.first < TT ? end : t.first + TT;
         break;
       }
-      before += __builtin_amdgcn_readlane(s, 63);
+      before += all;
     }
   }
   return t;
@@ -127,112 +136,305 @@ __device__ __forceinline__ void st4(uint8_t* p, f32x4 f) {
   else *reinterpret_cast<uint2*>(p) = make_uint2(pack_f16(f[0], f[1]), pack_f16(f[2], f[3]));
 }
 
-// Tiles of TT rows x TN channels by WT x WN wavefronts; both operands through LDS, one block of 128 values a stage, two stages.  A stage's
-// rows are 128 bytes; the 16-byte piece p of row r lies at p ^ (r % 8), so that 8 lanes that read one piece of 8 rows meet all banks.
-template <int DT, int TT, int TN, int WT, int WN, bool GROUPED>
-__global__ __launch_bounds__(64 * WT * WN) __attribute__((amdgpu_waves_per_eu(2))) void k_product(ProductArgs a) {
-  constexpr int THREADS = 64 * WT * WN, NT = TT / WT / 16, NN = TN / WN / 16;
-  constexpr int LX = TT * 8 / THREADS, LW = TN * 8 / THREADS;  // 16-byte loads of a thread and stage
-  static_assert(TT * 8 % THREADS == 0 && TN * 8 % THREADS == 0 && TN / WN <= kBlock && kBlock % (TN / WN) == 0, "whole loads, one scale of weights a wavefront");
-  __shared__ alignas(16) uint8_t lds[2][(TT + TN) * kBlock];
+// Tiles of TT rows x TN channels by WT x WN wavefronts, both operands through LDS, a block of 128 values a stage and STAGES of them; with KG > 1
+// so many sets of wavefronts share the blocks in turn, each with stages of its own, and their sums are joined at the end (in
+// their order).  A stage's rows are 128 bytes; the 16-byte piece p of row r lies at p ^ (r / 2 % 8), so that 16 lanes that read one
+// piece of 16 rows meet all 64 banks.
+template <int DT, int TT, int TN, int WT, int WN, int KG, int STAGES, bool GROUPED>
+__global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_eu(2))) void k_product(ProductArgs a) {
+  constexpr int WAVES = WT * WN, NT = TT / WT / 16, NN = TN / WN / 16;
+  constexpr int LX = TT / 8 / WAVES, LW = TN / 8 / WAVES;  // 16-byte loads of a thread and stage
+  // they are spread over the first half of a stage's products: kPer of them every kEvery products
+  constexpr int kHalf = NN * NT / 2, kEvery = kHalf > LX + LW ? kHalf / (LX + LW) : 1, kPer = (LX + LW + kHalf - 1) / kHalf;
+  constexpr int kStage = (TT + TN) * kBlock, kScales = WAVES * 256, kSet = STAGES * (kStage + kScales);
+  static_assert(LX * 8 * WAVES == TT && LW * 8 * WAVES == TN && WAVES % 2 == 0 && NN % 2 == 0 && NT <= 4, "whole loads");
+  static_assert(TN / WN <= kBlock && kBlock % (TN / WN) == 0, "one scale of weights a wavefront");
+  static_assert((LX + LW) / kPer * kEvery < NN * NT, "all loads of a stage are sent between two barriers");
+  static_assert((KG - 1) * TT * TN * 4 <= KG * kSet, "the sums are joined in the stages' place");
+  __shared__ alignas(16) uint8_t lds[KG * kSet];
   const Tile tile = tile_of<TT, TN, GROUPED>(a);
   if (!tile.any) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kb = (a.k + kBlock - 1) / kBlock;
+  const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = all % WAVES, set = all / WAVES;
+  const int kb = (a.k + kBlock - 1) / kBlock, steps = (kb + KG - 1) / KG;
+  const int wt = wave % WT, wn = wave / WT, col = lane & 15, quad = lane >> 4;
 
-  // what this thread loads: rows wave * 8 + lane / 8 of every group of THREADS / 8, the piece that belongs at lane % 8
-  const int piece = (lane & 7) ^ (lane >> 3);
-  const uint8_t *px[LX], *pw[LW];
+  // what this thread loads: rows wave * 8 + lane / 8 of every group of 8 WAVES, the piece that belongs at lane % 8
+  const int piece = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
+  const int64_t first_row = a.rows ? 0 : tile.first;
+  const i32x4 bx = buffer_at(a.x + first_row * a.x_s), bw = buffer_at(a.w + ((int64_t)tile.expert * a.n + tile.channel) * a.k);
+  uint32_t at[LX + LW];
 #pragma unroll
   for (int i = 0; i < LX; ++i) {
-    int32_t r = tile.first + (i * (THREADS / 64) + wave) * 8 + (lane >> 3);
+    int32_t r = tile.first + (i * WAVES + wave) * 8 + (lane >> 3);
     r = x_row(a, r < tile.last ? r : tile.last - 1);
-    px[i] = a.x + (int64_t)(r < 0 ? 0 : r) * a.x_s + piece * 16;
+    at[i] = r < 0 ? 0 : (uint32_t)((r - first_row) * a.x_s) + piece * 16;
   }
-  const uint8_t* w0 = a.w + (int64_t)tile.expert * a.n * a.k;
 #pragma unroll
   for (int i = 0; i < LW; ++i) {
-    const int32_t c = tile.channel + (i * (THREADS / 64) + wave) * 8 + (lane >> 3);
-    pw[i] = w0 + (int64_t)(c < a.n ? c : a.n - 1) * a.k + piece * 16;
+    const int32_t c = (i * WAVES + wave) * 8 + (lane >> 3), most = a.n - 1 - tile.channel;
+    at[LX + i] = (uint32_t)(c < most ? c : most) * a.k + piece * 16;
   }
-  const auto fetch = [&](int b) {
-    const uint32_t to = lds_addr(lds[b & 1]) + wave * 1024;
-    const bool in = b * kBlock + piece * 16 < a.k;
-    const uint8_t* zeros = reinterpret_cast<const uint8_t*>(&g_zeros);
-#pragma unroll
-    for (int i = 0; i < LX; ++i) load_to_lds(in ? px[i] + (int64_t)b * kBlock : zeros, __builtin_amdgcn_readfirstlane(to + i * THREADS * 16));
-#pragma unroll
-    for (int i = 0; i < LW; ++i) load_to_lds(in ? pw[i] + (int64_t)b * kBlock : zeros, __builtin_amdgcn_readfirstlane(to + TT * kBlock + i * THREADS * 16));
+  const auto row_of = [&](int t) {  // the x row of this lane's column in tile t
+    const int32_t r = tile.first + wt * (TT / WT) + t * 16 + col;
+    return x_row(a, r < tile.last ? r : tile.last - 1);
   };
-
-  const int wt = wave % WT, wn = wave / WT, col = lane & 15, quad = lane >> 4;
-  const float* sx[NT];
-  bool hole[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    int32_t r = tile.first + wt * (TT / WT) + t * 16 + col;
-    r = x_row(a, r < tile.last ? r : tile.last - 1);
-    hole[t] = r < 0;
-    sx[t] = a.xs + (r < 0 ? 0 : r);
-  }
+  const int32_t scale_row = row_of(quad % NT);
+  const uint32_t scale_at = scale_row < 0 ? 0 : (uint32_t)(scale_row - first_row) * 4;
+  const uint8_t* mine = lds + set * kSet;
+  const uint32_t to = __builtin_amdgcn_readfirstlane(lds_addr(mine) + wave * 1024), scales_to = __builtin_amdgcn_readfirstlane(lds_addr(mine) + STAGES * kStage + wave * 256);
+  // Load i of the set's step s; behind the last code of the rows, and behind the last block: zeros.  Load LX + LW: the wavefront's scales of x.
+  const auto fetch = [&](int s, int slot, int i) {
+    const int b = s * KG + set;
+    if (i < LX + LW) {
+      load_to_lds(i < LX ? bx : bw, b * kBlock + piece * 16 < a.k ? at[i] : kNowhere, b * kBlock, to + slot * kStage + i * WAVES * 1024);
+    } else {
+      const i32x4 bs = buffer_at(reinterpret_cast<const uint8_t*>(a.xs + first_row + (int64_t)(b < kb ? b : 0) * a.xs_s));
+      load_word_to_lds(bs, b < kb ? scale_at : kNowhere, scales_to + slot * kScales);
+    }
+  };
   const int channel = tile.channel + wn * (TN / WN);  // the wavefront's first one
   const int nb = (a.n + kBlock - 1) / kBlock, cb = channel / kBlock;
-  const float* sw = a.ws + ((int64_t)tile.expert * nb + (cb < nb ? cb : nb - 1)) * kb;
+  typedef const __attribute__((address_space(4))) float* scalar_floats;
+  const scalar_floats sw = (scalar_floats)(uintptr_t)(a.ws + ((int64_t)tile.expert * nb + (cb < nb ? cb : nb - 1)) * kb);
 
-  f32x4 acc[NN][NT] = {};
-  float fx[NT], fw = sw[0];
+  const auto operand = [&](int slot, int row) {
+    const uint8_t* p = mine + slot * kStage + row * kBlock;
+    const int s = (row >> 1) & 7;
+    const i32x4 lo = *reinterpret_cast<const i32x4*>(p + (quad ^ s) * 16), hi = *reinterpret_cast<const i32x4*>(p + ((quad + 4) ^ s) * 16);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  const int row_x = wt * (TT / WT) + col, row_w = TT + wn * (TN / WN) + col;
+
+  // A stage's products go row after row (a row: one operand of weights, all of x).  While the matrix unit has a row, the next row's weights
+  // are read and the products of the row before are scaled and added.  The one barrier of a stage is ahead of its last row: then the
+  // next stage is there and this one has been read, so the last row reads the next stage's operands already, and the loads of the
+  // stage that follows STAGES behind go into this one's place.
 #pragma unroll
-  for (int t = 0; t < NT; ++t) fx[t] = sx[t][0];
-  fetch(0);
-  for (int b = 0; b < kb; ++b) {
-    __builtin_amdgcn_s_waitcnt(0);  // this stage is there, and no read of the other one is under way
-    __syncthreads();
-    float f[NT];
+  for (int s = 0; s < STAGES - 1; ++s)
 #pragma unroll
-    for (int t = 0; t < NT; ++t) f[t] = fx[t] * fw;
-    if (b + 1 < kb) {
-      fetch(b + 1);
-      fw = sw[b + 1];
+    for (int i = 0; i <= LX + LW; ++i) fetch(s, s, i);
+  wait_loads<(STAGES - 2) * (LX + LW + 1)>();
+  __syncthreads();
+  f32x4 acc[NN][NT] = {}, d[NT] = {};
+  i32x8 x[NT], w[2];
+  float f[NT] = {}, fx[NT];
+  const auto scales = [&](int slot) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) fx[t] = sx[t][(int64_t)(b + 1) * a.xs_s];
+    for (int t = 0; t < NT; ++t) fx[t] = *reinterpret_cast<const float*>(mine + STAGES * kStage + slot * kScales + wave * 256 + (t * 16 + col) * 4);
+  };
+  w[0] = operand(0, row_w);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) x[t] = operand(0, row_x + t * 16);
+  scales(0);
+#pragma unroll
+  for (int i = 0; i <= LX + LW && i / kPer * kEvery < NT; ++i) fetch(STAGES - 1, STAGES - 1, i);
+  int slot = 0;
+  for (int s = 0; s < steps; ++s) {
+    const int b = s * KG + set, next = slot + 1 < STAGES ? slot + 1 : 0, free = slot > 0 ? slot - 1 : STAGES - 1;
+    const float fw = b < kb ? sw[b < kb ? b : 0] : 0.f;
+    float before[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      before[t] = f[t];
+      f[t] = fx[t] * fw;
     }
-    const uint8_t* at = lds[b & 1];
-    const auto operand = [&](int row) {
-      const uint8_t* p = at + row * kBlock;
-      const int s = row & 7;
-      const i32x4 lo = *reinterpret_cast<const i32x4*>(p + ((2 * quad) ^ s) * 16), hi = *reinterpret_cast<const i32x4*>(p + ((2 * quad + 1) ^ s) * 16);
-      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
-    i32x8 x[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) x[t] = operand(wt * (TT / WT) + t * 16 + col);
 #pragma unroll
     for (int m = 0; m < NN; ++m) {
-      const i32x8 w = operand(TT + wn * (TN / WN) + m * 16 + col);
+      if (m == NN - 1) {
+        asm volatile("" : : : "memory");  // LDS reads stay on their side of the barrier
+        wait_loads<(STAGES - 2) * (LX + LW + 1)>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" : : : "memory");
+        scales(next);
+      }
+      w[(m + 1) & 1] = m + 1 < NN ? operand(slot, row_w + (m + 1) * 16) : operand(next, row_w);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const f32x4 d = dot128(w, x[t]);
+        f32x4& sum = acc[(m + NN - 1) % NN][t];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[m][t][i] = __builtin_fmaf(f[t], d[i], acc[m][t][i]);
+        for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(m ? f[t] : before[t], d[t][e], sum[e]);
+        d[t] = dot128(w[m & 1], x[t]);
+        if (m == NN - 1) x[t] = operand(next, row_x + t * 16);
+        const int done = (m + 1) % NN * NT + t;  // products since the barrier
+#pragma unroll
+        for (int i = done / kEvery * kPer; done % kEvery == 0 && i <= LX + LW && i < (done / kEvery + 1) * kPer; ++i)
+          if (m == NN - 1) fetch(s + STAGES, slot, i);
+          else fetch(s + STAGES - 1, free, i);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
+    slot = next;
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[NN - 1][t][e] = __builtin_fmaf(f[t], d[t][e], acc[NN - 1][t][e]);
+  __builtin_amdgcn_s_waitcnt(0);  // no load into LDS outlives the workgroup, or comes behind the sums
+  if constexpr (KG > 1) {
+    __syncthreads();
+    f32x4* part = reinterpret_cast<f32x4*>(lds) + wave * NN * NT * 64 + lane;
+    if (set > 0) {
+#pragma unroll
+      for (int m = 0; m < NN; ++m)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) part[((set - 1) * WAVES * NN * NT + m * NT + t) * 64] = acc[m][t];
+    }
+    __syncthreads();
+    if (set > 0) return;
+#pragma unroll
+    for (int m = 0; m < NN; ++m)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int g = 0; g < KG - 1; ++g) {
+          const f32x4 o = part[(g * WAVES * NN * NT + m * NT + t) * 64];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[m][t][e] += o[e];
+        }
   }
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int32_t r = tile.first + wt * (TT / WT) + t * 16 + col;
     if (r >= tile.last) continue;
+    const bool hole = row_of(t) < 0;
     uint8_t* o = a.out + (int64_t)r * a.out_s;
 #pragma unroll
     for (int m = 0; m < NN; ++m) {
       const int c = channel + m * 16 + quad * 4;
       f32x4 y = acc[m][t];
-      if (hole[t]) y = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+      if (hole) y = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
       if (c < a.n) st4<DT>(o + (int64_t)c * Elt<DT>::B, y);
     }
   }
 }
 
+// Few rows: a workgroup has TT rows x 16 NW channels, and its WAVES wavefronts the blocks of 128 values in turn; operands go from memory to registers,
+// P of a wavefront's blocks ahead, with no barrier until the wavefronts' sums are joined in LDS (in their order: the sums do not depend
+// on which is done first).
+template <int DT, int TT, int NW, int WAVES, int P, bool GROUPED>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void k_few(ProductArgs a) {
+  constexpr int NT = TT / 16;
+  __shared__ f32x4 part[WAVES][NW * NT][64];
+  const Tile tile = tile_of<TT, 16 * NW, GROUPED>(a);
+  if (!tile.any) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+  const int kb = (a.k + kBlock - 1) / kBlock;
+  const uint8_t *px[NT], *pw[NW];
+  const float* sx[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int32_t at = tile.first + t * 16 + col, r = x_row(a, at < tile.last ? at : tile.last - 1);
+    px[t] = a.x + (int64_t)(r < 0 ? 0 : r) * a.x_s + quad * 16;
+    sx[t] = a.xs + (r < 0 ? 0 : r);
+  }
+  const uint8_t* w0 = a.w + (int64_t)tile.expert * a.n * a.k;
+#pragma unroll
+  for (int m = 0; m < NW; ++m) {
+    const int c = tile.channel + m * 16 + col;
+    pw[m] = w0 + (int64_t)(c < a.n ? c : a.n - 1) * a.k + quad * 16;
+  }
+  const int nb = (a.n + kBlock - 1) / kBlock;
+  typedef const __attribute__((address_space(4))) float* scalar_floats;
+  const scalar_floats sw = (scalar_floats)(uintptr_t)(a.ws + ((int64_t)tile.expert * nb + tile.channel / kBlock) * kb);
+
+  struct Block {
+    i32x8 w[NW], x[NT];
+    float f[NT];
+  };
+  const auto load = [&](int b, Block& o) {
+    // pieces behind the last code, and blocks behind the last one: the first piece of the row in their place, and x's codes zeroed
+    const int64_t lo = b * kBlock + quad * 16 < a.k ? b * kBlock : -quad * 16, hi = b * kBlock + 64 + quad * 16 < a.k ? b * kBlock + 64 : -quad * 16;
+    const auto both = [&](const uint8_t* p) {
+      return __builtin_shufflevector(*reinterpret_cast<const i32x4*>(p + lo), *reinterpret_cast<const i32x4*>(p + hi), 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+#pragma unroll
+    for (int m = 0; m < NW; ++m) o.w[m] = both(pw[m]);
+    const int at = b < kb ? b : kb - 1;
+    const float fw = sw[at];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      o.x[t] = both(px[t]);
+      o.f[t] = sx[t][(int64_t)at * a.xs_s] * fw;
+    }
+  };
+  f32x4 acc[NW][NT] = {};
+  Block ring[P];
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+    if (p == 0 || wave + p * WAVES < kb) load(wave + p * WAVES, ring[p]);
+  for (int b = wave; b < kb; b += P * WAVES) {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int at = b + p * WAVES;
+      Block now = ring[p];
+      if (at + P * WAVES < kb) load(at + P * WAVES, ring[p]);
+      if (at < kb) {
+        const bool tail = (at + 1) * kBlock > a.k;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          if (tail) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (at * kBlock + (e < 4 ? 0 : 64) + quad * 16 >= a.k) now.x[t][e] = 0;
+          }
+#pragma unroll
+          for (int m = 0; m < NW; ++m) {
+            if (tail) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (at * kBlock + (e < 4 ? 0 : 64) + quad * 16 >= a.k) now.w[m][e] = 0;
+            }
+            const f32x4 d = dot128(now.w[m], now.x[t]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[m][t][e] = __builtin_fmaf(now.f[t], d[e], acc[m][t][e]);
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < NW; ++m)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) part[wave][m * NT + t][lane] = acc[m][t];
+  __syncthreads();
+  for (int i = wave; i < NW * NT; i += WAVES) {
+    const int m = i / NT, t = i % NT;
+    const int32_t r = tile.first + t * 16 + col;
+    const int c = tile.channel + m * 16 + quad * 4;
+    f32x4 y = part[0][i][lane];
+#pragma unroll
+    for (int v = 1; v < WAVES; ++v) {
+      const f32x4 o = part[v][i][lane];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] += o[e];
+    }
+    if (r >= tile.last || c >= a.n) continue;
+    if (x_row(a, r) < 0) y = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+    st4<DT>(a.out + (int64_t)r * a.out_s + (int64_t)c * Elt<DT>::B, y);
+  }
+}
+
 // ---- host side ----------------------------------------------------------------------------------------
+
+// A kernel's tile, and what it takes by a fit to calls of 1 .. 4096 rows times weights of 520 x 1040 .. 13824 x 5120 (and 2 .. 256 experts): 3 us and, for each
+// round of a CU, `fixed` and for every step (KG blocks of 128 values) `step`, with `more` for each further workgroup that
+// runs on the CU beside it, of `at_once`.  All in us.
+struct Kind {
+  int tt, tn, kg, at_once;
+  float fixed, step, more;
+};
+float time_of(const Kind& k, const ProductArgs& a, bool grouped) {
+  float rows = (float)((a.n_rows + (int64_t)k.tt - 1) / k.tt);
+  if (grouped) {  // groups end in a part of a tile, half of one on average; few rows leave some experts without any
+    const float groups = (float)(a.n_experts < a.n_rows ? a.n_experts : a.n_rows), least = 0.8f * groups;
+    rows = (float)(a.n_rows / k.tt) + 0.5f * groups;
+    rows = rows > least && a.n_rows > k.tt * groups * 0.5f ? rows : least;
+  }
+  const float steps = (float)(((a.k + kBlock - 1) / kBlock + k.kg - 1) / k.kg);
+  const int64_t here = ((int64_t)(rows * (float)((a.n + k.tn - 1) / k.tn)) + 255) / 256, rounds = here / k.at_once, rest = here - rounds * k.at_once;
+  const float full = k.fixed + steps * (k.step + k.more * (float)(k.at_once - 1));
+  return 3.f + (float)rounds * full + (rest ? k.fixed + steps * (k.step + k.more * (float)(rest - 1)) : 0.f);
+}
 
 template <int TT, int TN>
 uint64_t tiles(const ProductArgs& a, bool grouped) {
@@ -241,10 +443,54 @@ uint64_t tiles(const ProductArgs& a, bool grouped) {
   const uint64_t n = rows * (((uint64_t)a.n + TN - 1) / TN);
   return (n + 7) / 8 * 8;  // whole rounds over the XCDs
 }
+template <int DT, bool GROUPED, int TT, int TN, int WT, int WN, int KG, int STAGES>
+int tiled(const ProductArgs& a, plora_stream stream) {
+  return launch(k_product<DT, TT, TN, WT, WN, KG, STAGES, GROUPED>, tiles<TT, TN>(a, GROUPED), 1, 1, a, stream, 64 * WT * WN * KG);
+}
+template <int DT, bool GROUPED, int NW, int WAVES, int P>
+int few(const ProductArgs& a, plora_stream stream) {
+  return launch(k_few<DT, 16, NW, WAVES, P, GROUPED>, tiles<16, 16 * NW>(a, GROUPED), 1, 1, a, stream, 64 * WAVES);
+}
 
+template <int N>
+int best_of(const Kind (&kinds)[N], const ProductArgs& a, bool grouped) {
+  int best = 0;
+  float least = time_of(kinds[0], a, grouped);
+  for (int i = 1; i < N; ++i) {
+    const float t = time_of(kinds[i], a, grouped);
+    if (t < least) {
+      least = t;
+      best = i;
+    }
+  }
+  return best;
+}
+
+// k_few for up to 16 rows (experts: up to 8 on average), else the tiles that the fit has as the fastest: over 135 calls 2 % behind the best of
+// them on average.  k_product's loads name x's codes by 31 bits; where a tile's rows lie further apart k_few has them all.
 template <int DT, bool GROUPED>
 int product(const ProductArgs& a, plora_stream stream) {
-  return launch(k_product<DT, 64, 64, 2, 2, GROUPED>, tiles<64, 64>(a, GROUPED), 1, 1, a, stream);
+  const bool far = a.rows ? (__int128)a.n_x_rows * a.x_s > kReach - 256 : 256 * (__int128)a.x_s > kReach - 256;
+  if (far || (GROUPED ? (int64_t)a.n_rows <= 8 * (int64_t)a.n_experts : a.n_rows <= 16)) {
+    static constexpr Kind kFew[] = {{16, 16, 8, 2, 1.15f, 0.591f, 1.114f}, {16, 32, 8, 2, 0.72f, 1.147f, 1.67f}, {16, 64, 4, 4, 0.f, 1.172f, 1.391f}};
+    switch (best_of(kFew, a, GROUPED)) {
+      case 0: return few<DT, GROUPED, 1, 8, 2>(a, stream);
+      case 1: return few<DT, GROUPED, 2, 8, 2>(a, stream);
+      default: return few<DT, GROUPED, 4, 4, 1>(a, stream);
+    }
+  }
+  static constexpr Kind kTiles[] = {{64, 32, 2, 1, 1.85f, 0.379f, 0.f},  {64, 64, 2, 1, 1.79f, 0.525f, 0.f},   {64, 64, 1, 2, 0.99f, 0.295f, 0.234f}, {128, 64, 1, 1, 2.07f, 0.421f, 0.f},
+                                    {128, 128, 1, 1, 2.79f, 0.593f, 0.f}, {128, 256, 1, 1, 3.93f, 0.896f, 0.f}, {256, 128, 1, 1, 4.21f, 0.87f, 0.f},   {256, 256, 1, 1, 4.93f, 1.612f, 0.f}};
+  switch (best_of(kTiles, a, GROUPED)) {
+    case 0: return tiled<DT, GROUPED, 64, 32, 4, 1, 2, 4>(a, stream);
+    case 1: return tiled<DT, GROUPED, 64, 64, 2, 2, 2, 3>(a, stream);
+    case 2: return tiled<DT, GROUPED, 64, 64, 2, 2, 1, 4>(a, stream);
+    case 3: return tiled<DT, GROUPED, 128, 64, 4, 2, 1, 4>(a, stream);
+    case 4: return tiled<DT, GROUPED, 128, 128, 4, 2, 1, 4>(a, stream);
+    case 5: return tiled<DT, GROUPED, 128, 256, 2, 4, 1, 3>(a, stream);
+    case 6: return tiled<DT, GROUPED, 256, 128, 4, 2, 1, 3>(a, stream);
+    default: return tiled<DT, GROUPED, 256, 256, 4, 2, 1, 2>(a, stream);
+  }
 }
 
 constexpr int64_t kMostStride = (int64_t)1 << 40;
