@@ -573,7 +573,7 @@ int plora_fp8_grouped(const plora_fp8_rows* x, int32_t n_x_rows, const plora_fp8
  * Behind the choice the chosen (token, j) are sorted by expert, then by token: offsets[n_experts + 1] is where each expert's rows start
  * and end, rows[n_tokens * top_k] the token of every sorted row (-1 behind the last one), places[t, j] where (t, j) went.
  * All outputs: device, int32 (weights: float), contiguous.  workspace: device, 16-byte aligned, at least
- * plora_route_workspace_bytes (0 up to 64 tokens); its contents do not matter; calls that may overlap need one each. */
+ * plora_route_workspace_bytes (0 up to 64 tokens and 512 experts); its contents do not matter; calls that may overlap need one each. */
 uint64_t plora_route_workspace_bytes(int32_t n_tokens, int32_t n_experts);
 int plora_route(int32_t dtype, int32_t n_tokens, int32_t n_experts, int32_t top_k, const plora_matrix* logits, int32_t renormalise, float scale,
                 int32_t* experts, float* weights, int32_t* offsets, int32_t* rows, int32_t* places, void* workspace, uint64_t workspace_bytes,
@@ -591,8 +591,8 @@ typedef struct {
 /* What lies between two blocks of a layer:
  *   u = block[t],  or with places  sum over j < top_k of place_weights[t, j] * block[places[t, j]]   (the experts' rows of the token)
  *   hidden = residual + scale * gate * post(u),      y = pre(hidden)
- * in 32 bits, each result rounded once: y comes from hidden as it is ahead of its rounding.  Parts that are NULL are left out: residual (0), gate (1), post and
- * pre (the value itself), hidden and out (not written).  y goes to out (rows of dtype) or out8 (8 bits), not both; at least one of hidden, out, out8.
+ * in 32 bits, each result rounded once: y comes from hidden as it is ahead of its rounding.  Parts that are NULL (matrices: their data) are left out: residual (0), gate (1),
+ * post and pre (the value itself), hidden and out (not written).  y goes to out (rows of dtype) or out8 (8 bits), not both; at least one of hidden, out, out8.
  * Squares are summed in 32 bits.  Entries of places outside [0, n_block_rows) add nothing, whatever their weight.
  * hidden and out may each be block (without places), residual or gate (same data and stride, a gate or residual of one row for all apart);
  * otherwise outputs overlap nothing. */
@@ -601,18 +601,14 @@ typedef struct {
   int32_t n_tokens;
   int32_t dim;      /* a multiple of 8, up to 16384 */
   float scale;      /* finite */
-  const plora_matrix* block;
+  plora_matrix block;
   const int32_t* places;      /* device, n_tokens x top_k entries, or NULL */
   const float* place_weights; /* device, as places */
   int32_t top_k;              /* with places: 1 .. 32 */
   int32_t n_block_rows;       /* with places: rows of block, >= 0 */
-  const plora_norm_weights* post;
-  const plora_matrix* gate;
-  const plora_matrix* residual;
-  const plora_matrix* hidden;
-  const plora_norm_weights* pre;
-  const plora_matrix* out;
-  const plora_fp8_rows* out8;
+  const plora_norm_weights *post, *pre; /* host */
+  plora_matrix gate, residual, hidden, out;
+  plora_fp8_rows out8;
 } plora_block_norm;
 int plora_norm(const plora_block_norm* args, plora_stream stream);
 

@@ -905,13 +905,15 @@ class NormWeightsStruct(C.Structure):
     _fields_ = [("weight", _vp), ("bias", _vp), ("eps", _f32), ("offset", _f32), ("center", _i32)]
 
 
-_matrix_p, _fp8_rows_p, _fp8_weights_p, _norm_p = (C.POINTER(t) for t in (MatrixStruct, Fp8RowsStruct, Fp8WeightsStruct, NormWeightsStruct))
+_matrix_p, _fp8_rows_p, _fp8_weights_p = (C.POINTER(t) for t in (MatrixStruct, Fp8RowsStruct, Fp8WeightsStruct))
 
 
 class BlockNormStruct(C.Structure):
-    _fields_ = [("dtype", _i32), ("n_tokens", _i32), ("dim", _i32), ("scale", _f32), ("block", _matrix_p), ("places", _vp), ("place_weights", _vp),
-                ("top_k", _i32), ("n_block_rows", _i32), ("post", _norm_p), ("gate", _matrix_p), ("residual", _matrix_p), ("hidden", _matrix_p),
-                ("pre", _norm_p), ("out", _matrix_p), ("out8", _fp8_rows_p)]
+    """plora_block_norm; its matrices' fields one by one."""
+    _fields_ = [("dtype", _i32), ("n_tokens", _i32), ("dim", _i32), ("scale", _f32), ("block", _vp), ("block_stride", C.c_int64), ("places", _vp),
+                ("place_weights", _vp), ("top_k", _i32), ("n_block_rows", _i32), ("post", _vp), ("pre", _vp)] + [
+                    f for m in ("gate", "residual", "hidden", "out") for f in ((m, _vp), (m + "_stride", C.c_int64))] + [
+                        ("codes", _vp), ("scales", _vp), ("code_stride", C.c_int64), ("scale_stride", C.c_int64)]
 
 
 lib.plora_norm.argtypes = [C.POINTER(BlockNormStruct), _vp]
@@ -1110,6 +1112,7 @@ class NormWeights:
                     t.get_device() != self.kept[0].get_device():
                 raise PloraError(call, PLORA_ERR_INVAL)
         self.c = NormWeightsStruct(None if weight is None else weight.data_ptr(), None if bias is None else bias.data_ptr(), eps, offset, int(center))
+        self.at = C.addressof(self.c)
 
     def fits(self, dim, dtype, device):
         return not self.kept or (self.kept[0].numel() == dim and _dtype_of(self.kept[0]) == dtype and self.kept[0].get_device() == device)
@@ -1144,15 +1147,22 @@ class BlockNorm:
         if out8 is not None and (out8.device != device or out8.n != n or out8.k != dim):
             raise PloraError(call, PLORA_ERR_INVAL)
 
-        def of(t, rows=n):
-            return None if t is None else C.pointer(_matrix_of(call, t, rows, dim, dtype, device))
-
         if gate is not None and gate.dim() == 1:
             gate = gate.expand(n, dim)
-        args = BlockNormStruct(dtype, n, dim, self.scale, of(block, block_rows), None if places is None else _ints_of(call, places, n * top_k, device),
+        parts = []
+        for t, rows in ((block, block_rows), (gate, n), (residual, n), (hidden, n), (out, n)):
+            if t is None:
+                parts += (None, 0)
+                continue
+            st = t.stride()
+            if t.shape != (rows, dim) or st[1] != 1 or _dtype_of(t) != dtype or t.get_device() != device:
+                raise PloraError(call, PLORA_ERR_INVAL)
+            parts += (t.data_ptr(), st[0])
+        e = None if out8 is None else out8.c
+        args = BlockNormStruct(dtype, n, dim, self.scale, parts[0], parts[1], None if places is None else _ints_of(call, places, n * top_k, device),
                                None if places is None else place_weights.data_ptr(), top_k, block_rows if places is not None else 0,
-                               None if self.post is None else C.pointer(self.post.c), of(gate), of(residual), of(hidden),
-                               None if self.pre is None else C.pointer(self.pre.c), of(out), None if out8 is None else C.pointer(out8.c))
+                               None if self.post is None else self.post.at, None if self.pre is None else self.pre.at, *parts[2:],
+                               *((None, None, 0, 0) if e is None else (e.codes, e.scales, e.code_stride, e.scale_stride)))
         rc = lib.plora_norm(args, stream)
         if rc:
             _check(call, rc)

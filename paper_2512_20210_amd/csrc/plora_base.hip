@@ -47,12 +47,6 @@ __device__ __forceinline__ float sum64(float v) {
   v += __shfl_xor(v, 16);
   return v + __shfl_xor(v, 32);
 }
-__device__ __forceinline__ float max64(float v) {
-#pragma unroll
-  for (int i = 1; i < 64; i *= 2) v = fmaxf(v, __shfl_xor(v, i));
-  return v;
-}
-
 // Scale and its inverse of a block whose largest |x| has the bits `amax` (as whole numbers the magnitudes order like the values,
 // infinities and NaN above all of them).
 __device__ __forceinline__ void block_scale(uint32_t amax, float& scale, float& inverse) {
@@ -384,20 +378,22 @@ __global__ __launch_bounds__(kThreads) void k_quantise_weights(WeightArgs a) {
 }
 
 // ---- routing ------------------------------------------------------------------------------------------
-// A counting sort by expert over chunks of 64 tokens.  In a chunk a token is a bit of each expert's word: counts are sums of bits and a
+// A counting sort by expert: the choosing workgroups count their 16 tokens, the sorting ones have 64 (up to 64 tokens: one workgroup does both).
+// In a chunk a token is a bit of each expert's words: counts are sums of bits and a
 // (token, expert)'s rank is the number of bits below its own, so atomics only set bits and no order of theirs shows.
 
-constexpr int kChunk = 64, kRouteThreads = 1024, kMostExperts = 1024, kMostChoices = 32;
-constexpr int kFewChunks = 64;  // up to here the last kernel sums the chunks' counts itself
+constexpr int kChunk = 64, kCounted = 16, kRouteThreads = 1024, kMostExperts = 1024, kMostChoices = 32;
+constexpr int kOneExperts = 512;  // above, a chunk's logits do not fit the registers of one workgroup of 64 tokens
+constexpr int kFewCounts = 64;  // up to here the last kernel sums an expert's counts itself
 
 struct RouteArgs {
   const uint8_t* logits;
   int64_t stride;  // elements
   int32_t *experts, *offsets, *rows, *places;
   float* weights;
-  int32_t *counts, *totals;  // counts [expert][chunk]; where there are many chunks: sums of the chunks ahead, and of all
+  int32_t *counts, *totals;  // counts [expert][16 tokens]; where there are many: sums of those ahead, and of all
   float scale;
-  int32_t n_tokens, n_experts, top_k, renormalise, n_chunks;
+  int32_t n_tokens, n_experts, top_k, renormalise, n_counts;
 };
 
 __device__ __forceinline__ int bits_below(const uint32_t* w, int t) {
@@ -423,7 +419,7 @@ __device__ __forceinline__ int scan1024(int v, int* waves, int& total) {
   }
   return ahead + s - v;
 }
-// The sorted places of a chunk whose experts start at base[]: rows and places, and the chunk's share of the rows behind the last one.
+// The sorted places of a chunk of 64 tokens whose experts start at base[]: rows and places, and the chunk's share of the rows behind the last one.
 __device__ __forceinline__ void place_chunk(const RouteArgs& a, int chunk, const int16_t* chosen, const uint32_t (*bits)[2], const int* base, int total) {
   const int64_t first = (int64_t)chunk * kChunk * a.top_k, all = (int64_t)a.n_tokens * a.top_k;
   for (int i = threadIdx.x; i < kChunk * a.top_k && first + i < all; i += kRouteThreads) {
@@ -435,107 +431,126 @@ __device__ __forceinline__ void place_chunk(const RouteArgs& a, int chunk, const
   }
 }
 
-// One wavefront a token; lane l has the logits of experts l, l + 64, ...  ONE: the call has one chunk, and this kernel sorts it too.
-template <int DT, int R, bool ONE>
-__global__ __launch_bounds__(kRouteThreads) void k_route_choose(RouteArgs a) {
-  constexpr int kTok = kChunk / (kRouteThreads / 64);
-  __shared__ uint32_t bits[64 * R][2];
-  __shared__ int16_t chosen[kChunk * kMostChoices];
-  __shared__ int base[ONE ? 64 * R : 1], waves[kRouteThreads / 64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), chunk = blockIdx.x;
-  float v[kTok][R];
+// Logits as whole numbers in the same order (0 and -0 alike); -inf and NaN are kNone, below all others.
+constexpr int kNone = INT32_MIN;
+__device__ __forceinline__ int ordered(float v) {
+  const int b = __float_as_int(v + 0.f);
+  return v > -INFINITY ? b ^ ((b >> 31) & 0x7fffffff) : kNone;
+}
+__device__ __forceinline__ float value_of(int key) { return __int_as_float(key ^ ((key >> 31) & 0x7fffffff)); }
+template <int CTRL>
+__device__ __forceinline__ int dpp_max(int v) {
+  const int o = __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false);
+  return v > o ? v : o;
+}
+__device__ __forceinline__ int row_max(int v) { return dpp_max<0x121>(dpp_max<0x122>(dpp_max<0x124>(dpp_max<0x128>(v)))); }
+
+// A wavefront has four tokens, 16 lanes each; a lane has the logits of experts c, c + 16, ... of its token.  The number of vector instructions of a
+// choice bounds it, and here four tokens share them (16k tokens, 8 of 256 experts: 19 us with a wavefront a token, 14 so).  THREADS =
+// 1024: the call's one chunk of 64 tokens, which is sorted as well; 256: 16 tokens and their counts.
+template <int DT, int V, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_route_choose(RouteArgs a) {
+  constexpr int TOK = THREADS / 16, WORDS = (TOK + 31) / 32;
+  constexpr bool ONE = TOK == kChunk;
+  static_assert(ONE || TOK == kCounted, "one chunk, or as many tokens as are counted together");
+  __shared__ uint32_t bits[16 * V][WORDS];
+  __shared__ int16_t chosen[ONE ? TOK * kMostChoices : 1];
+  __shared__ int base[ONE ? 16 * V : 1], waves[ONE ? THREADS / 64 : 1];
+  const int col = threadIdx.x & 15, slot = threadIdx.x >> 4;
+  const int64_t t = (int64_t)blockIdx.x * TOK + slot;
+  const bool live = t < a.n_tokens;
+  int key[V];
+  bool nan = false;
+  {
+    float v[V];
 #pragma unroll
-  for (int q = 0; q < kTok; ++q) {
-    const int64_t t = (int64_t)chunk * kChunk + wave * kTok + q;
+    for (int i = 0; i < V; ++i) {
+      const int e = col + 16 * i;
+      v[i] = live && e < a.n_experts ? ld1<DT>(a.logits, t * a.stride + e) : -INFINITY;
+    }
+    for (int i = threadIdx.x; i < 16 * V * WORDS; i += THREADS) (&bits[0][0])[i] = 0;
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const int e = lane + 64 * i;
-      v[q][i] = t < a.n_tokens && e < a.n_experts ? ld1<DT>(a.logits, t * a.stride + e) : -INFINITY;
+    for (int i = 0; i < V; ++i) {
+      nan |= v[i] != v[i];
+      key[i] = ordered(v[i]);
     }
   }
-  for (int i = threadIdx.x; i < 64 * R; i += kRouteThreads) bits[i][0] = bits[i][1] = 0;
-  __syncthreads();
+  const auto most = [&]() {
+    int m = key[0];
 #pragma unroll
-  for (int q = 0; q < kTok; ++q) {
-    const int slot = wave * kTok + q;
-    const int64_t t = (int64_t)chunk * kChunk + slot;
-    if (t >= a.n_tokens) break;
-    bool bad = false;
-    float top = -INFINITY;
+    for (int i = 1; i < V; ++i) m = key[i] > m ? key[i] : m;
+    return row_max(m);
+  };
+  int m = most();
+  const int top = m;
+  const bool bad = row_max(nan ? 1 : 0) > 0 || value_of(top) == INFINITY;
+  float sum = 0.f;
+  if (!a.renormalise) {
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      if (v[q][i] != v[q][i]) {
-        bad = true;
-        v[q][i] = -INFINITY;
+    for (int i = 0; i < V; ++i) sum += key[i] == kNone ? 0.f : expf(value_of(key[i]) - value_of(top));
+    sum = sum16(sum);
+  }
+  int expert[2] = {-1, -1}, mine[2] = {kNone, kNone};  // lane c: choices c and c + 16 and their logits
+  for (int j = 0; j < a.top_k; ++j) {
+    int at = 16 * V;  // the lowest expert with the largest logit
+#pragma unroll
+    for (int i = V - 1; i >= 0; --i) at = key[i] == m ? col + 16 * i : at;
+    at = -row_max(-at);
+    if (m == kNone) at = -1;
+    if (col == (j & 15)) {
+      if (j < 16) {
+        expert[0] = at;
+        mine[0] = m;
+      } else {
+        expert[1] = at;
+        mine[1] = m;
       }
-      top = fmaxf(top, v[q][i]);
     }
-    float sum = 0.f;
-    top = max64(top);
-    bad = __ballot(bad) != 0 || top == INFINITY;
-    if (!a.renormalise) {
+    const int own = (at & 15) == col ? at >> 4 : -1;  // (-1 >> 4: none)
 #pragma unroll
-      for (int i = 0; i < R; ++i) sum += v[q][i] == -INFINITY ? 0.f : expf(v[q][i] - top);
-      sum = sum64(sum);
-    }
-    int expert = -1;  // lane j: the j-th choice
-    float p = 0.f, m = top;
-    for (int j = 0; j < a.top_k && m > -INFINITY; ++j) {
-      int at = -1, l = 0;
+    for (int i = 0; i < V; ++i) key[i] = own == i ? kNone : key[i];
+    m = most();
+  }
+  float p[2];
 #pragma unroll
-      for (int i = R - 1; i >= 0; --i) {
-        const uint64_t same = __ballot(v[q][i] == m);
-        if (same) {
-          at = i;
-          l = __builtin_ctzll(same);
-        }
-      }
-      if (lane == j) {
-        expert = 64 * at + l;
-        p = expf(m - top);
-      }
-      float next = -INFINITY;
+  for (int h = 0; h < 2; ++h) p[h] = mine[h] == kNone ? 0.f : expf(value_of(mine[h]) - value_of(top));
+  if (a.renormalise) sum = sum16(p[0] + p[1]);
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        if (i == at && lane == l) v[q][i] = -INFINITY;
-        next = fmaxf(next, v[q][i]);
-      }
-      if (j + 1 < a.top_k) m = max64(next);
-    }
-    if (a.renormalise) sum = sum64(p);
-    if (lane < a.top_k) {
-      const int64_t o = t * a.top_k + lane;
-      a.experts[o] = expert;
-      a.weights[o] = bad ? quiet_nan() : expert < 0 ? 0.f : a.scale * (p / sum);
-      chosen[slot * a.top_k + lane] = (int16_t)expert;
-      if (expert >= 0) atomicOr(&bits[expert][slot >> 5], 1u << (slot & 31));
+  for (int h = 0; h < 2; ++h) {
+    const int j = col + 16 * h;
+    if (j < a.top_k && live) {
+      const int64_t o = t * a.top_k + j;
+      a.experts[o] = expert[h];
+      a.weights[o] = bad ? quiet_nan() : expert[h] < 0 ? 0.f : a.scale * (p[h] / sum);
+      if constexpr (ONE) chosen[slot * a.top_k + j] = (int16_t)expert[h];
+      if (expert[h] >= 0) atomicOr(&bits[expert[h]][slot >> 5], 1u << (slot & 31));
     }
   }
   __syncthreads();
-  const int e = threadIdx.x;
-  const int n = e < 64 * R ? __popc(bits[e][0]) + __popc(bits[e][1]) : 0;
   if constexpr (!ONE) {
-    if (e < a.n_experts) a.counts[(int64_t)e * a.n_chunks + chunk] = n;
+    for (int e = threadIdx.x; e < a.n_experts; e += THREADS) a.counts[(int64_t)e * a.n_counts + blockIdx.x] = __popc(bits[e][0]);
   } else {
+    const int e = threadIdx.x;
     int total;
-    const int ahead = scan1024(n, waves, total);
-    if (e < 64 * R) base[e] = ahead;
+    const int ahead = scan1024(e < 16 * V ? __popc(bits[e][0]) + __popc(bits[e][1]) : 0, waves, total);
+    if (e < 16 * V) base[e] = ahead;
     if (e < a.n_experts) a.offsets[e] = ahead;
     if (e == 0) a.offsets[a.n_experts] = total;
     __syncthreads();
-    place_chunk(a, chunk, chosen, bits, base, total);
+    place_chunk(a, 0, chosen, bits, base, total);
   }
 }
 
-// An expert's counts become sums of the chunks ahead; 256 threads, each with a run of neighbours.
+// An expert's counts become sums of those ahead; 256 threads, each with a run of neighbours.
 __global__ __launch_bounds__(kThreads) void k_route_scan(RouteArgs a) {
   __shared__ int waves[kThreads / 64];
-  int32_t* c = a.counts + (int64_t)blockIdx.x * a.n_chunks;
+  int32_t* c = a.counts + (int64_t)blockIdx.x * a.n_counts;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int64_t before = 0;
-  for (int at = 0; at < a.n_chunks; at += kThreads) {
+  for (int at = 0; at < a.n_counts; at += kThreads) {
     const int i = at + threadIdx.x;
-    const int v = i < a.n_chunks ? c[i] : 0;
+    const int v = i < a.n_counts ? c[i] : 0;
     int s = v;
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) {
@@ -550,7 +565,7 @@ __global__ __launch_bounds__(kThreads) void k_route_scan(RouteArgs a) {
       if (w < wave) s += waves[w];
       all += waves[w];
     }
-    if (i < a.n_chunks) c[i] = (int)before + s - v;
+    if (i < a.n_counts) c[i] = (int)before + s - v;
     before += all;
     __syncthreads();
   }
@@ -570,9 +585,10 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_place(RouteArgs a) {
     chosen[i] = (int16_t)e;
     if (e >= 0) atomicOr(&bits[e][t >> 5], 1u << (t & 31));
   }
-  if (a.n_chunks <= kFewChunks) {  // a wavefront an expert, a lane a chunk
+  constexpr int kCounts = kChunk / kCounted;
+  if (a.n_counts <= kFewCounts) {  // a wavefront an expert, a lane a count
     for (int e = wave; e < a.n_experts; e += kRouteThreads / 64) {
-      int n = lane < a.n_chunks ? a.counts[(int64_t)e * a.n_chunks + lane] : 0, ahead = lane < chunk ? n : 0;
+      int n = lane < a.n_counts ? a.counts[(int64_t)e * a.n_counts + lane] : 0, ahead = lane < chunk * kCounts ? n : 0;
 #pragma unroll
       for (int i = 1; i < 64; i *= 2) {
         n += __shfl_xor(n, i);
@@ -584,7 +600,7 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_place(RouteArgs a) {
       }
     }
   } else if (threadIdx.x < a.n_experts) {
-    base[threadIdx.x] = a.counts[(int64_t)threadIdx.x * a.n_chunks + chunk];
+    base[threadIdx.x] = a.counts[(int64_t)threadIdx.x * a.n_counts + chunk * kCounts];
     total_of[threadIdx.x] = a.totals[threadIdx.x];
   }
   __syncthreads();
@@ -600,20 +616,21 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_place(RouteArgs a) {
   place_chunk(a, chunk, chosen, bits, base, total);
 }
 
-template <int DT, int R>
+template <int DT, int V>
 int route(const RouteArgs& a, plora_stream stream) {
-  if (a.n_chunks <= 1) return launch(k_route_choose<DT, R, true>, 1, 1, 1, a, stream, kRouteThreads);
-  int rc = launch(k_route_choose<DT, R, false>, a.n_chunks, 1, 1, a, stream, kRouteThreads);
-  if (!rc && a.n_chunks > kFewChunks) rc = launch(k_route_scan, a.n_experts, 1, 1, a, stream);
-  return rc ? rc : launch(k_route_place, a.n_chunks, 1, 1, a, stream, kRouteThreads);
+  if constexpr (V <= 32)
+    if (a.n_tokens <= kChunk) return launch(k_route_choose<DT, V, kRouteThreads>, 1, 1, 1, a, stream, kRouteThreads);
+  int rc = launch(k_route_choose<DT, V, kThreads>, a.n_counts, 1, 1, a, stream);
+  if (!rc && a.n_counts > kFewCounts) rc = launch(k_route_scan, a.n_experts, 1, 1, a, stream);
+  return rc ? rc : launch(k_route_place, ((uint64_t)a.n_tokens + kChunk - 1) / kChunk, 1, 1, a, stream, kRouteThreads);
 }
 template <int DT>
 int route(const RouteArgs& a, plora_stream stream) {
-  return a.n_experts <= 64    ? route<DT, 1>(a, stream)
-         : a.n_experts <= 128 ? route<DT, 2>(a, stream)
-         : a.n_experts <= 256 ? route<DT, 4>(a, stream)
-         : a.n_experts <= 512 ? route<DT, 8>(a, stream)
-                              : route<DT, 16>(a, stream);
+  return a.n_experts <= 64 || a.n_tokens == 0 ? route<DT, 4>(a, stream)
+         : a.n_experts <= 128 ? route<DT, 8>(a, stream)
+         : a.n_experts <= 256 ? route<DT, 16>(a, stream)
+         : a.n_experts <= 512 ? route<DT, 32>(a, stream)
+                              : route<DT, 64>(a, stream);
 }
 
 // ---- checks -------------------------------------------------------------------------------------------
@@ -643,27 +660,31 @@ bool apart(const plora_matrix* out, const plora_matrix* in, bool may_be) {
 
 extern "C" int plora_norm(const plora_block_norm* n, plora_stream stream) {
   if (!n || !good_dtype(n->dtype) || n->n_tokens < 0 || n->dim < 8 || n->dim > 16384 || n->dim % 8 || !isfinite(n->scale)) return PLORA_ERR_INVAL;
-  if ((n->post && !good_norm(n->post)) || (n->pre && !good_norm(n->pre)) || (!n->hidden && !n->out && !n->out8) || (n->out && n->out8)) return PLORA_ERR_INVAL;
+  const auto there = [](const plora_matrix& m) { return m.data ? &m : nullptr; };
+  const plora_matrix *block = there(n->block), *gate = there(n->gate), *residual = there(n->residual), *hidden = there(n->hidden), *out = there(n->out);
+  const plora_fp8_rows* out8 = n->out8.codes ? &n->out8 : nullptr;
+  if ((n->post && !good_norm(n->post)) || (n->pre && !good_norm(n->pre))) return PLORA_ERR_INVAL;
   if (!n->places != !n->place_weights || (n->places && (n->top_k < 1 || n->top_k > 32 || n->n_block_rows < 0))) return PLORA_ERR_INVAL;
   if (n->n_tokens == 0) return PLORA_OK;
+  if ((!hidden && !out && !out8) || (out && out8)) return PLORA_ERR_INVAL;
   const int dt = n->dtype;
   const int64_t rows = n->n_tokens, dim = n->dim;
-  if (!(n->places && n->n_block_rows == 0) && !good_matrix(n->block, dt)) return PLORA_ERR_INVAL;
-  if ((n->gate && !good_matrix(n->gate, dt)) || (n->residual && !good_matrix(n->residual, dt)) || (n->hidden && !good_rows_out(n->hidden, dt, rows, dim)) ||
-      (n->out && !good_rows_out(n->out, dt, rows, dim)) || (n->out8 && !good_eight(n->out8, rows, dim)))
+  if (!(n->places && n->n_block_rows == 0) && !good_matrix(block, dt)) return PLORA_ERR_INVAL;
+  if ((gate && !good_matrix(gate, dt)) || (residual && !good_matrix(residual, dt)) || (hidden && !good_rows_out(hidden, dt, rows, dim)) ||
+      (out && !good_rows_out(out, dt, rows, dim)) || (out8 && !good_eight(out8, rows, dim)))
     return PLORA_ERR_INVAL;
-  for (const plora_matrix* o : {n->hidden, n->out})
-    if (!apart(o, n->block, !n->places) || !apart(o, n->gate, true) || !apart(o, n->residual, true)) return PLORA_ERR_INVAL;
-  if (n->hidden && n->out && n->hidden->data == n->out->data) return PLORA_ERR_INVAL;
+  for (const plora_matrix* o : {hidden, out})
+    if (!apart(o, block, !n->places) || !apart(o, gate, true) || !apart(o, residual, true)) return PLORA_ERR_INVAL;
+  if (hidden && out && hidden->data == out->data) return PLORA_ERR_INVAL;
   NormArgs a = {};
   const int elt = elt_bytes(dt);
-  a.block = n->block ? (const uint8_t*)n->block->data : nullptr;
-  a.block_s = n->block ? n->block->stride * elt : 0;
-  if (n->gate) a.gate = (const uint8_t*)n->gate->data, a.gate_s = n->gate->stride * elt;
-  if (n->residual) a.residual = (const uint8_t*)n->residual->data, a.residual_s = n->residual->stride * elt;
-  if (n->hidden) a.hidden = (uint8_t*)n->hidden->data, a.hidden_s = n->hidden->stride * elt;
-  if (n->out) a.out = (uint8_t*)n->out->data, a.out_s = n->out->stride * elt;
-  if (n->out8) a.codes = (uint8_t*)n->out8->codes, a.codes_s = n->out8->code_stride, a.scales = n->out8->scales, a.scales_s = n->out8->scale_stride;
+  a.block = block ? (const uint8_t*)block->data : nullptr;
+  a.block_s = block ? block->stride * elt : 0;
+  if (gate) a.gate = (const uint8_t*)gate->data, a.gate_s = gate->stride * elt;
+  if (residual) a.residual = (const uint8_t*)residual->data, a.residual_s = residual->stride * elt;
+  if (hidden) a.hidden = (uint8_t*)hidden->data, a.hidden_s = hidden->stride * elt;
+  if (out) a.out = (uint8_t*)out->data, a.out_s = out->stride * elt;
+  if (out8) a.codes = (uint8_t*)out8->codes, a.codes_s = out8->code_stride, a.scales = out8->scales, a.scales_s = out8->scale_stride;
   a.places = n->places;
   a.place_weights = n->place_weights;
   a.top_k = n->top_k;
@@ -703,9 +724,8 @@ extern "C" int plora_fp8_quantise_weights(int32_t dtype, const plora_matrix* w, 
 }
 
 extern "C" uint64_t plora_route_workspace_bytes(int32_t n_tokens, int32_t n_experts) {
-  if (n_tokens <= kChunk || n_experts < 1 || n_experts > kMostExperts) return 0;
-  const uint64_t chunks = ((uint64_t)n_tokens + kChunk - 1) / kChunk;
-  return (uint64_t)n_experts * (chunks + 1) * 4;
+  if (n_tokens <= (n_experts <= kOneExperts ? kChunk : 0) || n_experts < 1 || n_experts > kMostExperts) return 0;
+  return (uint64_t)n_experts * (((uint64_t)n_tokens + kCounted - 1) / kCounted + 1) * 4;
 }
 
 extern "C" int plora_route(int32_t dtype, int32_t n_tokens, int32_t n_experts, int32_t top_k, const plora_matrix* logits, int32_t renormalise, float scale,
@@ -732,8 +752,8 @@ extern "C" int plora_route(int32_t dtype, int32_t n_tokens, int32_t n_experts, i
   a.n_experts = n_experts;
   a.top_k = top_k;
   a.renormalise = renormalise != 0;
-  a.n_chunks = (int32_t)(((int64_t)n_tokens + kChunk - 1) / kChunk);
+  a.n_counts = (int32_t)(((int64_t)n_tokens + kCounted - 1) / kCounted);
   a.counts = (int32_t*)workspace;
-  a.totals = a.counts ? a.counts + (int64_t)n_experts * a.n_chunks : nullptr;
+  a.totals = a.counts ? a.counts + (int64_t)n_experts * a.n_counts : nullptr;
   return dtype == PLORA_BF16 ? route<PLORA_BF16>(a, stream) : dtype == PLORA_F16 ? route<PLORA_F16>(a, stream) : route<PLORA_F32>(a, stream);
 }

@@ -28,12 +28,24 @@ def norm_of(weight=AT, bias=None, eps=1e-6, offset=0.0, center=0):
 
 
 def block(**kw):
-    a = dict(dtype=P.PLORA_BF16, n_tokens=3, dim=256, scale=1.0, block=matrix(), places=None, place_weights=None, top_k=0, n_block_rows=0, post=None, gate=None,
-             residual=None, hidden=None, pre=norm_of(), out=matrix(FAR), out8=None)
+    a = dict(dtype=P.PLORA_BF16, n_tokens=3, dim=256, scale=1.0, block=matrix(), places=None, place_weights=None, top_k=0, n_block_rows=0, post=None, pre=norm_of(),
+             gate=None, residual=None, hidden=None, out=matrix(FAR), out8=None)
     a.update(kw)
-    return P.BlockNormStruct(*(C.pointer(v) if isinstance(v, C.Structure) else v for v in a.values()))
+    flat = []
+    for name, v in a.items():
+        if name in ("post", "pre"):
+            flat.append(None if v is None else C.addressof(v))
+            kept.append(v)
+        elif name == "out8":
+            flat += [None, None, 0, 0] if v is None else [getattr(v, f) for f, _ in v._fields_]
+        elif name in ("block", "gate", "residual", "hidden", "out"):
+            flat += [None, 0] if v is None else [v.data, v.stride]
+        else:
+            flat.append(v)
+    return P.BlockNormStruct(*flat)
 
 
+kept = []  # what the records point to
 BAD_MATRIX = [matrix(None), matrix(AT + 8), matrix(stride=-256), matrix(stride=257), matrix(stride=1 << 41)]
 BAD_OUT = BAD_MATRIX + [matrix(stride=0), matrix(stride=248)]
 BAD_EIGHT = [rows8(None), rows8(AT + 8), rows8(scales=None), rows8(scales=FAR + 2), rows8(stride=252), rows8(stride=248), rows8(stride=-256), rows8(scale_stride=2),
@@ -61,9 +73,12 @@ def test_norms(kw):
 
 def test_norm_matrices():
     for m in BAD_MATRIX:
-        assert P.plora_norm(block(block=m)) == P.plora_norm(block(gate=m)) == P.plora_norm(block(residual=m)) == INVAL
+        assert P.plora_norm(block(block=m)) == INVAL
+        if m.data:  # (none is no gate)
+            assert P.plora_norm(block(gate=m)) == P.plora_norm(block(residual=m)) == INVAL
     for m in BAD_OUT:
-        assert P.plora_norm(block(out=m)) == P.plora_norm(block(hidden=m)) == INVAL
+        assert P.plora_norm(block(out=m)) == INVAL
+        assert not m.data or P.plora_norm(block(hidden=m)) == INVAL
     for r in BAD_EIGHT:
         assert P.plora_norm(block(out=None, out8=r)) == INVAL
     assert P.lib.plora_norm(None, None) == INVAL
@@ -105,14 +120,14 @@ def test_routing():
     for kw in [dict(dtype=4), dict(n_tokens=-1), dict(n_experts=0), dict(n_experts=1025), dict(top_k=0), dict(top_k=9), dict(n_experts=64, top_k=33), dict(logits=None),
                dict(logits=matrix(None)), dict(logits=matrix(AT + 2)), dict(logits=matrix(stride=-1)), dict(logits=matrix(stride=1 << 41)), dict(scale=float("nan")),
                dict(scale=float("inf")), dict(experts_ptr=None), dict(weights_ptr=None), dict(offsets_ptr=None), dict(rows_ptr=None), dict(places_ptr=None),
-               dict(workspace_ptr=AT + 8), dict(workspace_ptr=None), dict(n_tokens=65, workspace_bytes=8 * 3 * 4 - 1)]:
+               dict(workspace_ptr=AT + 8), dict(workspace_ptr=None), dict(n_tokens=65, workspace_bytes=8 * 6 * 4 - 1)]:
         assert P.plora_route(**{**good, **kw}) == INVAL
     assert P.plora_route(**{**good, "n_tokens": 1 << 30, "workspace_bytes": 1 << 40}) == LIMIT
 
 
 def test_workspace_of_routing():
-    assert P.plora_route_workspace_bytes(64, 8) == 0 and P.plora_route_workspace_bytes(65, 8) == 8 * 3 * 4
-    assert P.plora_route_workspace_bytes(65, 0) == P.plora_route_workspace_bytes(65, 1025) == P.plora_route_workspace_bytes(-5, 8) == 0
+    assert P.plora_route_workspace_bytes(64, 512) == P.plora_route_workspace_bytes(0, 1024) == 0 and P.plora_route_workspace_bytes(1, 513) == 513 * 2 * 4 and P.plora_route_workspace_bytes(65, 8) == 8 * 6 * 4
+    assert P.plora_route_workspace_bytes(300, 0) == P.plora_route_workspace_bytes(300, 1025) == P.plora_route_workspace_bytes(-5, 8) == 0
 
 
 def test_wrappers_refuse_tensors_that_do_not_fit():

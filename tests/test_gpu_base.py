@@ -3,8 +3,10 @@
 Bounds, from the arithmetic (a step of a rounding: eps / 2 of the type):
   codes      equal bytes, where the choice runs in 32 bits on the inputs; behind an activation or a norm the value is off by some units of
              32 bits first, so a code may be its neighbour: half a step of the code (2^-4 relative, 2^-10 scales below the normal codes) and that.
-  products   products of codes are exact; each of the 128 additions inside a block loses at most 2^-23 of the block's sum of magnitudes, each
-             of a row's blocks 3 roundings (two scales, one multiply-add) of 2^-24.
+  products   products of codes are exact.  fp32: each of the 128 additions inside a block loses at most 2^-23 of the block's sum of magnitudes.
+             16-bit types: of 8 neighbouring products the matrix unit keeps the bits down to 2^-13 of the largest one's power of two, so each of the
+             7 others loses less than 2^-13 of the largest; the 16 sums of 8 are added as above.  Each of a row's blocks has 3 roundings
+             (two scales, one multiply-add) of 2^-24.  As a 2-norm the error stays below what the results' own rounding may have at most.
   norms      a sum of squares over 16384 channels is 64 additions a thread and 8 between threads: 72 * 2^-24 relative, the root halves it;
              the parts of hidden are 4 roundings and one for each expert's row.
 """
@@ -156,7 +158,25 @@ def test_weights(dtype, experts, n, k):
 
 def product_bound(x, w, ref, dtype):
     kb = -(-x.shape[1] // 128)
-    return DT[dtype][0] * np.abs(ref) + (128 * 2 + 3 * kb) * U * (np.abs(x) @ np.abs(w).T) + 1e-37
+    off = DT[dtype][0] * np.abs(ref) + (128 * 2 + 3 * kb) * U * (np.abs(x) @ np.abs(w).T) + 1e-37
+    if dtype == "fp16":
+        off += 2.0 ** -25  # half a step of its smallest values
+    if dtype != "fp32":
+        gx, gw = (np.abs(v).reshape(len(v), -1, 8).max(-1) for v in (x, w))  # k is a multiple of 16
+        off += 7 * 2.0 ** -13 * (gx @ gw.T) * (1 + DT[dtype][0])
+    return off
+
+
+def check_product(got, x, w, dtype):
+    ref = x @ w.T
+    off = product_bound(x, w, ref, dtype)
+    if dtype == "fp16":  # 65520 is the middle between fp16's largest value and the power of two behind it: from there on a rounding gives inf
+        over = np.isinf(got)
+        assert (np.abs(ref) + off >= 65520)[over].all() and (np.sign(got) == np.sign(ref))[over].all() and (np.abs(ref) - off < 65520)[~over].all()
+        got, ref, off = (np.where(over, 0, v) for v in (got, ref, off))
+    assert (np.abs(got - ref) <= off).all()
+    if dtype != "fp32":
+        assert np.linalg.norm(got - ref) <= DT[dtype][0] * np.linalg.norm(ref)
 
 
 SIZES = [(1, 8, 16), (1, 4096, 4096), (2, 264, 144), (5, 1000, 2048), (16, 128, 128), (17, 136, 272), (33, 1024, 5120), (64, 72, 4096), (65, 512, 1040),
@@ -170,10 +190,9 @@ def test_product(dtype, t, n, k):
     rng = np.random.default_rng(t + n + k)
     x, xv = made_rows(rng, t, k)
     w, wv = made_weights(rng, n, k)
-    ref = xv @ wv.T
     out = torch.full((t + 1, n + 8), 7.0, device="cuda", dtype=getattr(torch, DT[dtype][1]))
     w.matmul(x, out[:t, :n], stream())
-    assert (np.abs(host(out[:t, :n]) - ref) <= product_bound(xv, wv, ref, dtype)).all()
+    check_product(host(out[:t, :n]), xv, wv, dtype)
     assert (out[t:] == 7).all() and (out[:, n:] == 7).all()
 
 
@@ -188,10 +207,9 @@ def test_product_of_rows_in_wider_ones():
     scales[:, :70] = torch.from_numpy(s).cuda()
     w, wv = made_weights(rng, 264, 400)
     xv = O.row_values(c, s)
-    ref = xv @ wv.T
     out = torch.empty(70, 264, device="cuda")
     w.matmul(P.Fp8Rows(codes[:, :400], scales[:, :70]), out, stream())
-    assert (np.abs(host(out) - ref) <= product_bound(xv, wv, ref, "fp32")).all()
+    check_product(host(out), xv, wv, "fp32")
 
 
 @pytest.mark.parametrize("t", [1, 20, 64, 130, 300])
@@ -260,8 +278,7 @@ def test_grouped(dtype, gather, sizes, n, k):
             if not 0 <= src < have:
                 assert np.isnan(got[r]).all()
                 continue
-            ref = xv[src] @ wv[e].T
-            assert (np.abs(got[r] - ref) <= product_bound(xv[src][None], wv[e], ref, dtype)).all()
+            check_product(got[r][None], xv[src][None], wv[e], dtype)
 
 
 @pytest.mark.parametrize("offsets", [[0, -5, 40, 1000, 90], [-3, -1, 0, 0, 5], [10, 20, 20, 30, 2000000000], [50, 40, 30, 20, 10]])
@@ -286,8 +303,98 @@ def test_offsets_out_of_range(offsets):
         if of[r] < 0:
             assert (got[r] == 7).all()
         else:
-            ref = xv[r] @ wv[of[r]].T
-            assert (np.abs(got[r] - ref) <= product_bound(xv[r][None], wv[of[r]], ref, "fp32")).all()
+            check_product(got[r][None], xv[r][None], wv[of[r]], "fp32")
+
+
+def random_codes(rng, *shape):
+    """All codes but NaN alike: sizes over 16 powers of two."""
+    c = rng.integers(0, 127, shape, dtype=np.uint8)
+    return c | (rng.integers(0, 2, shape, dtype=np.uint8) << 7)
+
+
+# rows, channels, values: each of the kernels that the rule chooses from (few rows: 3, tiles: 8), and an odd end everywhere
+KINDS = [(9, 72, 528), (9, 4104, 528), (9, 72, 144), (17, 72, 2064), (2070, 264, 4112), (17, 72, 144), (2070, 520, 2064), (1500, 2056, 144), (1030, 5128, 144),
+         (2070, 2056, 2064), (1030, 7176, 144)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("t,n,k", KINDS)
+def test_product_of_each_kernel(dtype, t, n, k):
+    import torch
+    P = lib()
+    rng = np.random.default_rng(t * n + k)
+    xc, wc = random_codes(rng, t, k), random_codes(rng, n, k)
+    xs, ws = (np.exp(rng.normal(size=z)).astype(np.float32) for z in ((-(-k // 128), t), (-(-n // 128), -(-k // 128))))
+    put_ = lambda v: torch.from_numpy(v).cuda()  # noqa: E731
+    out = torch.full((t + 1, n + 8), 7.0, device="cuda", dtype=torch.float32 if dtype == "fp32" else getattr(torch, DT[dtype][1]))
+    xs /= 30 * k  # (fp16: results stay in range)
+    P.Fp8Weights(put_(wc), put_(ws)).matmul(P.Fp8Rows(put_(xc), put_(xs)), out[:t, :n], stream())
+    got = host(out)
+    assert (got[t:] == 7).all() and (got[:, n:] == 7).all()
+    check_product(got[:t, :n], O.row_values(xc, xs), O.weight_values(wc, ws), dtype)
+
+
+GROUPED_KINDS = [(9, 72, 528), (9, 1032, 528), (9, 72, 144), (100, 72, 2064), (100, 2056, 4112), (100, 72, 144), (413, 2056, 2064), (1500, 2056, 144), (257, 13832, 144),
+                 (600, 5128, 2064), (413, 13832, 144)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("t,n,k", GROUPED_KINDS)
+def test_grouped_of_each_kernel(dtype, t, n, k):
+    """Five experts, one of them with half of the rows, one with none; rows gathered and not."""
+    import torch
+    P = lib()
+    rng = np.random.default_rng(t * n + k)
+    xc, wc = random_codes(rng, t, k), random_codes(rng, 5, n, k)
+    xs, ws = (np.exp(rng.normal(size=z)).astype(np.float32) for z in ((-(-k // 128), t), (5, -(-n // 128), -(-k // 128))))
+    xs /= 30 * k
+    put_ = lambda v: torch.from_numpy(v).cuda()  # noqa: E731
+    x, w = P.Fp8Rows(put_(xc), put_(xs)), P.Fp8Weights(put_(wc), put_(ws))
+    offsets = np.array([0, 1, 1 + t // 2, 1 + t // 2, 3 + t // 2, t])
+    rows = rng.integers(0, t, t)
+    xv = O.row_values(xc, xs)
+    for r in (None, rows):
+        out = torch.full((t, n), 7.0, device="cuda", dtype=getattr(torch, DT[dtype][1]))
+        w.grouped(x, ints(offsets), out, None if r is None else ints(r), stream())
+        got = host(out)
+        for e in range(5):
+            a, b = offsets[e], offsets[e + 1]
+            if a < b:
+                check_product(got[a:b], xv[a:b] if r is None else xv[r[a:b]], O.weight_values(wc[e], ws[e]), dtype)
+
+
+def test_rows_far_apart():
+    """x's rows behind 2 and 4 GiB, and results behind 4 GiB."""
+    import torch
+    P = lib()
+    rng = np.random.default_rng(8)
+    n, k, total, step = 136, 272, 5000, 1 << 20
+    codes = torch.empty(total, step, device="cuda", dtype=torch.uint8)
+    pick = np.concatenate([rng.integers(0, total, 30), [0, 2047, 2048, 4095, 4096, total - 1]])
+    xc, xs = random_codes(rng, total, k), np.exp(rng.normal(size=(3, total))).astype(np.float32)
+    codes[:, :k] = torch.from_numpy(xc).cuda()
+    x = P.Fp8Rows(codes[:, :k], torch.from_numpy(xs).cuda())
+    xv = O.row_values(xc, xs)
+    w, wv = made_weights(rng, n, k, 2)
+    wide = torch.empty(len(pick), 1 << 26, device="cuda")  # 256 MiB a row
+    w.grouped(x, ints([0, 20, len(pick)]), wide[:, :n], ints(pick), stream())
+    got = host(wide[:, :n])
+    check_product(got[:20], xv[pick[:20]], wv[0], "fp32")
+    check_product(got[20:], xv[pick[20:]], wv[1], "fp32")
+    one = P.Fp8Weights(w.codes[0], w.scales[0])
+    out = torch.empty(total, n, device="cuda", dtype=torch.bfloat16)
+    one.matmul(x, out, stream())
+    check_product(host(out), xv, wv[0], "bf16")
+    few = codes[::625]  # 8 rows, 655 MB from one to the next
+    few.copy_(codes[:8])
+    out = torch.empty(8, n, device="cuda")
+    one.matmul(P.Fp8Rows(few[:, :k], x.scales[:, :8]), out, stream())
+    check_product(host(out), xv[:8], wv[0], "fp32")
+    many = codes.view(-1, 1 << 23)[:600, :k]  # 600 rows, 8 MiB from one to the next: a tile's rows pass 2 GiB
+    many.copy_(torch.from_numpy(xc[:600]).cuda())
+    out = torch.empty(600, n, device="cuda")
+    one.matmul(P.Fp8Rows(many, x.scales[:, :600]), out, stream())
+    check_product(host(out), xv[:600], wv[0], "fp32")
 
 
 # ---- routing ------------------------------------------------------------------------------------------
@@ -317,7 +424,7 @@ def check_route(r, logits64, k, renormalise, scale):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
-@pytest.mark.parametrize("n,e,k", [(1, 1, 1), (1, 8, 2), (5, 64, 6), (63, 65, 8), (64, 256, 8), (65, 64, 4), (130, 7, 7), (300, 128, 32), (1000, 512, 3),
+@pytest.mark.parametrize("n,e,k", [(1, 1, 1), (1, 8, 2), (5, 64, 6), (63, 65, 8), (64, 256, 8), (65, 64, 4), (130, 7, 7), (300, 128, 32), (200, 130, 9), (256, 1024, 2), (257, 16, 16), (1, 513, 8), (64, 512, 8), (64, 1000, 32), (1100, 300, 17), (1000, 512, 3),
                                    (700, 1024, 8), (4097, 60, 2), (5000, 200, 6)])
 def test_routing(dtype, n, e, k):
     import torch
@@ -340,15 +447,16 @@ def test_routing(dtype, n, e, k):
     check_route(r, x64, k, False, 2.5)
 
 
-def test_routing_of_no_tokens():
+@pytest.mark.parametrize("e", [8, 1000])
+def test_routing_of_no_tokens(e):
     import torch
     P = lib()
-    r = P.Routing(ints(np.zeros((0, 2))), torch.zeros(0, 2, device="cuda"), ints([5] * 9), ints([]), ints(np.zeros((0, 2))))
-    r.route(torch.zeros(0, 8, device="cuda"), stream=stream())
+    r = P.Routing(ints(np.zeros((0, 2))), torch.zeros(0, 2, device="cuda"), ints([5] * (e + 1)), ints([]), ints(np.zeros((0, 2))))
+    r.route(torch.zeros(0, e, device="cuda"), stream=stream())
     assert (r.offsets == 0).all()
 
 
-@pytest.mark.parametrize("chunks", [64, 65, 300])
+@pytest.mark.parametrize("chunks", [15, 16, 17, 64, 300])
 def test_routing_over_many_chunks(chunks):
     """Both ways in which the chunks' counts are summed, at the size where they change: against torch's stable sort."""
     import torch
