@@ -101,12 +101,13 @@ struct NormArgs {
 };
 
 // A row has TPR threads, each with V groups of 8 channels (group i of thread j: channels 8 * (j + TPR * i)), held in registers from the
-// first load to the last store: every input is read once.
-template <int DT, int TPR, int V>
+// first load to the last store: every input is read once.  PLACES: a token's rows are gathered; FULL: with a gate or a norm ahead of it.  (Kernels of
+// their own for the registers of calls without them: 4096 channels take 58 in place of 103.)  Memory bounds it: 5093 rows of 5120 with all parts 48 us
+// for 236 MB, 2049 rows of 4096 that gather 4 rows each 28 us for 118 MB (four rows in flight and 140 registers: 30).
+template <int DT, int TPR, int V, bool PLACES, bool FULL>
 __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
   constexpr int B = Elt<DT>::B, ROWS = kThreads / TPR;
   constexpr bool EARLY = V <= 4;  // weights asked for ahead of the reductions
-  constexpr int U = V <= 2 ? 4 : V <= 4 ? 2 : 1;  // experts' rows in flight
   __shared__ float part[4][kThreads / 64];
   const int j = threadIdx.x % TPR;
   const int64_t row = (int64_t)neighbours(blockIdx.x, gridDim.x) * ROWS + threadIdx.x / TPR;
@@ -125,17 +126,17 @@ __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
   if (a.residual)
 #pragma unroll
     for (int i = 0; i < V; ++i) rr[i] = raw8<DT>(a.residual + t * a.residual_s + (int64_t)c[i] * B);
-  if (a.gate)
+  if (FULL && a.gate)
 #pragma unroll
     for (int i = 0; i < V; ++i) gg[i] = raw8<DT>(a.gate + t * a.gate_s + (int64_t)c[i] * B);
-  if (EARLY && a.post.w)
+  if (EARLY && FULL && a.post.w)
 #pragma unroll
     for (int i = 0; i < V; ++i) wpo[i] = raw8<DT>(a.post.w + (int64_t)c[i] * B);
   if (EARLY && a.pre.w)
 #pragma unroll
     for (int i = 0; i < V; ++i) wpr[i] = raw8<DT>(a.pre.w + (int64_t)c[i] * B);
 
-  if (!a.places) {
+  if constexpr (!PLACES) {
 #pragma unroll
     for (int i = 0; i < V; ++i) ld8<DT>(a.block + t * a.block_s + (int64_t)c[i] * B, x[i]);
   } else {
@@ -143,30 +144,35 @@ __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
     for (int i = 0; i < V; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
-    for (int k0 = 0; k0 < a.top_k; k0 += U) {
-      float w[U];
-      Raw8<DT> q[U][V] = {};
+    // the next row is on its way while one is added; one that is not there is the first row, whose values are left out
+    const int64_t t0 = t * a.top_k;
+    const auto ask = [&](int k, Raw8<DT>* q) {
+      const int32_t p = a.places[t0 + k];
+      const bool ok = (uint32_t)p < (uint32_t)a.n_block_rows;
+      const uint8_t* from = a.block + (int64_t)(ok ? p : 0) * a.block_s;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const bool in = k0 + u < a.top_k;
-        const int64_t at = t * a.top_k + (in ? k0 + u : 0);
-        const int32_t p = a.places[at];
-        const bool ok = in && (uint32_t)p < (uint32_t)a.n_block_rows;
-        w[u] = ok ? a.place_weights[at] : 0.f;
-        if (ok) {
+      for (int i = 0; i < V; ++i) q[i] = raw8<DT>(from + (int64_t)c[i] * B);
+      return ok;
+    };
+    const auto add = [&](int k, const Raw8<DT>* q) {
+      const float w = a.place_weights[t0 + k];
 #pragma unroll
-          for (int i = 0; i < V; ++i) q[u][i] = raw8<DT>(a.block + (int64_t)p * a.block_s + (int64_t)c[i] * B);
-        }
+      for (int i = 0; i < V; ++i) {
+        float f[8];
+        unpack<DT>(q[i], f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[i][e] = __builtin_fmaf(w, f[e], x[i][e]);
       }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          float f[8];
-          unpack<DT>(q[u][i], f);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[i][e] = __builtin_fmaf(w[u], f[e], x[i][e]);
-        }
+    };
+    if (a.n_block_rows > 0) {
+      Raw8<DT> q[2][V];
+      bool ok = ask(0, q[0]);
+      for (int k = 0; k < a.top_k; k += 2) {
+        const bool second = k + 1 < a.top_k && ask(k + 1, q[1]);
+        if (ok) add(k, q[0]);
+        ok = k + 2 < a.top_k && ask(k + 2, q[0]);
+        if (second) add(k + 1, q[1]);
+      }
     }
   }
 
@@ -221,13 +227,14 @@ __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
     }
   };
 
-  if (a.post.on) norm(a.post, wpo);
+  if constexpr (FULL)
+    if (a.post.on) norm(a.post, wpo);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     float f[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[i][e] *= a.scale;
-    if (a.gate) {
+    if (FULL && a.gate) {
       unpack<DT>(gg[i], f);
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[i][e] *= f[e];
@@ -259,18 +266,24 @@ __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
   }
 }
 
-template <int DT>
+template <int DT, bool PLACES, bool FULL>
 int norm(const NormArgs& a, plora_stream stream) {
   const auto go = [&](void (*k)(NormArgs), int tpr) { return launch(k, ((uint64_t)a.n_tokens * tpr + kThreads - 1) / kThreads, 1, 1, a, stream); };
   const int d = a.dim;
-  return d <= 128    ? go(k_norm<DT, 16, 1>, 16)
-         : d <= 512  ? go(k_norm<DT, 64, 1>, 64)
-         : d <= 1024 ? go(k_norm<DT, 64, 2>, 64)
-         : d <= 2048 ? go(k_norm<DT, 256, 1>, 256)
-         : d <= 4096 ? go(k_norm<DT, 256, 2>, 256)
-         : d <= 6144 ? go(k_norm<DT, 256, 3>, 256)
-         : d <= 8192 ? go(k_norm<DT, 256, 4>, 256)
-                     : go(k_norm<DT, 256, 8>, 256);
+  return d <= 128    ? go(k_norm<DT, 16, 1, PLACES, FULL>, 16)
+         : d <= 512  ? go(k_norm<DT, 64, 1, PLACES, FULL>, 64)
+         : d <= 1024 ? go(k_norm<DT, 64, 2, PLACES, FULL>, 64)
+         : d <= 2048 ? go(k_norm<DT, 256, 1, PLACES, FULL>, 256)
+         : d <= 4096 ? go(k_norm<DT, 256, 2, PLACES, FULL>, 256)
+         : d <= 6144 ? go(k_norm<DT, 256, 3, PLACES, FULL>, 256)
+         : d <= 8192 ? go(k_norm<DT, 256, 4, PLACES, FULL>, 256)
+                     : go(k_norm<DT, 256, 8, PLACES, FULL>, 256);
+}
+template <int DT>
+int norm(const NormArgs& a, plora_stream stream) {
+  const bool full = a.gate || a.post.on;
+  return a.places ? (full ? norm<DT, true, true>(a, stream) : norm<DT, true, false>(a, stream))
+                  : (full ? norm<DT, false, true>(a, stream) : norm<DT, false, false>(a, stream));
 }
 
 // ---- rows and weights in 8 bits -----------------------------------------------------------------------
