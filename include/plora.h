@@ -513,7 +513,8 @@ int plora_kv_attend(const plora_kv_cache* cache, const plora_kv_batch* batch, in
  * caller's, and what device arrays hold is defined below for every value.
  *
  * Matrices.  plora_matrix: rows of contiguous elements, row r at data + r * stride (in elements; outputs: at least a row).  data
- * is 16-byte aligned and the stride a multiple of 16 bytes (routing's logits: any).  Inputs may have stride 0 (one row for all). */
+ * is 16-byte aligned and the stride a multiple of 16 bytes (routing's logits: any).  Inputs may have stride 0 (one row for all).  Outputs overlap
+ * no input and no other output unless a call says so.  LIMIT: more rows than a launch holds (from 16 million on). */
 typedef struct {
   void* data; /* device; read only where the call takes a const plora_matrix that it does not write */
   int64_t stride;

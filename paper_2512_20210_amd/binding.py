@@ -970,7 +970,7 @@ def _matrix_of(call, t, n_rows, width, dtype, device):
     st = t.stride()
     if t.shape != (n_rows, width) or (width > 1 and st[1] != 1) or _dtype_of(t) != dtype or t.get_device() != device:
         raise PloraError(call, PLORA_ERR_INVAL)
-    return MatrixStruct(t.data_ptr(), st[0])
+    return MatrixStruct(t.data_ptr(), st[0] if n_rows > 1 else -(-width // 8) * 8)  # (one row may have any stride)
 
 
 def _two(call, t):
@@ -1157,7 +1157,7 @@ class BlockNorm:
             st = t.stride()
             if t.shape != (rows, dim) or st[1] != 1 or _dtype_of(t) != dtype or t.get_device() != device:
                 raise PloraError(call, PLORA_ERR_INVAL)
-            parts += (t.data_ptr(), st[0])
+            parts += (t.data_ptr(), st[0] if rows > 1 else dim)
         e = None if out8 is None else out8.c
         args = BlockNormStruct(dtype, n, dim, self.scale, parts[0], parts[1], None if places is None else _ints_of(call, places, n * top_k, device),
                                None if places is None else place_weights.data_ptr(), top_k, block_rows if places is not None else 0,

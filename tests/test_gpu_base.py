@@ -594,3 +594,63 @@ def test_no_rows():
     r.quantise(e, stream=stream())
     w, _ = made_weights(np.random.default_rng(0), 8, 64, 2)
     w.grouped(r, ints([0, 0, 0]), torch.empty(0, 8, device="cuda"), None, stream())
+
+
+def test_one_row_of_a_wider_tensor():
+    """A row cut out of a tensor whose width is no multiple of 16 bytes: its stride does not matter."""
+    import torch
+    P = lib()
+    rng = np.random.default_rng(4)
+    wide, w64 = put(rng.normal(size=(1, 403)), "bf16")
+    x = wide[:, :400]
+    out = torch.empty(1, 413, device="cuda", dtype=torch.bfloat16)[:, :400]
+    P.BlockNorm(P.NormWeights()).run(x, out=out, stream=stream())
+    ref = O.norm(w64[:, :400])
+    assert (np.abs(host(out) - ref) <= 2.0 ** -8 * np.abs(ref) + 1e-5).all()
+    r, codes, scales = empty_rows(1, 400)
+    r.quantise(x, stream=stream())
+    c, s = O.rows(w64[:, :400].astype(np.float32))
+    assert (codes.cpu().numpy() == c).all() and (scales.cpu().numpy() == s).all()
+    w, wv = made_weights(rng, 264, 400)
+    y = torch.empty(1, 271, device="cuda")[:, :264]
+    w.matmul(r, y, stream())
+    check_product(host(y), O.row_values(c, s), wv, "fp32")
+
+
+def test_wrappers_refuse():
+    """Tensors that are not on the GPU, of other types, sizes or strides."""
+    import torch
+    P = lib()
+    f = lambda *z, d=torch.bfloat16: torch.zeros(*z, device="cuda", dtype=d)  # noqa: E731
+    i = lambda *z: torch.zeros(*z, device="cuda", dtype=torch.int32)  # noqa: E731
+    u8 = torch.uint8
+    rows = P.Fp8Rows(f(4, 256, d=u8), f(2, 4, d=torch.float32))
+    w = P.Fp8Weights(f(264, 256, d=u8), f(3, 2, d=torch.float32))
+    ws = P.Fp8Weights(f(2, 264, 256, d=u8), f(2, 3, 2, d=torch.float32))
+    route = P.Routing(i(4, 2), f(4, 2, d=torch.float32), i(9), i(8), i(4, 2))
+    norm = P.BlockNorm(P.NormWeights(f(256)))
+    x = f(4, 256)
+    bad = [
+        lambda: P.Fp8Rows(f(4, 256, d=u8), f(2, 5, d=torch.float32)), lambda: P.Fp8Rows(f(4, 256, d=u8), f(3, 4, d=torch.float32)),
+        lambda: P.Fp8Rows(f(4, 256), f(2, 4, d=torch.float32)), lambda: P.Fp8Rows(f(4, 512, d=u8)[:, ::2], f(2, 4, d=torch.float32)),
+        lambda: P.Fp8Rows(f(4, 256, d=u8), f(2, 4)), lambda: P.Fp8Rows(f(4, 256, d=u8).cpu(), f(2, 4, d=torch.float32)),
+        lambda: P.Fp8Weights(f(264, 256, d=u8), f(2, 2, d=torch.float32)), lambda: P.Fp8Weights(f(264, 512, d=u8)[:, :256], f(3, 2, d=torch.float32)),
+        lambda: rows.quantise(x.cpu()), lambda: rows.quantise(f(4, 264)), lambda: rows.quantise(x, P.PLORA_ACT_SILU), lambda: rows.quantise(f(4, 256, d=torch.float64)),
+        lambda: rows.quantise(x, 7), lambda: w.quantise(f(264, 512)[:, :256]), lambda: w.quantise(f(264, 264)),
+        lambda: w.matmul(rows, f(4, 256)), lambda: w.matmul(rows, f(5, 264)), lambda: w.matmul(rows, f(4, 264).cpu()), lambda: ws.matmul(rows, f(4, 264)),
+        lambda: w.matmul(P.Fp8Rows(f(4, 272, d=u8), f(3, 4, d=torch.float32)), f(4, 264)), lambda: w.matmul(rows, f(4, 268)[:, :264]),
+        lambda: ws.grouped(rows, i(2), f(4, 264)), lambda: ws.grouped(rows, i(3).long(), f(4, 264)), lambda: ws.grouped(rows, i(3), f(5, 264)),
+        lambda: ws.grouped(rows, i(3), f(8, 264), i(7)), lambda: ws.grouped(rows, i(3).cpu(), f(4, 264)),
+        lambda: route.route(f(4, 9)), lambda: route.route(f(5, 8)), lambda: route.route(f(4, 8).cpu()), lambda: P.Routing(i(4, 2), f(4, 2), i(9), i(8), i(4, 2)),
+        lambda: P.Routing(i(4, 2), f(4, 2, d=torch.float32), i(9), i(7), i(4, 2)), lambda: P.Routing(i(4, 9), f(4, 9, d=torch.float32), i(9), i(36), i(4, 9)).route(f(4, 8)),
+        lambda: P.Routing(i(70, 2), f(70, 2, d=torch.float32), i(9), i(140), i(70, 2)).route(f(70, 8)),  # no workspace
+        lambda: norm.run(x), lambda: norm.run(x, out=f(4, 264)), lambda: norm.run(x, out=f(4, 256, d=torch.float16)), lambda: norm.run(x, out=x.cpu()),
+        lambda: norm.run(f(4, 264), out=f(4, 264)), lambda: norm.run(x, out=f(4, 256), out8=rows), lambda: norm.run(x, out=f(4, 256), residual=f(3, 256)),
+        lambda: norm.run(x, out=f(2, 256), places=i(2, 2)), lambda: norm.run(x, out=f(4, 256), place_weights=f(4, 2, d=torch.float32)),
+        lambda: norm.run(x, out=x, places=i(4, 2), place_weights=f(4, 2, d=torch.float32)), lambda: norm.run(x, hidden=x, out=x),
+        lambda: P.NormWeights(f(256), f(255)), lambda: P.NormWeights(f(256), f(256, d=torch.float16)), lambda: P.NormWeights(f(512)[::2]),
+    ]
+    for n, call in enumerate(bad):
+        with pytest.raises(P.PloraError):
+            call()
+            print("call %d was not refused" % n)
