@@ -168,8 +168,15 @@ __device__ __forceinline__ void st4(uint8_t* p, f32x4 f) {
 
 // Tiles of TT rows x TN channels by WT x WN wavefronts, both operands through LDS, a block of 128 values a stage and STAGES of them; with KG > 1
 // so many sets of wavefronts share the blocks in turn, each with stages of its own, and their sums are joined at the end (in
-// their order).  A stage's rows are 128 bytes; the 16-byte piece p of row r lies at p ^ (r / 2 % 8), so that 16 lanes that read one
-// piece of 16 rows meet all 64 banks.
+// their order).  LDS bounds the large tile: a stage of 256 x 256 is written once (64 KiB) and read by wavefronts of 64 x 128 (192 KiB) beside 64
+// matrix instructions a SIMD; 16384 x 13824 x 5120 takes 950 us (2.44 PFLOP/s), matrix units busy 61 % of the time at 1.9 GHz.  Ways there: 64 x 64
+// tiles 1920 us; 256 x 256 1262; results used four products later 1069 (one: 1088); loads spread over the products 1013 (as one: 1061);
+// the barrier ahead of the last row, one load of scales a stage 961; bands of 4 row tiles 950 (of 8: 961).  Not kept: weights two rows ahead (973),
+// 32 x 32 x 64 instructions (registers spill: 2032), 4 wavefronts of 128 x 128 (1196), lines asked for 4 stages ahead (1040), wave priorities (952).
+// Small tiles are bound by a stage's chain of barrier, reads and products (64 x 64: 0.3 us a block): two sets of wavefronts where there
+// are few tiles.
+// A stage's rows are 128 bytes; the 16-byte piece p of row r lies at p ^ (r / 2 % 8), so that 16 lanes that read one
+// piece of 16 rows meet all 64 banks (with r % 8 half of the reads' cycles were conflicts).
 template <int DT, int TT, int TN, int WT, int WN, int KG, int STAGES, bool GROUPED>
 __global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_eu(2))) void k_product(ProductArgs a) {
   constexpr int WAVES = WT * WN, NT = TT / WT / 16, NN = TN / WN / 16;
