@@ -168,25 +168,30 @@ __device__ __forceinline__ void st4(uint8_t* p, f32x4 f) {
 
 // Tiles of TT rows x TN channels by WT x WN wavefronts, both operands through LDS, a block of 128 values a stage and STAGES of them; with KG > 1
 // so many sets of wavefronts share the blocks in turn, each with stages of its own, and their sums are joined at the end (in
-// their order).  LDS bounds the large tile: a stage of 256 x 256 is written once (64 KiB) and read by wavefronts of 64 x 128 (192 KiB) beside 64
-// matrix instructions a SIMD; 16384 x 13824 x 5120 takes 950 us (2.44 PFLOP/s), matrix units busy 61 % of the time at 1.9 GHz.  Ways there: 64 x 64
-// tiles 1920 us; 256 x 256 1262; results used four products later 1069 (one: 1088); loads spread over the products 1013 (as one: 1061);
-// the barrier ahead of the last row, one load of scales a stage 961; bands of 4 row tiles 950 (of 8: 961).  Not kept: weights two rows ahead (973),
-// 32 x 32 x 64 instructions (registers spill: 2032), 4 wavefronts of 128 x 128 (1196), lines asked for 4 stages ahead (1040), wave priorities (952).
-// Small tiles are bound by a stage's chain of barrier, reads and products (64 x 64: 0.3 us a block): two sets of wavefronts where there
-// are few tiles.
-// A stage's rows are 128 bytes; the 16-byte piece p of row r lies at p ^ (r / 2 % 8), so that 16 lanes that read one
-// piece of 16 rows meet all 64 banks (with r % 8 half of the reads' cycles were conflicts).
-template <int DT, int TT, int TN, int WT, int WN, int KG, int STAGES, bool GROUPED>
+// their order).  ONE_X: x has one stage only, which is free again when all wavefronts have read it into registers (a second barrier); that
+// leaves room for a third stage of weights of 256 channels.  A stage's rows are 128 bytes; the 16-byte piece p of row r lies at
+// p ^ (r / 2 % 8), so that 16 lanes that read one piece of 16 rows meet all 64 banks (with r % 8 half of the reads' cycles were conflicts).
+// LDS bounds the large tile: a stage of 256 x 256 is written once (64 KiB) and read by wavefronts of 64 x 128 (192 KiB) beside 64 matrix
+// instructions a SIMD (without the reads of weights it would take 734 us in place of 943).  16384 x 13824 x 5120: 943 us (2.46 PFLOP/s), matrix
+// units busy 61 % of the time at 1.9 GHz.  Ways there: 64 x 64 tiles 1920 us; 256 x 256 1262; results used four products later 1069
+// (one: 1088); loads spread over the products 1013 (as one: 1061); the barrier ahead of the last row and one load of scales a stage 961; bands
+// of 4 row tiles 950 (of 8: 961); one stage of x, three of weights 943 (experts' prompts: 350 -> 336).  Not kept: weights two rows ahead
+// (973), 32 x 32 x 64 instructions (registers spill: 2032), 4 wavefronts of 128 x 128 (1196), lines asked for 4 stages ahead (1040), wave
+// priorities (952).
+// Smaller tiles are bound by how fast a CU gets its operands (0.5 - 0.6 us for 24 - 32 KiB of a 128 x 64 or 128 x 128 block, with two blocks a
+// barrier as well); two sets of wavefronts where there are few tiles.
+template <int DT, int TT, int TN, int WT, int WN, int KG, int STAGES, bool ONE_X, bool GROUPED>
 __global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_eu(2))) void k_product(ProductArgs a) {
   constexpr int WAVES = WT * WN, NT = TT / WT / 16, NN = TN / WN / 16;
   constexpr int LX = TT / 8 / WAVES, LW = TN / 8 / WAVES;  // 16-byte loads of a thread and stage
   // they are spread over the first half of a stage's products: kPer of them every kEvery products
   constexpr int kHalf = NN * NT / 2, kEvery = kHalf > LX + LW ? kHalf / (LX + LW) : 1, kPer = (LX + LW + kHalf - 1) / kHalf;
-  constexpr int kStage = (TT + TN) * kBlock, kScales = WAVES * 256, kSet = STAGES * (kStage + kScales);
+  constexpr int kX = TT * kBlock, kW = TN * kBlock, kScales = WAVES * 256, kSlotsX = ONE_X ? 1 : STAGES;
+  constexpr int kAtW = kSlotsX * kX, kAtScales = kAtW + STAGES * kW, kSet = kAtScales + kSlotsX * kScales;  // of a set's LDS: x, weights, scales
   static_assert(LX * 8 * WAVES == TT && LW * 8 * WAVES == TN && WAVES % 2 == 0 && NN % 2 == 0 && NT <= 4, "whole loads");
   static_assert(TN / WN <= kBlock && kBlock % (TN / WN) == 0, "one scale of weights a wavefront");
-  static_assert((LX + LW) / kPer * kEvery < NN * NT, "all loads of a stage are sent between two barriers");
+  static_assert(ONE_X || (LX + LW) / kPer * kEvery < NN * NT, "all loads of a stage are sent between two barriers");
+  static_assert(!ONE_X || (KG == 1 && STAGES == 3 && 2 * (LX + 1 + LW) <= (NN - 2) * NT), "and between the second barrier and the next stage's first");
   static_assert((KG - 1) * TT * TN * 4 <= KG * kSet, "the sums are joined in the stages' place");
   __shared__ alignas(16) uint8_t lds[KG * kSet];
   const Tile tile = tile_of<TT, TN, GROUPED>(a);
@@ -218,15 +223,17 @@ __global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_
   const int32_t scale_row = row_of(quad % NT);
   const uint32_t scale_at = scale_row < 0 ? 0 : (uint32_t)(scale_row - first_row) * 4;
   const uint8_t* mine = lds + set * kSet;
-  const uint32_t to = __builtin_amdgcn_readfirstlane(lds_addr(mine) + wave * 1024), scales_to = __builtin_amdgcn_readfirstlane(lds_addr(mine) + STAGES * kStage + wave * 256);
-  // Load i of the set's step s; behind the last code of the rows, and behind the last block: zeros.  Load LX + LW: the wavefront's scales of x.
+  const uint32_t to = __builtin_amdgcn_readfirstlane(lds_addr(mine) + wave * 1024), scales_to = __builtin_amdgcn_readfirstlane(lds_addr(mine) + kAtScales + wave * 256);
+  // Load i of the set's step s: LX of x, the wavefront's scales of x, LW of weights.  Behind the last code of the rows, and behind the last block: zeros.
   const auto fetch = [&](int s, int slot, int i) {
     const int b = s * KG + set;
-    if (i < LX + LW) {
-      load_to_lds(i < LX ? bx : bw, b * kBlock + piece * 16 < a.k ? at[i] : kNowhere, b * kBlock, to + slot * kStage + i * WAVES * 1024);
-    } else {
+    if (i == LX) {
       const i32x4 bs = buffer_at(reinterpret_cast<const uint8_t*>(a.xs + first_row + (int64_t)(b < kb ? b : 0) * a.xs_s));
-      load_word_to_lds(bs, b < kb ? scale_at : kNowhere, scales_to + slot * kScales);
+      load_word_to_lds(bs, b < kb ? scale_at : kNowhere, scales_to + (ONE_X ? 0 : slot) * kScales);
+    } else {
+      const int l = i < LX ? i : i - 1;
+      const uint32_t dst = i < LX ? to + (ONE_X ? 0 : slot) * kX + l * WAVES * 1024 : to + kAtW + slot * kW + (l - LX) * WAVES * 1024;
+      load_to_lds(i < LX ? bx : bw, b * kBlock + piece * 16 < a.k ? at[l] : kNowhere, b * kBlock, dst);
     }
   };
   const int channel = tile.channel + wn * (TN / WN);  // the wavefront's first one
@@ -234,13 +241,14 @@ __global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_
   typedef const __attribute__((address_space(4))) float* scalar_floats;
   const scalar_floats sw = (scalar_floats)(uintptr_t)(a.ws + ((int64_t)tile.expert * nb + (cb < nb ? cb : nb - 1)) * kb);
 
-  const auto operand = [&](int slot, int row) {
-    const uint8_t* p = mine + slot * kStage + row * kBlock;
+  const auto operand = [&](const uint8_t* rows, int row) {
+    const uint8_t* p = rows + row * kBlock;
     const int s = (row >> 1) & 7;
     const i32x4 lo = *reinterpret_cast<const i32x4*>(p + (quad ^ s) * 16), hi = *reinterpret_cast<const i32x4*>(p + ((quad + 4) ^ s) * 16);
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  const int row_x = wt * (TT / WT) + col, row_w = TT + wn * (TN / WN) + col;
+  const auto operand_x = [&](int slot, int t) { return Unit<DT>::make(operand(mine + (ONE_X ? 0 : slot) * kX, wt * (TT / WT) + col + t * 16)); };
+  const auto operand_w = [&](int slot, int m) { return operand(mine + kAtW + slot * kW, wn * (TN / WN) + col + m * 16); };
 
   // A stage's products go row after row (a row: one operand of weights, all of x).  While the matrix unit has a row, the next row's weights
   // are read and the products of the row before are scaled and added.  The one barrier of a stage is ahead of its last row: then the
@@ -249,24 +257,25 @@ __global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_
 #pragma unroll
   for (int s = 0; s < STAGES - 1; ++s)
 #pragma unroll
-    for (int i = 0; i <= LX + LW; ++i) fetch(s, s, i);
-  wait_loads<(STAGES - 2) * (LX + LW + 1)>();
+    for (int i = ONE_X && s > 0 ? LX + 1 : 0; i <= LX + LW; ++i) fetch(s, s, i);
+  constexpr int kLater = ONE_X ? LW : (STAGES - 2) * (LX + LW + 1);  // loads under way that are of stages behind the next one
+  wait_loads<kLater>();
   __syncthreads();
   f32x4 acc[NN][NT] = {}, d[NT] = {};
-  typedef typename Unit<DT>::operand operand_t;
-  operand_t x[NT];
+  typename Unit<DT>::operand x[NT];
   i32x8 w[2];
   float f[NT] = {}, fx[NT];
   const auto scales = [&](int slot) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) fx[t] = *reinterpret_cast<const float*>(mine + STAGES * kStage + slot * kScales + wave * 256 + (t * 16 + col) * 4);
+    for (int t = 0; t < NT; ++t) fx[t] = *reinterpret_cast<const float*>(mine + kAtScales + (ONE_X ? 0 : slot) * kScales + wave * 256 + (t * 16 + col) * 4);
   };
-  w[0] = operand(0, row_w);
+  w[0] = operand_w(0, 0);
 #pragma unroll
-  for (int t = 0; t < NT; ++t) x[t] = Unit<DT>::make(operand(0, row_x + t * 16));
+  for (int t = 0; t < NT; ++t) x[t] = operand_x(0, t);
   scales(0);
+  if constexpr (!ONE_X)
 #pragma unroll
-  for (int i = 0; i <= LX + LW && i / kPer * kEvery < NT; ++i) fetch(STAGES - 1, STAGES - 1, i);
+    for (int i = 0; i <= LX + LW && i / kPer * kEvery < NT; ++i) fetch(STAGES - 1, STAGES - 1, i);
   int slot = 0;
   for (int s = 0; s < steps; ++s) {
     const int b = s * KG + set, next = slot + 1 < STAGES ? slot + 1 : 0, free = slot > 0 ? slot - 1 : STAGES - 1;
@@ -281,25 +290,34 @@ __global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_
     for (int m = 0; m < NN; ++m) {
       if (m == NN - 1) {
         asm volatile("" : : : "memory");  // LDS reads stay on their side of the barrier
-        wait_loads<(STAGES - 2) * (LX + LW + 1)>();
+        wait_loads<kLater>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" : : : "memory");
         scales(next);
+      } else if (ONE_X && m == 1) {  // all wavefronts have x (their first row's products went ahead of this)
+        asm volatile("" : : : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" : : : "memory");
       }
-      w[(m + 1) & 1] = m + 1 < NN ? operand(slot, row_w + (m + 1) * 16) : operand(next, row_w);
-      const operand_t row = Unit<DT>::make(w[m & 1]);
+      w[(m + 1) & 1] = m + 1 < NN ? operand_w(slot, m + 1) : operand_w(next, 0);
+      const auto row = Unit<DT>::make(w[m & 1]);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         f32x4& sum = acc[(m + NN - 1) % NN][t];
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(m ? f[t] : before[t], d[t][e], sum[e]);
         d[t] = Unit<DT>::dot(row, x[t]);
-        if (m == NN - 1) x[t] = Unit<DT>::make(operand(next, row_x + t * 16));
-        const int done = (m + 1) % NN * NT + t;  // products since the barrier
+        if (m == NN - 1) x[t] = operand_x(next, t);
+        if constexpr (ONE_X) {
+          const int done = (m - 1) * NT + t;  // products since the second barrier
+          if (m > 0 && done % 2 == 0 && done / 2 <= LX + LW) fetch(done / 2 <= LX ? s + 1 : s + 2, free, done / 2);
+        } else {
+          const int done = (m + 1) % NN * NT + t;  // products since the barrier
 #pragma unroll
-        for (int i = done / kEvery * kPer; done % kEvery == 0 && i <= LX + LW && i < (done / kEvery + 1) * kPer; ++i)
-          if (m == NN - 1) fetch(s + STAGES, slot, i);
-          else fetch(s + STAGES - 1, free, i);
+          for (int i = done / kEvery * kPer; done % kEvery == 0 && i <= LX + LW && i < (done / kEvery + 1) * kPer; ++i)
+            if (m == NN - 1) fetch(s + STAGES, slot, i);
+            else fetch(s + STAGES - 1, free, i);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -483,9 +501,9 @@ uint64_t tiles(const ProductArgs& a, bool grouped) {
   const uint64_t n = rows * (((uint64_t)a.n + TN - 1) / TN);
   return (n + 7) / 8 * 8;  // whole rounds over the XCDs
 }
-template <int DT, bool GROUPED, int TT, int TN, int WT, int WN, int KG, int STAGES>
+template <int DT, bool GROUPED, int TT, int TN, int WT, int WN, int KG, int STAGES, bool ONE_X = false>
 int tiled(const ProductArgs& a, plora_stream stream) {
-  return launch(k_product<DT, TT, TN, WT, WN, KG, STAGES, GROUPED>, tiles<TT, TN>(a, GROUPED), 1, 1, a, stream, 64 * WT * WN * KG);
+  return launch(k_product<DT, TT, TN, WT, WN, KG, STAGES, ONE_X, GROUPED>, tiles<TT, TN>(a, GROUPED), 1, 1, a, stream, 64 * WT * WN * KG);
 }
 template <int DT, bool GROUPED, int NW, int WAVES, int P>
 int few(const ProductArgs& a, plora_stream stream) {
@@ -531,7 +549,7 @@ int product(const ProductArgs& a, plora_stream stream) {
     case 5: return tiled<DT, GROUPED, 128, 256, 2, 4, 1, 3>(a, stream);
     case 6: return tiled<DT, GROUPED, 256, 128, 4, 2, 1, 3>(a, stream);
     default:
-      if constexpr (kOf == 8) return tiled<DT, GROUPED, 256, 256, 4, 2, 1, 2>(a, stream);
+      if constexpr (kOf == 8) return tiled<DT, GROUPED, 256, 256, 4, 2, 1, 3, true>(a, stream);
       else return PLORA_ERR_INVAL;
   }
 }
