@@ -963,14 +963,22 @@ def plora_route(dtype, n_tokens, n_experts, top_k, logits, renormalise, scale, e
 
 _ELEMENTS = (PLORA_F16, PLORA_BF16, PLORA_F32)
 _EIGHT = ("torch.float8_e4m3fn", "torch.uint8")
+_NO_ROWS = (None, None, 0, 0)
+
+
+def _place_of(call, t, n_rows, width, dtype, device):
+    """(pointer, row stride) of a torch tensor [rows, width] (a row's elements one behind the other)."""
+    if t.shape != (n_rows, width) or _dtype_of(t) != dtype or t.get_device() != device:
+        raise PloraError(call, PLORA_ERR_INVAL)
+    row, element = t.stride()
+    if element != 1 and width > 1:
+        raise PloraError(call, PLORA_ERR_INVAL)
+    return t.data_ptr(), row if n_rows > 1 else -(-width // 8) * 8  # (one row may have any stride)
 
 
 def _matrix_of(call, t, n_rows, width, dtype, device):
-    """plora_matrix of a torch tensor [rows, width] (a row's elements one behind the other)."""
-    st = t.stride()
-    if t.shape != (n_rows, width) or (width > 1 and st[1] != 1) or _dtype_of(t) != dtype or t.get_device() != device:
-        raise PloraError(call, PLORA_ERR_INVAL)
-    return MatrixStruct(t.data_ptr(), st[0] if n_rows > 1 else -(-width // 8) * 8)  # (one row may have any stride)
+    """plora_matrix of such a tensor."""
+    return MatrixStruct(*_place_of(call, t, n_rows, width, dtype, device))
 
 
 def _two(call, t):
@@ -994,7 +1002,8 @@ class Fp8Rows:
         self.codes, self.scales = codes, scales  # kept alive
         self.n, self.k = n, k
         # (a tensor of one row or one block may have any stride there)
-        self.c = Fp8RowsStruct(codes.data_ptr(), scales.data_ptr(), codes.stride(0) if n > 1 else -(-k // 16) * 16, scales.stride(0) if blocks > 1 else n)
+        self.fields = (codes.data_ptr(), scales.data_ptr(), codes.stride(0) if n > 1 else -(-k // 16) * 16, scales.stride(0) if blocks > 1 else n)
+        self.c = Fp8RowsStruct(*self.fields)
 
     def quantise(self, x, activation=PLORA_ACT_NONE, stream=None):
         """Becomes x [rows, k]; with an activation x is [rows, 2k], the gate's half first."""
@@ -1113,9 +1122,10 @@ class NormWeights:
                 raise PloraError(call, PLORA_ERR_INVAL)
         self.c = NormWeightsStruct(None if weight is None else weight.data_ptr(), None if bias is None else bias.data_ptr(), eps, offset, int(center))
         self.at = C.addressof(self.c)
+        self.of = (self.kept[0].numel(), _dtype_of(self.kept[0]), self.kept[0].get_device()) if self.kept else None
 
     def fits(self, dim, dtype, device):
-        return not self.kept or (self.kept[0].numel() == dim and _dtype_of(self.kept[0]) == dtype and self.kept[0].get_device() == device)
+        return self.of is None or self.of == (dim, dtype, device)
 
 
 class BlockNorm:
@@ -1130,39 +1140,31 @@ class BlockNorm:
         call = "plora_norm"
         device = _device()
         dtype = _dtype_of(block)
-        n, dim = _two(call, block)
-        if dtype not in _ELEMENTS:
-            raise PloraError(call, PLORA_ERR_INVAL)
-        top_k, block_rows = 0, n
+        rows, dim = _two(call, block)
+        n, top_k, block_rows, at, weights_at = rows, 0, 0, None, None
         if places is not None:
             n, top_k = _two(call, places)
+            block_rows, at = rows, _ints_of(call, places, n * top_k, device)
             if place_weights is None or place_weights.shape != (n, top_k) or str(place_weights.dtype) != "torch.float32" or \
                     not place_weights.is_contiguous() or place_weights.get_device() != device:
                 raise PloraError(call, PLORA_ERR_INVAL)
+            weights_at = place_weights.data_ptr()
         elif place_weights is not None:
             raise PloraError(call, PLORA_ERR_INVAL)
-        for p in (self.pre, self.post):
-            if p is not None and not p.fits(dim, dtype, device):
-                raise PloraError(call, PLORA_ERR_INVAL)
-        if out8 is not None and (out8.device != device or out8.n != n or out8.k != dim):
+        pre, post = self.pre, self.post
+        if dtype not in _ELEMENTS or (pre is not None and not pre.fits(dim, dtype, device)) or (post is not None and not post.fits(dim, dtype, device)) or \
+                (out8 is not None and (out8.device != device or out8.n != n or out8.k != dim)):
             raise PloraError(call, PLORA_ERR_INVAL)
-
         if gate is not None and gate.dim() == 1:
             gate = gate.expand(n, dim)
-        parts = []
-        for t, rows in ((block, block_rows), (gate, n), (residual, n), (hidden, n), (out, n)):
-            if t is None:
-                parts += (None, 0)
-                continue
-            st = t.stride()
-            if t.shape != (rows, dim) or st[1] != 1 or _dtype_of(t) != dtype or t.get_device() != device:
-                raise PloraError(call, PLORA_ERR_INVAL)
-            parts += (t.data_ptr(), st[0] if rows > 1 else dim)
-        e = None if out8 is None else out8.c
-        args = BlockNormStruct(dtype, n, dim, self.scale, parts[0], parts[1], None if places is None else _ints_of(call, places, n * top_k, device),
-                               None if places is None else place_weights.data_ptr(), top_k, block_rows if places is not None else 0,
-                               None if self.post is None else self.post.at, None if self.pre is None else self.pre.at, *parts[2:],
-                               *((None, None, 0, 0) if e is None else (e.codes, e.scales, e.code_stride, e.scale_stride)))
+        b, bs = _place_of(call, block, rows, dim, dtype, device)
+        g, gs = (None, 0) if gate is None else _place_of(call, gate, n, dim, dtype, device)
+        r, rs = (None, 0) if residual is None else _place_of(call, residual, n, dim, dtype, device)
+        h, hs = (None, 0) if hidden is None else _place_of(call, hidden, n, dim, dtype, device)
+        o, os_ = (None, 0) if out is None else _place_of(call, out, n, dim, dtype, device)
+        c, s, cs, ss = _NO_ROWS if out8 is None else out8.fields
+        args = BlockNormStruct(dtype, n, dim, self.scale, b, bs, at, weights_at, top_k, block_rows, None if post is None else post.at,
+                               None if pre is None else pre.at, g, gs, r, rs, h, hs, o, os_, c, s, cs, ss)
         rc = lib.plora_norm(args, stream)
         if rc:
             _check(call, rc)
