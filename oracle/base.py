@@ -1,4 +1,5 @@
-"""The base layer's operators in numpy, from their formulas: rows and weights in 8 bits, products, routing, norms between blocks.
+"""CPU oracle of the base layer's operators (TEST INFRASTRUCTURE ONLY; shares nothing with the library), from their formulas: rows and weights in 8 bits,
+products, routing, norms between blocks.
 
 What a choice of codes is decided by (quotients, products, the rounding) is computed in 32 bits with one rounding per operation, as the
 library's contract has it; everything else in 64 bits.

@@ -40,8 +40,8 @@ __device__ __forceinline__ i32x4 buffer_at(const uint8_t* p) {
 __device__ __forceinline__ void load_to_lds(i32x4 buffer, uint32_t offset, uint32_t uniform, uint32_t dst) {
   asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" : : "v"(offset), "s"(buffer), "s"(uniform), "s"(dst) : "memory", "m0");
 }
-__device__ __forceinline__ void load_word_to_lds(i32x4 buffer, uint32_t offset, uint32_t dst) {  // 4 bytes per lane
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" : : "v"(offset), "s"(buffer), "s"(dst) : "memory", "m0");
+__device__ __forceinline__ void load_word_to_lds(const float* from, uint32_t dst) {  // 4 bytes per lane
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(from), "s"(dst) : "memory", "m0");
 }
 #pragma clang diagnostic pop
 template <int N>
@@ -178,8 +178,11 @@ __device__ __forceinline__ void st4(uint8_t* p, f32x4 f) {
 // of 4 row tiles 950 (of 8: 961); one stage of x, three of weights 943 (experts' prompts: 350 -> 336).  Not kept: weights two rows ahead
 // (973), 32 x 32 x 64 instructions (registers spill: 2032), 4 wavefronts of 128 x 128 (1196), lines asked for 4 stages ahead (1040), wave
 // priorities (952).
-// Smaller tiles are bound by how fast a CU gets its operands (0.5 - 0.6 us for 24 - 32 KiB of a 128 x 64 or 128 x 128 block, with two blocks a
-// barrier as well); two sets of wavefronts where there are few tiles.
+// Smaller tiles are bound by how fast a CU gets operands that are not in its L2: with no products and no LDS reads at all, 512 x 4096 x 4096 takes
+// 17.7 us of 18.3 (14.2 from L2, which alone feeds a CU with 140 - 150 GB/s; from memory it gets 40 - 60).  Two blocks a barrier, five or six stages, all
+// operands of a stage in registers a stage ahead, and tiles that begin at different blocks change nothing or cost up to 10 %; two sets of
+// wavefronts where there are few tiles.  Scales come through LDS as well: a scalar load in flight makes each wait for an LDS read wait for it
+// too (1024 x 1024 x 4096: 12.5 -> 11.1 us; 2048 x 5120 x 13824: 173 -> 167).
 template <int DT, int TT, int TN, int WT, int WN, int KG, int STAGES, bool ONE_X, bool GROUPED>
 __global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_eu(2))) void k_product(ProductArgs a) {
   constexpr int WAVES = WT * WN, NT = TT / WT / 16, NN = TN / WN / 16;
@@ -190,6 +193,7 @@ __global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_
   constexpr int kAtW = kSlotsX * kX, kAtScales = kAtW + STAGES * kW, kSet = kAtScales + kSlotsX * kScales;  // of a set's LDS: x, weights, scales
   static_assert(LX * 8 * WAVES == TT && LW * 8 * WAVES == TN && WAVES % 2 == 0 && NN % 2 == 0 && NT <= 4, "whole loads");
   static_assert(TN / WN <= kBlock && kBlock % (TN / WN) == 0, "one scale of weights a wavefront");
+  static_assert(NT < 4 || WN > 1, "a second wavefront for the weights' scales");
   static_assert(ONE_X || (LX + LW) / kPer * kEvery < NN * NT, "all loads of a stage are sent between two barriers");
   static_assert(!ONE_X || (KG == 1 && STAGES == 3 && 2 * (LX + 1 + LW) <= (NN - 2) * NT), "and between the second barrier and the next stage's first");
   static_assert((KG - 1) * TT * TN * 4 <= KG * kSet, "the sums are joined in the stages' place");
@@ -220,27 +224,29 @@ __global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_
     const int32_t r = tile.first + wt * (TT / WT) + t * 16 + col;
     return x_row(a, r < tile.last ? r : tile.last - 1);
   };
+  const int channel = tile.channel + wn * (TN / WN);  // the wavefront's first one
+  // One load of 64 words a stage brings a wavefront's scales: a row of x a lane, and by its last 16 lanes the weights' one; with 64 rows a wavefront the
+  // first wavefront of those rows has the rows', the second one the weights' of all (lane l: of wavefront column l % WN).
+  const bool of_w = NT < 4 ? quad == 3 : wn > 0;
   const int32_t scale_row = row_of(quad % NT);
-  const uint32_t scale_at = scale_row < 0 ? 0 : (uint32_t)(scale_row - first_row) * 4;
+  const int nb = (a.n + kBlock - 1) / kBlock, cb = (NT < 4 ? channel : tile.channel + lane % WN * (TN / WN)) / kBlock, b0 = set < kb ? set : kb - 1;
+  const float* scale = of_w ? a.ws + ((int64_t)tile.expert * nb + (cb < nb ? cb : nb - 1)) * kb + b0 : a.xs + (scale_row < 0 ? 0 : scale_row) + b0 * a.xs_s;
+  const int64_t scale_step = KG * (of_w ? 1 : a.xs_s);
   const uint8_t* mine = lds + set * kSet;
   const uint32_t to = __builtin_amdgcn_readfirstlane(lds_addr(mine) + wave * 1024), scales_to = __builtin_amdgcn_readfirstlane(lds_addr(mine) + kAtScales + wave * 256);
-  // Load i of the set's step s: LX of x, the wavefront's scales of x, LW of weights.  Behind the last code of the rows, and behind the last block: zeros.
+  // Load i of the set's step s: LX of x, the wavefront's scales of x, LW of weights.  Behind the last code of the rows, and behind the last block: zeros (of scales the
+  // last block's again).
   const auto fetch = [&](int s, int slot, int i) {
     const int b = s * KG + set;
     if (i == LX) {
-      const i32x4 bs = buffer_at(reinterpret_cast<const uint8_t*>(a.xs + first_row + (int64_t)(b < kb ? b : 0) * a.xs_s));
-      load_word_to_lds(bs, b < kb ? scale_at : kNowhere, scales_to + (ONE_X ? 0 : slot) * kScales);
+      load_word_to_lds(scale, scales_to + (ONE_X ? 0 : slot) * kScales);
+      scale += b + KG < kb ? scale_step : 0;
     } else {
       const int l = i < LX ? i : i - 1;
       const uint32_t dst = i < LX ? to + (ONE_X ? 0 : slot) * kX + l * WAVES * 1024 : to + kAtW + slot * kW + (l - LX) * WAVES * 1024;
       load_to_lds(i < LX ? bx : bw, b * kBlock + piece * 16 < a.k ? at[l] : kNowhere, b * kBlock, dst);
     }
   };
-  const int channel = tile.channel + wn * (TN / WN);  // the wavefront's first one
-  const int nb = (a.n + kBlock - 1) / kBlock, cb = channel / kBlock;
-  typedef const __attribute__((address_space(4))) float* scalar_floats;
-  const scalar_floats sw = (scalar_floats)(uintptr_t)(a.ws + ((int64_t)tile.expert * nb + (cb < nb ? cb : nb - 1)) * kb);
-
   const auto operand = [&](const uint8_t* rows, int row) {
     const uint8_t* p = rows + row * kBlock;
     const int s = (row >> 1) & 7;
@@ -264,10 +270,12 @@ __global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_
   f32x4 acc[NN][NT] = {}, d[NT] = {};
   typename Unit<DT>::operand x[NT];
   i32x8 w[2];
-  float f[NT] = {}, fx[NT];
+  float f[NT] = {}, fx[NT], fw;
   const auto scales = [&](int slot) {
+    const uint8_t* p = mine + kAtScales + (ONE_X ? 0 : slot) * kScales;
+    fw = *reinterpret_cast<const float*>(p + (NT < 4 ? wave * 64 + 48 : (wt + WT) * 64 + wn) * 4);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) fx[t] = *reinterpret_cast<const float*>(mine + kAtScales + (ONE_X ? 0 : slot) * kScales + wave * 256 + (t * 16 + col) * 4);
+    for (int t = 0; t < NT; ++t) fx[t] = *reinterpret_cast<const float*>(p + ((NT < 4 ? wave : wt) * 64 + t * 16 + col) * 4);
   };
   w[0] = operand_w(0, 0);
 #pragma unroll
@@ -279,12 +287,11 @@ __global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_
   int slot = 0;
   for (int s = 0; s < steps; ++s) {
     const int b = s * KG + set, next = slot + 1 < STAGES ? slot + 1 : 0, free = slot > 0 ? slot - 1 : STAGES - 1;
-    const float fw = b < kb ? sw[b < kb ? b : 0] : 0.f;
     float before[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       before[t] = f[t];
-      f[t] = fx[t] * fw;
+      f[t] = b < kb ? fx[t] * fw : 0.f;
     }
 #pragma unroll
     for (int m = 0; m < NN; ++m) {
