@@ -580,25 +580,33 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_place(RouteArgs a) {
   __shared__ uint32_t bits[kMostExperts][2];
   __shared__ int16_t chosen[kChunk * kMostChoices];
   __shared__ int base[kMostExperts], total_of[kMostExperts], waves[kRouteThreads / 64];
-  const int chunk = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int kCounts = kChunk / kCounted, kMine = kChunk * kMostChoices / kRouteThreads;
+  const int chunk = blockIdx.x, col = threadIdx.x & 15;
   const int64_t first = (int64_t)chunk * kChunk * a.top_k, all = (int64_t)a.n_tokens * a.top_k;
-  bits[threadIdx.x][0] = bits[threadIdx.x][1] = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < kChunk * a.top_k && first + i < all; i += kRouteThreads) {
-    const int e = a.experts[first + i], t = i / a.top_k;
-    chosen[i] = (int16_t)e;
-    if (e >= 0) atomicOr(&bits[e][t >> 5], 1u << (t & 31));
-  }
-  constexpr int kCounts = kChunk / kCounted;
-  if (a.n_counts <= kFewCounts) {  // a wavefront an expert, a lane a count
-    for (int e = wave; e < a.n_experts; e += kRouteThreads / 64) {
-      int n = lane < a.n_counts ? a.counts[(int64_t)e * a.n_counts + lane] : 0, ahead = lane < chunk * kCounts ? n : 0;
+  int mine[kMine];  // the choices are on their way together with the counts
 #pragma unroll
-      for (int i = 1; i < 64; i *= 2) {
+  for (int h = 0; h < kMine; ++h) {
+    const int i = threadIdx.x + h * kRouteThreads;
+    mine[h] = i < kChunk * a.top_k && first + i < all ? a.experts[first + i] : -1;
+  }
+  bits[threadIdx.x][0] = bits[threadIdx.x][1] = 0;
+  if (a.n_counts <= kFewCounts) {  // 16 lanes an expert
+#pragma unroll 4
+    for (int e0 = 0; e0 < a.n_experts; e0 += kRouteThreads / 16) {
+      const int e = e0 + (threadIdx.x >> 4);
+      int n = 0, ahead = 0;
+#pragma unroll
+      for (int j = 0; j < kFewCounts / 16; ++j) {
+        const int i = col + 16 * j, c = e < a.n_experts && i < a.n_counts ? a.counts[(int64_t)e * a.n_counts + i] : 0;
+        n += c;
+        ahead += i < chunk * kCounts ? c : 0;
+      }
+#pragma unroll
+      for (int i = 1; i < 16; i *= 2) {
         n += __shfl_xor(n, i);
         ahead += __shfl_xor(ahead, i);
       }
-      if (lane == 0) {
+      if (col == 0 && e < a.n_experts) {
         base[e] = ahead;
         total_of[e] = n;
       }
@@ -608,6 +616,12 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_place(RouteArgs a) {
     total_of[threadIdx.x] = a.totals[threadIdx.x];
   }
   __syncthreads();
+#pragma unroll
+  for (int h = 0; h < kMine; ++h) {
+    const int i = threadIdx.x + h * kRouteThreads;
+    if (i < kChunk * a.top_k) chosen[i] = (int16_t)mine[h];
+    if (mine[h] >= 0) atomicOr(&bits[mine[h]][i / a.top_k >> 5], 1u << (i / a.top_k & 31));
+  }
   const int e = threadIdx.x;
   int total;
   const int start = scan1024(e < a.n_experts ? total_of[e] : 0, waves, total);
