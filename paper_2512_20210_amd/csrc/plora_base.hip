@@ -442,6 +442,18 @@ __device__ __forceinline__ int ordered(float v) {
   return v > -INFINITY ? b ^ ((b >> 31) & 0x7fffffff) : kNone;
 }
 __device__ __forceinline__ float value_of(int key) { return __int_as_float(key ^ ((key >> 31) & 0x7fffffff)); }
+// A 16-bit logit's lowest 13 bits as fp32 are zeros, so its expert goes there (the lowest one is the largest): then no two are alike, and the largest
+// number of a row says both, in half the instructions of a choice (64 tokens of 64 experts, 6 each: 5.9 -> 5.1 us; 16k of 256, 8 each: 22.0 -> 20.3).
+constexpr int kIndex = (1 << 13) - 1;
+template <int DT>
+struct Keys {
+  static constexpr bool INDEXED = DT != PLORA_F32;
+  static __device__ __forceinline__ int of(float v, int e) {
+    const int k = ordered(v);
+    return INDEXED && k != kNone ? (k & ~kIndex) | (kIndex - e) : k;
+  }
+  static __device__ __forceinline__ float value(int k) { return value_of(INDEXED ? (k & ~kIndex) | ((k >> 31) & kIndex) : k); }
+};
 template <int CTRL>
 __device__ __forceinline__ int dpp_max(int v) {
   const int o = __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false);
@@ -477,7 +489,7 @@ __global__ __launch_bounds__(THREADS) void k_route_choose(RouteArgs a) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       nan |= v[i] != v[i];
-      key[i] = ordered(v[i]);
+      key[i] = Keys<DT>::of(v[i], col + 16 * i);
     }
   }
   const auto most = [&]() {
@@ -488,19 +500,24 @@ __global__ __launch_bounds__(THREADS) void k_route_choose(RouteArgs a) {
   };
   int m = most();
   const int top = m;
-  const bool bad = row_max(nan ? 1 : 0) > 0 || value_of(top) == INFINITY;
+  const float most_of_all = Keys<DT>::value(top);
+  const bool bad = row_max(nan ? 1 : 0) > 0 || most_of_all == INFINITY;
   float sum = 0.f;
   if (!a.renormalise) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) sum += key[i] == kNone ? 0.f : expf(value_of(key[i]) - value_of(top));
+    for (int i = 0; i < V; ++i) sum += key[i] == kNone ? 0.f : expf(Keys<DT>::value(key[i]) - most_of_all);
     sum = sum16(sum);
   }
   int expert[2] = {-1, -1}, mine[2] = {kNone, kNone};  // lane c: choices c and c + 16 and their logits
   for (int j = 0; j < a.top_k; ++j) {
     int at = 16 * V;  // the lowest expert with the largest logit
+    if constexpr (Keys<DT>::INDEXED) {
+      at = kIndex - (m & kIndex);
+    } else {
 #pragma unroll
-    for (int i = V - 1; i >= 0; --i) at = key[i] == m ? col + 16 * i : at;
-    at = -row_max(-at);
+      for (int i = V - 1; i >= 0; --i) at = key[i] == m ? col + 16 * i : at;
+      at = -row_max(-at);
+    }
     if (m == kNone) at = -1;
     if (col == (j & 15)) {
       if (j < 16) {
@@ -513,12 +530,12 @@ __global__ __launch_bounds__(THREADS) void k_route_choose(RouteArgs a) {
     }
     const int own = (at & 15) == col ? at >> 4 : -1;  // (-1 >> 4: none)
 #pragma unroll
-    for (int i = 0; i < V; ++i) key[i] = own == i ? kNone : key[i];
+    for (int i = 0; i < V; ++i) key[i] = (Keys<DT>::INDEXED ? key[i] == m : own == i) ? kNone : key[i];
     m = most();
   }
   float p[2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) p[h] = mine[h] == kNone ? 0.f : expf(value_of(mine[h]) - value_of(top));
+  for (int h = 0; h < 2; ++h) p[h] = mine[h] == kNone ? 0.f : expf(Keys<DT>::value(mine[h]) - most_of_all);
   if (a.renormalise) sum = sum16(p[0] + p[1]);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
