@@ -459,14 +459,31 @@ __device__ __forceinline__ int dpp_max(int v) {
   const int o = __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false);
   return v > o ? v : o;
 }
+template <int CTRL>
+__device__ __forceinline__ int dpp_sum(int v) {
+  return v + __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false);
+}
+__device__ __forceinline__ int row_sum(int v) { return dpp_sum<0x121>(dpp_sum<0x122>(dpp_sum<0x124>(dpp_sum<0x128>(v)))); }
 __device__ __forceinline__ int row_max(int v) { return dpp_max<0x121>(dpp_max<0x122>(dpp_max<0x124>(dpp_max<0x128>(v)))); }
 
-// A wavefront has four tokens, 16 lanes each; a lane has the logits of experts c, c + 16, ... of its token.  The number of vector instructions of a
+template <int DT>
+__device__ __forceinline__ void ld4(const uint8_t* p, float* f) {
+  if constexpr (DT == PLORA_F32) {
+    *reinterpret_cast<f32x4*>(f) = *reinterpret_cast<const f32x4*>(p);
+  } else {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    const uint8_t* q = reinterpret_cast<const uint8_t*>(&u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = ld1<DT>(q, i);
+  }
+}
+
+// A wavefront has four tokens, 16 lanes each; a lane has the logits of 8 neighbouring experts of each 128 (of up to 64: 4).  The number of vector instructions of a
 // choice bounds it, and here four tokens share them (16k tokens, 8 of 256 experts: 19 us with a wavefront a token, 14 so).  THREADS =
 // 1024: the call's one chunk of 64 tokens, which is sorted as well; 256: 16 tokens and their counts.
 template <int DT, int V, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_route_choose(RouteArgs a) {
-  constexpr int TOK = THREADS / 16, WORDS = (TOK + 31) / 32;
+  constexpr int TOK = THREADS / 16, WORDS = (TOK + 31) / 32, G = V < 8 ? V : 8;
   constexpr bool ONE = TOK == kChunk;
   static_assert(ONE || TOK == kCounted, "one chunk, or as many tokens as are counted together");
   __shared__ uint32_t bits[16 * V][WORDS];
@@ -475,21 +492,28 @@ __global__ __launch_bounds__(THREADS) void k_route_choose(RouteArgs a) {
   const int col = threadIdx.x & 15, slot = threadIdx.x >> 4;
   const int64_t t = (int64_t)blockIdx.x * TOK + slot;
   const bool live = t < a.n_tokens;
+  const auto expert_of = [&](int i) { return i / G * 16 * G + col * G + i % G; };
   int key[V];
   bool nan = false;
   {
     float v[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int e = col + 16 * i;
-      v[i] = live && e < a.n_experts ? ld1<DT>(a.logits, t * a.stride + e) : -INFINITY;
+    for (int i = 0; i < V; i += G) {
+      const uint8_t* p = a.logits + (t * a.stride + expert_of(i)) * Elt<DT>::B;
+      if (live && expert_of(i) + G <= a.n_experts) {
+        if constexpr (G == 8) ld8<DT>(p, v + i);
+        else ld4<DT>(p, v + i);
+      } else {
+#pragma unroll
+        for (int j = 0; j < G; ++j) v[i + j] = live && expert_of(i + j) < a.n_experts ? ld1<DT>(p, j) : -INFINITY;
+      }
     }
     for (int i = threadIdx.x; i < 16 * V * WORDS; i += THREADS) (&bits[0][0])[i] = 0;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       nan |= v[i] != v[i];
-      key[i] = Keys<DT>::of(v[i], col + 16 * i);
+      key[i] = Keys<DT>::of(v[i], expert_of(i));
     }
   }
   const auto most = [&]() {
@@ -515,7 +539,7 @@ __global__ __launch_bounds__(THREADS) void k_route_choose(RouteArgs a) {
       at = kIndex - (m & kIndex);
     } else {
 #pragma unroll
-      for (int i = V - 1; i >= 0; --i) at = key[i] == m ? col + 16 * i : at;
+      for (int i = V - 1; i >= 0; --i) at = key[i] == m ? expert_of(i) : at;
       at = -row_max(-at);
     }
     if (m == kNone) at = -1;
@@ -528,7 +552,7 @@ __global__ __launch_bounds__(THREADS) void k_route_choose(RouteArgs a) {
         mine[1] = m;
       }
     }
-    const int own = (at & 15) == col ? at >> 4 : -1;  // (-1 >> 4: none)
+    const int own = at >= 0 && (at / G & 15) == col ? at / (16 * G) * G + at % G : -1;
 #pragma unroll
     for (int i = 0; i < V; ++i) key[i] = (Keys<DT>::INDEXED ? key[i] == m : own == i) ? kNone : key[i];
     m = most();
@@ -608,7 +632,6 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_place(RouteArgs a) {
   }
   bits[threadIdx.x][0] = bits[threadIdx.x][1] = 0;
   if (a.n_counts <= kFewCounts) {  // 16 lanes an expert
-#pragma unroll 4
     for (int e0 = 0; e0 < a.n_experts; e0 += kRouteThreads / 16) {
       const int e = e0 + (threadIdx.x >> 4);
       int n = 0, ahead = 0;
@@ -618,11 +641,8 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_place(RouteArgs a) {
         n += c;
         ahead += i < chunk * kCounts ? c : 0;
       }
-#pragma unroll
-      for (int i = 1; i < 16; i *= 2) {
-        n += __shfl_xor(n, i);
-        ahead += __shfl_xor(ahead, i);
-      }
+      n = row_sum(n);
+      ahead = row_sum(ahead);
       if (col == 0 && e < a.n_experts) {
         base[e] = ahead;
         total_of[e] = n;
