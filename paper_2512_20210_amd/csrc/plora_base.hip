@@ -403,15 +403,22 @@ struct RouteArgs {
 __device__ __forceinline__ int bits_below(const uint32_t* w, int t) {
   return t < 32 ? __popc(w[0] & ((1u << t) - 1)) : __popc(w[0]) + __popc(w[1] & ((1u << (t - 32)) - 1));
 }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_from(int v) {  // 0 where there is no lane to take from, and in rows that are not in ROWS
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_scan(int v) {  // the sum up to and with this lane
+  v += dpp_from<0x111, 0xf>(v);
+  v += dpp_from<0x112, 0xf>(v);
+  v += dpp_from<0x114, 0xf>(v);
+  v += dpp_from<0x118, 0xf>(v);
+  v += dpp_from<0x142, 0xa>(v);  // the last lane of a row to the next one
+  return v + dpp_from<0x143, 0xc>(v);  // and of half a wavefront
+}
 // Sum of v over the threads ahead of this one, and over all 1024 of them.
 __device__ __forceinline__ int scan1024(int v, int* waves, int& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int s = v;
-#pragma unroll
-  for (int i = 1; i < 64; i *= 2) {
-    const int o = __shfl_up(s, i);
-    if (lane >= i) s += o;
-  }
+  const int s = wave_scan(v);
   if (lane == 63) waves[wave] = s;
   __syncthreads();
   int ahead = 0;
@@ -596,12 +603,7 @@ __global__ __launch_bounds__(kThreads) void k_route_scan(RouteArgs a) {
   for (int at = 0; at < a.n_counts; at += kThreads) {
     const int i = at + threadIdx.x;
     const int v = i < a.n_counts ? c[i] : 0;
-    int s = v;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-      const int u = __shfl_up(s, o);
-      if (lane >= o) s += u;
-    }
+    int s = wave_scan(v);
     if (lane == 63) waves[wave] = s;
     __syncthreads();
     int all = 0;
