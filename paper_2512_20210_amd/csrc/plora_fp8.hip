@@ -404,7 +404,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 
   struct Block {
     i32x8 w[NW], x[NT];
-    float f[NT];
+    float fx[NT], fw;  // multiplied where they are used: a product here would wait for all of the block's loads
   };
   const auto load = [&](int b, Block& o) {
     // pieces behind the last code, and blocks behind the last one: the first piece of the row in their place, and x's codes zeroed
@@ -415,47 +415,63 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 #pragma unroll
     for (int m = 0; m < NW; ++m) o.w[m] = both(pw[m]);
     const int at = b < kb ? b : kb - 1;
-    const float fw = sw[at];
+    o.fw = sw[at];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       o.x[t] = both(px[t]);
-      o.f[t] = sx[t][(int64_t)at * a.xs_s] * fw;
+      o.fx[t] = sx[t][(int64_t)at * a.xs_s];
     }
   };
   f32x4 acc[NW][NT] = {};
   Block ring[P];
+  const auto use = [&](Block& o) {
 #pragma unroll
-  for (int p = 0; p < P; ++p)
-    if (p == 0 || wave + p * WAVES < kb) load(wave + p * WAVES, ring[p]);
-  for (int b = wave; b < kb; b += P * WAVES) {
+    for (int t = 0; t < NT; ++t) {
+      const float f = o.fx[t] * o.fw;
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int at = b + p * WAVES;
-      Block now = ring[p];
-      if (at + P * WAVES < kb) load(at + P * WAVES, ring[p]);
-      if (at < kb) {
-        const bool tail = (at + 1) * kBlock > a.k;
+      for (int m = 0; m < NW; ++m) {
+        const f32x4 d = Unit<DT>::dot(Unit<DT>::make(o.w[m]), Unit<DT>::make(o.x[t]));
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          if (tail) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (at * kBlock + (e < 4 ? 0 : 64) + quad * 16 >= a.k) now.x[t][e] = 0;
-          }
-#pragma unroll
-          for (int m = 0; m < NW; ++m) {
-            if (tail) {
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (at * kBlock + (e < 4 ? 0 : 64) + quad * 16 >= a.k) now.w[m][e] = 0;
-            }
-            const f32x4 d = Unit<DT>::dot(Unit<DT>::make(now.w[m]), Unit<DT>::make(now.x[t]));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[m][t][e] = __builtin_fmaf(now.f[t], d[e], acc[m][t][e]);
-          }
-        }
+        for (int e = 0; e < 4; ++e) acc[m][t][e] = __builtin_fmaf(f, d[e], acc[m][t][e]);
       }
     }
+  };
+  const auto use_last = [&](int b, Block& o) {  // with the codes behind k zeroed
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool there = b * kBlock + (e < 4 ? 0 : 64) + quad * 16 < a.k;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) o.x[t][e] = there ? o.x[t][e] : 0;
+#pragma unroll
+      for (int m = 0; m < NW; ++m) o.w[m][e] = there ? o.w[m][e] : 0;
+    }
+    use(o);
+  };
+  int b = wave;
+  if (b + (2 * P - 1) * WAVES < kb) {
+    // no branch in here, and none ahead of it that not all loads are behind: the waits would be for all loads under way
+#pragma unroll
+    for (int p = 0; p < P; ++p) load(b + p * WAVES, ring[p]);
+    do {
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        use(ring[p]);
+        __builtin_amdgcn_sched_barrier(0);  // (else all uses would be ahead of all loads)
+        load(b + (P + p) * WAVES, ring[p]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      b += P * WAVES;
+    } while (b + (2 * P - 1) * WAVES < kb);
+  } else {
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      if (p == 0 || b + p * WAVES < kb) load(b + p * WAVES, ring[p]);
+  }
+#pragma unroll
+  for (int p = 0; p < 2 * P - 1; ++p) {
+    const int at = b + p * WAVES;
+    if (at < kb) use_last(at, ring[p % P]);
+    if (p < P - 1 && at + P * WAVES < kb) load(at + P * WAVES, ring[p]);
   }
 #pragma unroll
   for (int m = 0; m < NW; ++m)
@@ -541,7 +557,7 @@ int product(const ProductArgs& a, plora_stream stream) {
     switch (best_of<3>(kFew, a, GROUPED)) {
       case 0: return few<DT, GROUPED, 1, 8, 2>(a, stream);
       case 1: return few<DT, GROUPED, 2, 8, 2>(a, stream);
-      default: return few<DT, GROUPED, 4, 4, 1>(a, stream);
+      default: return few<DT, GROUPED, 4, 4, 2>(a, stream);
     }
   }
   static constexpr Kind kTiles[] = {{64, 32, 2, 1, 1.85f, 0.379f, 0.f},  {64, 64, 2, 1, 1.79f, 0.525f, 0.f},   {64, 64, 1, 2, 0.99f, 0.295f, 0.234f}, {128, 64, 1, 1, 2.07f, 0.421f, 0.f},
