@@ -376,6 +376,9 @@ __global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_
 // Few rows: a workgroup has TT rows x 16 NW channels, and its WAVES wavefronts the blocks of 128 values in turn; operands go from memory to registers,
 // P of a wavefront's blocks ahead, with no barrier until the wavefronts' sums are joined in LDS (in their order: the sums do not depend
 // on which is done first).
+// Memory bounds it: 64 experts of 2816 x 2048 with 6 rows each read 5.4 TB/s (67 us). Not kept: a workgroup with 128 channels, which goes through them
+// with x in registers, the next ones' weights on their way and a join a step (78); x in LDS and wavefronts that read their channels on their
+// own, 2 to 8 blocks ahead and with nothing to join (69 - 75).
 template <int DT, int TT, int NW, int WAVES, int P, bool GROUPED>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void k_few(ProductArgs a) {
   constexpr int NT = TT / 16;
@@ -557,7 +560,9 @@ int product(const ProductArgs& a, plora_stream stream) {
     switch (best_of<3>(kFew, a, GROUPED)) {
       case 0: return few<DT, GROUPED, 1, 8, 2>(a, stream);
       case 1: return few<DT, GROUPED, 2, 8, 2>(a, stream);
-      default: return few<DT, GROUPED, 4, 4, 2>(a, stream);
+      default:  // less than 3 blocks for each of 4 wavefronts: two of them (256 experts of 4096 x 512, 512 rows: 134 -> 96 us; 128 of 2048 x 768: 45.3 -> 41.4)
+        if (a.k <= 11 * kBlock) return few<DT, GROUPED, 4, 2, 2>(a, stream);
+        return few<DT, GROUPED, 4, 4, 2>(a, stream);
     }
   }
   static constexpr Kind kTiles[] = {{64, 32, 2, 1, 1.85f, 0.379f, 0.f},  {64, 64, 2, 1, 1.79f, 0.525f, 0.f},   {64, 64, 1, 2, 0.99f, 0.295f, 0.234f}, {128, 64, 1, 1, 2.07f, 0.421f, 0.f},

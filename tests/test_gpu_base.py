@@ -281,6 +281,19 @@ def test_grouped(dtype, gather, sizes, n, k):
             check_product(got[r][None], xv[src][None], wv[e], dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("t,n,k", [(7, 520, 13840), (16, 16392, 2576), (3, 32776, 1040), (12, 32776, 144)])
+def test_few_rows_of_many_blocks_or_channels(dtype, t, n, k):
+    test_product(dtype, t, n, k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("k", [16, 528, 1408, 1424])
+def test_many_experts_of_few_blocks(dtype, k):
+    """Two wavefronts share K up to 1408 values, then four."""
+    test_grouped(dtype, k != 528, [int(v) for v in np.random.default_rng(k).integers(0, 10, 40)], 1032, k)
+
+
 @pytest.mark.parametrize("offsets", [[0, -5, 40, 1000, 90], [-3, -1, 0, 0, 5], [10, 20, 20, 30, 2000000000], [50, 40, 30, 20, 10]])
 def test_offsets_out_of_range(offsets):
     """Each is held to the rows there are; a group that ends ahead of its start is empty."""
