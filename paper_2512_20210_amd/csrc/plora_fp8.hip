@@ -500,24 +500,29 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 
 // ---- host side ----------------------------------------------------------------------------------------
 
-// A kernel's tile, and what it takes by a fit to calls of 1 .. 4096 rows times weights of 520 x 1040 .. 13824 x 5120 (and 2 .. 256 experts): 3 us and, for each
-// round of a CU, `fixed` and for every step (KG blocks of 128 values) `step`, with `more` for each further workgroup that
-// runs on the CU beside it, of `at_once`.  All in us.
+// A kernel's tile, and what it takes by a fit to calls of 1 .. 4096 rows times weights of 520 x 1040 .. 13824 x 5120 (and 2 .. 256 experts): for each round of
+// a CU `fixed` and for every step (KG blocks of 128 values) `step`, with `more` for each further workgroup that runs on the CU beside it, of
+// `at_once`; all in us.  Beside that the weights are read, with 5.3 TB/s where workgroups overlap on a CU and 4.4 where not; the two as a
+// root of squares (16 experts of 4096 x 13824, 512 rows of uneven groups: 253 -> 203 us; 8 of 7168 x 4096, 800 rows: 115 -> 78; 256 of 4096 x 512, 4096 rows: 256 -> 164).
 struct Kind {
   int tt, tn, kg, at_once;
   float fixed, step, more;
 };
 float time_of(const Kind& k, const ProductArgs& a, bool grouped) {
-  float rows = (float)((a.n_rows + (int64_t)k.tt - 1) / k.tt);
-  if (grouped) {  // groups end in a part of a tile, half of one on average; few rows leave some experts without any
-    const float groups = (float)(a.n_experts < a.n_rows ? a.n_experts : a.n_rows), least = 0.8f * groups;
-    rows = (float)(a.n_rows / k.tt) + 0.5f * groups;
-    rows = rows > least && a.n_rows > k.tt * groups * 0.5f ? rows : least;
+  float rows = (float)((a.n_rows + (int64_t)k.tt - 1) / k.tt), there = 1.f;
+  if (grouped) {  // groups of random sizes: of n rows or more with a probability of q^n
+    const float q = (float)a.n_rows / (float)((int64_t)a.n_rows + a.n_experts);
+    float none = q;
+    for (int i = 1; i < k.tt; i *= 2) none *= none;
+    there = q * (float)a.n_experts;
+    rows = there / (1.f - none) + 0.15f * sqrtf((float)a.n_experts);  // (a tile more than there are CUs costs a round, one less saves nothing)
   }
   const float steps = (float)(((a.k + kBlock - 1) / kBlock + k.kg - 1) / k.kg);
   const int64_t here = ((int64_t)(rows * (float)((a.n + k.tn - 1) / k.tn)) + 255) / 256, rounds = here / k.at_once, rest = here - rounds * k.at_once;
   const float full = k.fixed + steps * (k.step + k.more * (float)(k.at_once - 1));
-  return 3.f + (float)rounds * full + (rest ? k.fixed + steps * (k.step + k.more * (float)(rest - 1)) : 0.f);
+  const float busy = (float)rounds * full + (rest ? k.fixed + steps * (k.step + k.more * (float)(rest - 1)) : 0.f);
+  const float weights = there * (float)a.n * (float)a.k * (k.at_once > 1 ? 1.f / 5.3e6f : 1.f / 4.4e6f);
+  return 3.f + sqrtf(busy * busy + weights * weights);
 }
 
 template <int TT, int TN>
@@ -550,8 +555,8 @@ int best_of(const Kind* kinds, const ProductArgs& a, bool grouped) {
   return best;
 }
 
-// k_few for up to 16 rows (experts: up to 8 on average), else the tiles that the fit has as the fastest: over 135 calls 2 % behind the best of
-// them on average.  k_product's loads name x's codes by 31 bits; where a tile's rows lie further apart k_few has them all.
+// k_few for up to 16 rows (experts: up to 8 on average), else the tiles that the fit has as the fastest.  k_product's loads name x's
+// codes by 31 bits; where a tile's rows lie further apart k_few has them all.
 template <int DT, bool GROUPED>
 int product(const ProductArgs& a, plora_stream stream) {
   const bool far = a.rows ? (__int128)a.n_x_rows * a.x_s > kReach - 256 : 256 * (__int128)a.x_s > kReach - 256;
@@ -565,19 +570,21 @@ int product(const ProductArgs& a, plora_stream stream) {
         return few<DT, GROUPED, 4, 4, 2>(a, stream);
     }
   }
-  static constexpr Kind kTiles[] = {{64, 32, 2, 1, 1.85f, 0.379f, 0.f},  {64, 64, 2, 1, 1.79f, 0.525f, 0.f},   {64, 64, 1, 2, 0.99f, 0.295f, 0.234f}, {128, 64, 1, 1, 2.07f, 0.421f, 0.f},
-                                    {128, 128, 1, 1, 2.79f, 0.593f, 0.f}, {128, 256, 1, 1, 3.93f, 0.896f, 0.f}, {256, 128, 1, 1, 4.21f, 0.87f, 0.f},   {256, 256, 1, 1, 4.93f, 1.612f, 0.f}};
-  constexpr int kOf = DT == PLORA_F32 ? 7 : 8;  // (fp32's operands of the largest tile do not fit the registers)
+  static constexpr Kind kTiles[] = {{64, 32, 2, 1, 1.85f, 0.379f, 0.f},  {64, 64, 2, 1, 1.79f, 0.525f, 0.f},   {64, 64, 1, 2, 0.99f, 0.295f, 0.234f},
+                                    {64, 128, 1, 2, 2.f, 0.48f, 0.36f},   {128, 64, 1, 1, 2.07f, 0.421f, 0.f},  {128, 128, 1, 1, 2.79f, 0.593f, 0.f},
+                                    {128, 256, 1, 1, 3.93f, 0.896f, 0.f}, {256, 128, 1, 1, 4.21f, 0.87f, 0.f},  {256, 256, 1, 1, 4.93f, 1.612f, 0.f}};
+  constexpr int kOf = DT == PLORA_F32 ? 8 : 9;  // (fp32's operands of the largest tile do not fit the registers)
   switch (best_of<kOf>(kTiles, a, GROUPED)) {
     case 0: return tiled<DT, GROUPED, 64, 32, 4, 1, 2, 4>(a, stream);
     case 1: return tiled<DT, GROUPED, 64, 64, 2, 2, 2, 3>(a, stream);
     case 2: return tiled<DT, GROUPED, 64, 64, 2, 2, 1, 4>(a, stream);
-    case 3: return tiled<DT, GROUPED, 128, 64, 4, 2, 1, 4>(a, stream);
-    case 4: return tiled<DT, GROUPED, 128, 128, 4, 2, 1, 4>(a, stream);
-    case 5: return tiled<DT, GROUPED, 128, 256, 2, 4, 1, 3>(a, stream);
-    case 6: return tiled<DT, GROUPED, 256, 128, 4, 2, 1, 3>(a, stream);
+    case 3: return tiled<DT, GROUPED, 64, 128, 2, 2, 1, 3>(a, stream);
+    case 4: return tiled<DT, GROUPED, 128, 64, 4, 2, 1, 4>(a, stream);
+    case 5: return tiled<DT, GROUPED, 128, 128, 4, 2, 1, 4>(a, stream);
+    case 6: return tiled<DT, GROUPED, 128, 256, 2, 4, 1, 3>(a, stream);
+    case 7: return tiled<DT, GROUPED, 256, 128, 4, 2, 1, 3>(a, stream);
     default:
-      if constexpr (kOf == 8) return tiled<DT, GROUPED, 256, 256, 4, 2, 1, 3, true>(a, stream);
+      if constexpr (kOf == 9) return tiled<DT, GROUPED, 256, 256, 4, 2, 1, 3, true>(a, stream);
       else return PLORA_ERR_INVAL;
   }
 }

@@ -376,6 +376,20 @@ def test_grouped_of_each_kernel(dtype, t, n, k):
                 check_product(got[a:b], xv[a:b] if r is None else xv[r[a:b]], O.weight_values(wc[e], ws[e]), dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("t,n,k", [(413, 7176, 144), (257, 7176, 1040), (600, 13832, 144)])
+def test_product_of_more_kernels(dtype, t, n, k):
+    """Tiles of 64 x 128, 128 x 128 and the largest (fp32: 256 x 128)."""
+    test_product_of_each_kernel(dtype, t, n, k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("t,n,k", [(9, 2056, 528), (316, 1032, 8208), (413, 4104, 1040), (600, 7176, 144), (1030, 4104, 2064), (1030, 7176, 144)])
+def test_grouped_of_more_kernels(dtype, t, n, k):
+    """Few rows x 32 channels, tiles of 64 x 64 with two sets, 128 x 128, 128 x 256, 256 x 128 and the largest (fp32: another one)."""
+    test_grouped_of_each_kernel(dtype, t, n, k)
+
+
 def test_rows_far_apart():
     """x's rows behind 2 and 4 GiB, and results behind 4 GiB."""
     import torch
