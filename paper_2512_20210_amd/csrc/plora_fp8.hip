@@ -515,7 +515,8 @@ float time_of(const Kind& k, const ProductArgs& a, bool grouped) {
     float none = q;
     for (int i = 1; i < k.tt; i *= 2) none *= none;
     there = q * (float)a.n_experts;
-    rows = there / (1.f - none) + 0.15f * sqrtf((float)a.n_experts);  // (a tile more than there are CUs costs a round, one less saves nothing)
+    rows = none < 0.9f ? there / (1.f - none) : (float)(a.n_rows / k.tt) + 0.5f * (float)a.n_experts;  // (the same for large groups, where q is nearly 1)
+    rows += 0.15f * sqrtf((float)a.n_experts);  // (a tile more than there are CUs costs a round, one less saves nothing)
   }
   const float steps = (float)(((a.k + kBlock - 1) / kBlock + k.kg - 1) / k.kg);
   const int64_t here = ((int64_t)(rows * (float)((a.n + k.tn - 1) / k.tn)) + 255) / 256, rounds = here / k.at_once, rest = here - rounds * k.at_once;

@@ -390,6 +390,22 @@ def test_grouped_of_more_kernels(dtype, t, n, k):
     test_grouped_of_each_kernel(dtype, t, n, k)
 
 
+def test_one_expert_of_very_many_rows():
+    """More rows than 32-bit floats count (the rule's sizes of groups)."""
+    import torch
+    P = lib()
+    rng = np.random.default_rng(12)
+    total, k, n = (1 << 25) + 8, 16, 8
+    xc, wc = random_codes(rng, 64, k), random_codes(rng, 1, n, k)
+    codes = torch.from_numpy(xc).cuda().repeat(total // 64 + 1, 1)[:total].contiguous()
+    w = P.Fp8Weights(torch.from_numpy(wc).cuda(), torch.ones(1, 1, 1, device="cuda"))
+    out = torch.zeros(total, n, device="cuda")
+    w.grouped(P.Fp8Rows(codes, torch.ones(1, total, device="cuda")), ints([0, total]), out, stream=stream())
+    expected = O.row_values(xc, np.ones((1, 64), np.float32))
+    check_product(host(out[:64]), expected, O.weight_values(wc[0], np.ones((1, 1), np.float32)), "fp32")
+    assert (out[64:] == out[:64].repeat(total // 64, 1)[:total - 64]).all()
+
+
 def test_rows_far_apart():
     """x's rows behind 2 and 4 GiB, and results behind 4 GiB."""
     import torch
