@@ -561,7 +561,7 @@ int plora_fp8_matmul(const plora_fp8_rows* x, const plora_fp8_weights* w, int32_
 
 /* The same with a matrix for each group of rows: out rows offsets[e] .. offsets[e+1] - 1 are products with expert e's weights.  offsets: device,
  * n_experts + 1 entries, ascending, as plora_route makes them; each is held to [0, n_rows], and a group that ends ahead of its
- * start is empty.  Rows of no group are left alone; where groups overlap (offsets that are not ascending) their rows are undefined.
+ * start is empty.  Rows of no group are left alone; where groups overlap (offsets that are not ascending) the rows that they share are undefined.
  * rows: device, n_rows entries, or NULL: the x row of every out row (one x row may be read for several); an entry outside
  * [0, n_x_rows) gives a row of NaN.  NULL: x row r for out row r (n_x_rows >= n_rows). */
 int plora_fp8_grouped(const plora_fp8_rows* x, int32_t n_x_rows, const plora_fp8_weights* w, const int32_t* offsets, const int32_t* rows,

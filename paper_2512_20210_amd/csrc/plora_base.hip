@@ -403,18 +403,6 @@ struct RouteArgs {
 __device__ __forceinline__ int bits_below(const uint32_t* w, int t) {
   return t < 32 ? __popc(w[0] & ((1u << t) - 1)) : __popc(w[0]) + __popc(w[1] & ((1u << (t - 32)) - 1));
 }
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int dpp_from(int v) {  // 0 where there is no lane to take from, and in rows that are not in ROWS
-  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
-}
-__device__ __forceinline__ int wave_scan(int v) {  // the sum up to and with this lane
-  v += dpp_from<0x111, 0xf>(v);
-  v += dpp_from<0x112, 0xf>(v);
-  v += dpp_from<0x114, 0xf>(v);
-  v += dpp_from<0x118, 0xf>(v);
-  v += dpp_from<0x142, 0xa>(v);  // the last lane of a row to the next one
-  return v + dpp_from<0x143, 0xc>(v);  // and of half a wavefront
-}
 // Sum of v over the threads ahead of this one, and over all 1024 of them.
 __device__ __forceinline__ int scan1024(int v, int* waves, int& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;

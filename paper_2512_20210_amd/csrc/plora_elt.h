@@ -80,6 +80,21 @@ __device__ __forceinline__ void st8(uint8_t* p, const float* f) {
   }
 }
 
+// ---- along a wavefront --------------------------------------------------------------------------------
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_from(int v) {  // 0 where there is no lane to take from, and in rows that are not in ROWS
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_scan(int v) {  // the sum up to and with this lane
+  v += dpp_from<0x111, 0xf>(v);
+  v += dpp_from<0x112, 0xf>(v);
+  v += dpp_from<0x114, 0xf>(v);
+  v += dpp_from<0x118, 0xf>(v);
+  v += dpp_from<0x142, 0xa>(v);  // the last lane of a row to the next one
+  return v + dpp_from<0x143, 0xc>(v);  // and of half a wavefront
+}
+
 // ---- host side ----------------------------------------------------------------------------------------
 
 template <class A>

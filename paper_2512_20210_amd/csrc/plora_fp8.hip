@@ -87,17 +87,17 @@ template <> struct Unit<PLORA_F32> {
 // Which tile a workgroup has: rows first .. last - 1 (at most TT of them) of an expert, and a tile of output channels.
 struct Tile {
   int32_t expert, first, last, channel;
-  bool any;
+  bool any, more;  // more: the workgroup has a further one, gridDim.x behind this
 };
 __device__ __forceinline__ int32_t clamped(int32_t v, int32_t hi) { return v < 0 ? 0 : v > hi ? hi : v; }
 // Consecutive workgroups run on the 8 XCDs in turn: each XCD gets a range of neighbouring tiles (of those there are), and walks it in
 // bands of kBand row tiles, so that what runs on it at once shares rows and weights in its L2.
 template <int TT, int TN, bool GROUPED>
-__device__ __forceinline__ Tile tile_of(const ProductArgs& a) {
+__device__ __forceinline__ Tile tile_of(const ProductArgs& a, uint32_t block, uint32_t thread) {
   constexpr uint32_t kBand = 4;
-  Tile t = {0, 0, 0, 0, false};
+  Tile t = {0, 0, 0, 0, false, false};
   const uint32_t columns = (uint32_t)(a.n + TN - 1) / TN;
-  const int lane = threadIdx.x & 63;
+  const int lane = thread & 63;
   // experts e0 .. e0 + 63, one a lane: their rows, their row tiles, and the sum of these up to the lane's
   int32_t from = 0, to = 0;
   uint32_t n = 0, sum = 0;
@@ -108,12 +108,8 @@ __device__ __forceinline__ Tile tile_of(const ProductArgs& a) {
       from = clamped(a.offsets[e], a.n_rows);
       to = clamped(a.offsets[e + 1], a.n_rows);
     }
-    sum = n = to > from ? (uint32_t)(to - from + TT - 1) / TT : 0;
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) {
-      const uint32_t o = __shfl_up(sum, i);
-      if (lane >= i) sum += o;
-    }
+    n = to > from ? (uint32_t)(to - from + TT - 1) / TT : 0;
+    sum = (uint32_t)wave_scan((int)n);
     return (uint32_t)__builtin_amdgcn_readlane(sum, 63);
   };
   uint32_t row_tiles = 0;
@@ -121,7 +117,7 @@ __device__ __forceinline__ Tile tile_of(const ProductArgs& a) {
   else
     for (int e0 = 0; e0 < a.n_experts; e0 += 64) row_tiles += look(e0);
   const uint64_t tiles = (uint64_t)row_tiles * columns;
-  const uint32_t xcd = blockIdx.x & 7, at = blockIdx.x >> 3, per = (uint32_t)(tiles >> 3), more = (uint32_t)(tiles & 7);
+  const uint32_t xcd = block & 7, at = block >> 3, per = (uint32_t)(tiles >> 3), more = (uint32_t)(tiles & 7);
   if (at >= per + (xcd < more ? 1 : 0)) return t;
   const uint32_t id = xcd * per + (xcd < more ? xcd : more) + at;
   const uint32_t band = id / (kBand * columns), in = id - band * (kBand * columns);
@@ -129,6 +125,7 @@ __device__ __forceinline__ Tile tile_of(const ProductArgs& a) {
   const uint32_t q = band * kBand + in % high;
   t.channel = (int32_t)(in / high) * TN;
   t.any = true;
+  t.more = GROUPED && (uint64_t)block + gridDim.x < (tiles >> 32 ? (uint64_t)UINT32_MAX : tiles);
   if constexpr (!GROUPED) {
     t.first = (int32_t)q * TT;
     t.last = a.n_rows - t.first < TT ? a.n_rows : t.first + TT;
@@ -150,6 +147,18 @@ __device__ __forceinline__ Tile tile_of(const ProductArgs& a) {
     }
   }
   return t;
+}
+
+// The record of arguments for a tile, and its thread.  A workgroup has one tile; only groups that overlap have more tiles than the host can know of, and then workgroups take
+// several in turn, so that a row which belongs to one group alone is there whatever the others are.  Both go through an empty assembly line: else the compiler keeps what
+// it makes of them for a second tile, 20 vector registers that no call with ascending offsets has a use for.
+template <bool GROUPED>
+__device__ __forceinline__ ProductArgs args_of(const ProductArgs& args, uint32_t& thread) {
+  if constexpr (!GROUPED) return args;
+  typedef const __attribute__((address_space(4))) ProductArgs* constant_args;
+  constant_args at = (constant_args)__builtin_amdgcn_kernarg_segment_ptr();  // (args is all that a kernel has)
+  asm volatile("" : "+s"(at), "+v"(thread));
+  return *(const ProductArgs*)at;
 }
 
 // The x row of an out row; -1: none, the row becomes NaN.
@@ -184,7 +193,7 @@ __device__ __forceinline__ void st4(uint8_t* p, f32x4 f) {
 // wavefronts where there are few tiles.  Scales come through LDS as well: a scalar load in flight makes each wait for an LDS read wait for it
 // too (1024 x 1024 x 4096: 12.5 -> 11.1 us; 2048 x 5120 x 13824: 173 -> 167).
 template <int DT, int TT, int TN, int WT, int WN, int KG, int STAGES, bool ONE_X, bool GROUPED>
-__global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_eu(2))) void k_product(ProductArgs a) {
+__global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_eu(2))) void k_product(ProductArgs args) {
   constexpr int WAVES = WT * WN, NT = TT / WT / 16, NN = TN / WN / 16;
   constexpr int LX = TT / 8 / WAVES, LW = TN / 8 / WAVES;  // 16-byte loads of a thread and stage
   // they are spread over the first half of a stage's products: kPer of them every kEvery products
@@ -198,178 +207,184 @@ __global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_
   static_assert(!ONE_X || (KG == 1 && STAGES == 3 && 2 * (LX + 1 + LW) <= (NN - 2) * NT), "and between the second barrier and the next stage's first");
   static_assert((KG - 1) * TT * TN * 4 <= KG * kSet, "the sums are joined in the stages' place");
   __shared__ alignas(16) uint8_t lds[KG * kSet];
-  const Tile tile = tile_of<TT, TN, GROUPED>(a);
-  if (!tile.any) return;
-  const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = all % WAVES, set = all / WAVES;
-  const int kb = (a.k + kBlock - 1) / kBlock, steps = (kb + KG - 1) / KG;
-  const int wt = wave % WT, wn = wave / WT, col = lane & 15, quad = lane >> 4;
+  for (uint32_t block = blockIdx.x;; block += gridDim.x) {
+    uint32_t thread = threadIdx.x;
+    const ProductArgs a = args_of<GROUPED>(args, thread);
+    const Tile tile = tile_of<TT, TN, GROUPED>(a, block, thread);
+    if (!tile.any) return;
+    const int lane = thread & 63, all = __builtin_amdgcn_readfirstlane(thread >> 6), wave = all % WAVES, set = all / WAVES;
+    const int kb = (a.k + kBlock - 1) / kBlock, steps = (kb + KG - 1) / KG;
+    const int wt = wave % WT, wn = wave / WT, col = lane & 15, quad = lane >> 4;
 
-  // what this thread loads: rows wave * 8 + lane / 8 of every group of 8 WAVES, the piece that belongs at lane % 8
-  const int piece = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
-  const int64_t first_row = a.rows ? 0 : tile.first;
-  const i32x4 bx = buffer_at(a.x + first_row * a.x_s), bw = buffer_at(a.w + ((int64_t)tile.expert * a.n + tile.channel) * a.k);
-  uint32_t at[LX + LW];
+    // what this thread loads: rows wave * 8 + lane / 8 of every group of 8 WAVES, the piece that belongs at lane % 8
+    const int piece = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
+    const int64_t first_row = a.rows ? 0 : tile.first;
+    const i32x4 bx = buffer_at(a.x + first_row * a.x_s), bw = buffer_at(a.w + ((int64_t)tile.expert * a.n + tile.channel) * a.k);
+    uint32_t at[LX + LW];
 #pragma unroll
-  for (int i = 0; i < LX; ++i) {
-    int32_t r = tile.first + (i * WAVES + wave) * 8 + (lane >> 3);
-    r = x_row(a, r < tile.last ? r : tile.last - 1);
-    at[i] = r < 0 ? 0 : (uint32_t)((r - first_row) * a.x_s) + piece * 16;
-  }
-#pragma unroll
-  for (int i = 0; i < LW; ++i) {
-    const int32_t c = (i * WAVES + wave) * 8 + (lane >> 3), most = a.n - 1 - tile.channel;
-    at[LX + i] = (uint32_t)(c < most ? c : most) * a.k + piece * 16;
-  }
-  const auto row_of = [&](int t) {  // the x row of this lane's column in tile t
-    const int32_t r = tile.first + wt * (TT / WT) + t * 16 + col;
-    return x_row(a, r < tile.last ? r : tile.last - 1);
-  };
-  const int channel = tile.channel + wn * (TN / WN);  // the wavefront's first one
-  // One load of 64 words a stage brings a wavefront's scales: a row of x a lane, and by its last 16 lanes the weights' one; with 64 rows a wavefront the
-  // first wavefront of those rows has the rows', the second one the weights' of all (lane l: of wavefront column l % WN).
-  const bool of_w = NT < 4 ? quad == 3 : wn > 0;
-  const int32_t scale_row = row_of(quad % NT);
-  const int nb = (a.n + kBlock - 1) / kBlock, cb = (NT < 4 ? channel : tile.channel + lane % WN * (TN / WN)) / kBlock, b0 = set < kb ? set : kb - 1;
-  const float* scale = of_w ? a.ws + ((int64_t)tile.expert * nb + (cb < nb ? cb : nb - 1)) * kb + b0 : a.xs + (scale_row < 0 ? 0 : scale_row) + b0 * a.xs_s;
-  const int64_t scale_step = KG * (of_w ? 1 : a.xs_s);
-  const uint8_t* mine = lds + set * kSet;
-  const uint32_t to = __builtin_amdgcn_readfirstlane(lds_addr(mine) + wave * 1024), scales_to = __builtin_amdgcn_readfirstlane(lds_addr(mine) + kAtScales + wave * 256);
-  // Load i of the set's step s: LX of x, the wavefront's scales of x, LW of weights.  Behind the last code of the rows, and behind the last block: zeros (of scales the
-  // last block's again).
-  const auto fetch = [&](int s, int slot, int i) {
-    const int b = s * KG + set;
-    if (i == LX) {
-      load_word_to_lds(scale, scales_to + (ONE_X ? 0 : slot) * kScales);
-      scale += b + KG < kb ? scale_step : 0;
-    } else {
-      const int l = i < LX ? i : i - 1;
-      const uint32_t dst = i < LX ? to + (ONE_X ? 0 : slot) * kX + l * WAVES * 1024 : to + kAtW + slot * kW + (l - LX) * WAVES * 1024;
-      load_to_lds(i < LX ? bx : bw, b * kBlock + piece * 16 < a.k ? at[l] : kNowhere, b * kBlock, dst);
-    }
-  };
-  const auto operand = [&](const uint8_t* rows, int row) {
-    const uint8_t* p = rows + row * kBlock;
-    const int s = (row >> 1) & 7;
-    const i32x4 lo = *reinterpret_cast<const i32x4*>(p + (quad ^ s) * 16), hi = *reinterpret_cast<const i32x4*>(p + ((quad + 4) ^ s) * 16);
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-  };
-  const auto operand_x = [&](int slot, int t) { return Unit<DT>::make(operand(mine + (ONE_X ? 0 : slot) * kX, wt * (TT / WT) + col + t * 16)); };
-  const auto operand_w = [&](int slot, int m) { return operand(mine + kAtW + slot * kW, wn * (TN / WN) + col + m * 16); };
-
-  // A stage's products go row after row (a row: one operand of weights, all of x).  While the matrix unit has a row, the next row's weights
-  // are read and the products of the row before are scaled and added.  The one barrier of a stage is ahead of its last row: then the
-  // next stage is there and this one has been read, so the last row reads the next stage's operands already, and the loads of the
-  // stage that follows STAGES behind go into this one's place.
-#pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s)
-#pragma unroll
-    for (int i = ONE_X && s > 0 ? LX + 1 : 0; i <= LX + LW; ++i) fetch(s, s, i);
-  constexpr int kLater = ONE_X ? LW : (STAGES - 2) * (LX + LW + 1);  // loads under way that are of stages behind the next one
-  wait_loads<kLater>();
-  __syncthreads();
-  f32x4 acc[NN][NT] = {}, d[NT] = {};
-  typename Unit<DT>::operand x[NT];
-  i32x8 w[2];
-  float f[NT] = {}, fx[NT], fw;
-  const auto scales = [&](int slot) {
-    const uint8_t* p = mine + kAtScales + (ONE_X ? 0 : slot) * kScales;
-    fw = *reinterpret_cast<const float*>(p + (NT < 4 ? wave * 64 + 48 : (wt + WT) * 64 + wn) * 4);
-#pragma unroll
-    for (int t = 0; t < NT; ++t) fx[t] = *reinterpret_cast<const float*>(p + ((NT < 4 ? wave : wt) * 64 + t * 16 + col) * 4);
-  };
-  w[0] = operand_w(0, 0);
-#pragma unroll
-  for (int t = 0; t < NT; ++t) x[t] = operand_x(0, t);
-  scales(0);
-  if constexpr (!ONE_X)
-#pragma unroll
-    for (int i = 0; i <= LX + LW && i / kPer * kEvery < NT; ++i) fetch(STAGES - 1, STAGES - 1, i);
-  int slot = 0;
-  for (int s = 0; s < steps; ++s) {
-    const int b = s * KG + set, next = slot + 1 < STAGES ? slot + 1 : 0, free = slot > 0 ? slot - 1 : STAGES - 1;
-    float before[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      before[t] = f[t];
-      f[t] = b < kb ? fx[t] * fw : 0.f;
+    for (int i = 0; i < LX; ++i) {
+      int32_t r = tile.first + (i * WAVES + wave) * 8 + (lane >> 3);
+      r = x_row(a, r < tile.last ? r : tile.last - 1);
+      at[i] = r < 0 ? 0 : (uint32_t)((r - first_row) * a.x_s) + piece * 16;
     }
 #pragma unroll
-    for (int m = 0; m < NN; ++m) {
-      if (m == NN - 1) {
-        asm volatile("" : : : "memory");  // LDS reads stay on their side of the barrier
-        wait_loads<kLater>();
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" : : : "memory");
-        scales(next);
-      } else if (ONE_X && m == 1) {  // all wavefronts have x (their first row's products went ahead of this)
-        asm volatile("" : : : "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" : : : "memory");
+    for (int i = 0; i < LW; ++i) {
+      const int32_t c = (i * WAVES + wave) * 8 + (lane >> 3), most = a.n - 1 - tile.channel;
+      at[LX + i] = (uint32_t)(c < most ? c : most) * a.k + piece * 16;
+    }
+    const auto row_of = [&](int t) {  // the x row of this lane's column in tile t
+      const int32_t r = tile.first + wt * (TT / WT) + t * 16 + col;
+      return x_row(a, r < tile.last ? r : tile.last - 1);
+    };
+    const int channel = tile.channel + wn * (TN / WN);  // the wavefront's first one
+    // One load of 64 words a stage brings a wavefront's scales: a row of x a lane, and by its last 16 lanes the weights' one; with 64 rows a wavefront the
+    // first wavefront of those rows has the rows', the second one the weights' of all (lane l: of wavefront column l % WN).
+    const bool of_w = NT < 4 ? quad == 3 : wn > 0;
+    const int32_t scale_row = row_of(quad % NT);
+    const int nb = (a.n + kBlock - 1) / kBlock, cb = (NT < 4 ? channel : tile.channel + lane % WN * (TN / WN)) / kBlock, b0 = set < kb ? set : kb - 1;
+    const float* scale = of_w ? a.ws + ((int64_t)tile.expert * nb + (cb < nb ? cb : nb - 1)) * kb + b0 : a.xs + (scale_row < 0 ? 0 : scale_row) + b0 * a.xs_s;
+    const int64_t scale_step = KG * (of_w ? 1 : a.xs_s);
+    const uint8_t* mine = lds + set * kSet;
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds_addr(mine) + wave * 1024), scales_to = __builtin_amdgcn_readfirstlane(lds_addr(mine) + kAtScales + wave * 256);
+    // Load i of the set's step s: LX of x, the wavefront's scales of x, LW of weights.  Behind the last code of the rows, and behind the last block: zeros (of scales the
+    // last block's again).
+    const auto fetch = [&](int s, int slot, int i) {
+      const int b = s * KG + set;
+      if (i == LX) {
+        load_word_to_lds(scale, scales_to + (ONE_X ? 0 : slot) * kScales);
+        scale += b + KG < kb ? scale_step : 0;
+      } else {
+        const int l = i < LX ? i : i - 1;
+        const uint32_t dst = i < LX ? to + (ONE_X ? 0 : slot) * kX + l * WAVES * 1024 : to + kAtW + slot * kW + (l - LX) * WAVES * 1024;
+        load_to_lds(i < LX ? bx : bw, b * kBlock + piece * 16 < a.k ? at[l] : kNowhere, b * kBlock, dst);
       }
-      w[(m + 1) & 1] = m + 1 < NN ? operand_w(slot, m + 1) : operand_w(next, 0);
-      const auto row = Unit<DT>::make(w[m & 1]);
+    };
+    const auto operand = [&](const uint8_t* rows, int row) {
+      const uint8_t* p = rows + row * kBlock;
+      const int s = (row >> 1) & 7;
+      const i32x4 lo = *reinterpret_cast<const i32x4*>(p + (quad ^ s) * 16), hi = *reinterpret_cast<const i32x4*>(p + ((quad + 4) ^ s) * 16);
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    const auto operand_x = [&](int slot, int t) { return Unit<DT>::make(operand(mine + (ONE_X ? 0 : slot) * kX, wt * (TT / WT) + col + t * 16)); };
+    const auto operand_w = [&](int slot, int m) { return operand(mine + kAtW + slot * kW, wn * (TN / WN) + col + m * 16); };
+
+    // A stage's products go row after row (a row: one operand of weights, all of x).  While the matrix unit has a row, the next row's weights
+    // are read and the products of the row before are scaled and added.  The one barrier of a stage is ahead of its last row: then the
+    // next stage is there and this one has been read, so the last row reads the next stage's operands already, and the loads of the
+    // stage that follows STAGES behind go into this one's place.
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s)
+#pragma unroll
+      for (int i = ONE_X && s > 0 ? LX + 1 : 0; i <= LX + LW; ++i) fetch(s, s, i);
+    constexpr int kLater = ONE_X ? LW : (STAGES - 2) * (LX + LW + 1);  // loads under way that are of stages behind the next one
+    wait_loads<kLater>();
+    __syncthreads();
+    f32x4 acc[NN][NT] = {}, d[NT] = {};
+    typename Unit<DT>::operand x[NT];
+    i32x8 w[2];
+    float f[NT] = {}, fx[NT], fw;
+    const auto scales = [&](int slot) {
+      const uint8_t* p = mine + kAtScales + (ONE_X ? 0 : slot) * kScales;
+      fw = *reinterpret_cast<const float*>(p + (NT < 4 ? wave * 64 + 48 : (wt + WT) * 64 + wn) * 4);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) fx[t] = *reinterpret_cast<const float*>(p + ((NT < 4 ? wave : wt) * 64 + t * 16 + col) * 4);
+    };
+    w[0] = operand_w(0, 0);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) x[t] = operand_x(0, t);
+    scales(0);
+    if constexpr (!ONE_X)
+#pragma unroll
+      for (int i = 0; i <= LX + LW && i / kPer * kEvery < NT; ++i) fetch(STAGES - 1, STAGES - 1, i);
+    int slot = 0;
+    for (int s = 0; s < steps; ++s) {
+      const int b = s * KG + set, next = slot + 1 < STAGES ? slot + 1 : 0, free = slot > 0 ? slot - 1 : STAGES - 1;
+      float before[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        f32x4& sum = acc[(m + NN - 1) % NN][t];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(m ? f[t] : before[t], d[t][e], sum[e]);
-        d[t] = Unit<DT>::dot(row, x[t]);
-        if (m == NN - 1) x[t] = operand_x(next, t);
-        if constexpr (ONE_X) {
-          const int done = (m - 1) * NT + t;  // products since the second barrier
-          if (m > 0 && done % 2 == 0 && done / 2 <= LX + LW) fetch(done / 2 <= LX ? s + 1 : s + 2, free, done / 2);
-        } else {
-          const int done = (m + 1) % NN * NT + t;  // products since the barrier
-#pragma unroll
-          for (int i = done / kEvery * kPer; done % kEvery == 0 && i <= LX + LW && i < (done / kEvery + 1) * kPer; ++i)
-            if (m == NN - 1) fetch(s + STAGES, slot, i);
-            else fetch(s + STAGES - 1, free, i);
-        }
-        __builtin_amdgcn_sched_barrier(0);
+        before[t] = f[t];
+        f[t] = b < kb ? fx[t] * fw : 0.f;
       }
+#pragma unroll
+      for (int m = 0; m < NN; ++m) {
+        if (m == NN - 1) {
+          asm volatile("" : : : "memory");  // LDS reads stay on their side of the barrier
+          wait_loads<kLater>();
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" : : : "memory");
+          scales(next);
+        } else if (ONE_X && m == 1) {  // all wavefronts have x (their first row's products went ahead of this)
+          asm volatile("" : : : "memory");
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" : : : "memory");
+        }
+        w[(m + 1) & 1] = m + 1 < NN ? operand_w(slot, m + 1) : operand_w(next, 0);
+        const auto row = Unit<DT>::make(w[m & 1]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          f32x4& sum = acc[(m + NN - 1) % NN][t];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(m ? f[t] : before[t], d[t][e], sum[e]);
+          d[t] = Unit<DT>::dot(row, x[t]);
+          if (m == NN - 1) x[t] = operand_x(next, t);
+          if constexpr (ONE_X) {
+            const int done = (m - 1) * NT + t;  // products since the second barrier
+            if (m > 0 && done % 2 == 0 && done / 2 <= LX + LW) fetch(done / 2 <= LX ? s + 1 : s + 2, free, done / 2);
+          } else {
+            const int done = (m + 1) % NN * NT + t;  // products since the barrier
+#pragma unroll
+            for (int i = done / kEvery * kPer; done % kEvery == 0 && i <= LX + LW && i < (done / kEvery + 1) * kPer; ++i)
+              if (m == NN - 1) fetch(s + STAGES, slot, i);
+              else fetch(s + STAGES - 1, free, i);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      slot = next;
     }
-    slot = next;
-  }
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[NN - 1][t][e] = __builtin_fmaf(f[t], d[t][e], acc[NN - 1][t][e]);
-  __builtin_amdgcn_s_waitcnt(0);  // no load into LDS outlives the workgroup, or comes behind the sums
-  if constexpr (KG > 1) {
-    __syncthreads();
-    f32x4* part = reinterpret_cast<f32x4*>(lds) + wave * NN * NT * 64 + lane;
-    if (set > 0) {
+      for (int e = 0; e < 4; ++e) acc[NN - 1][t][e] = __builtin_fmaf(f[t], d[t][e], acc[NN - 1][t][e]);
+    __builtin_amdgcn_s_waitcnt(0);  // no load into LDS outlives the workgroup, or comes behind the sums
+    if constexpr (KG > 1) {
+      __syncthreads();
+      f32x4* part = reinterpret_cast<f32x4*>(lds) + wave * NN * NT * 64 + lane;
+      if (set > 0) {
+#pragma unroll
+        for (int m = 0; m < NN; ++m)
+#pragma unroll
+          for (int t = 0; t < NT; ++t) part[((set - 1) * WAVES * NN * NT + m * NT + t) * 64] = acc[m][t];
+      }
+      __syncthreads();
+      if (set > 0 && (!GROUPED || !tile.more)) return;
 #pragma unroll
       for (int m = 0; m < NN; ++m)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) part[((set - 1) * WAVES * NN * NT + m * NT + t) * 64] = acc[m][t];
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int g = 0; g < KG - 1; ++g) {
+            const f32x4 o = part[(g * WAVES * NN * NT + m * NT + t) * 64];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[m][t][e] += o[e];
+          }
     }
-    __syncthreads();
-    if (set > 0) return;
 #pragma unroll
-    for (int m = 0; m < NN; ++m)
+    for (int t = 0; t < NT; ++t) {
+      const int32_t r = tile.first + wt * (TT / WT) + t * 16 + col;
+      if (r >= tile.last || (GROUPED && set > 0)) continue;
+      const bool hole = row_of(t) < 0;
+      uint8_t* o = a.out + (int64_t)r * a.out_s;
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int g = 0; g < KG - 1; ++g) {
-          const f32x4 o = part[(g * WAVES * NN * NT + m * NT + t) * 64];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[m][t][e] += o[e];
-        }
-  }
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int32_t r = tile.first + wt * (TT / WT) + t * 16 + col;
-    if (r >= tile.last) continue;
-    const bool hole = row_of(t) < 0;
-    uint8_t* o = a.out + (int64_t)r * a.out_s;
-#pragma unroll
-    for (int m = 0; m < NN; ++m) {
-      const int c = channel + m * 16 + quad * 4;
-      f32x4 y = acc[m][t];
-      if (hole) y = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
-      if (c < a.n) st4<DT>(o + (int64_t)c * Elt<DT>::B, y);
+      for (int m = 0; m < NN; ++m) {
+        const int c = channel + m * 16 + quad * 4;
+        f32x4 y = acc[m][t];
+        if (hole) y = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+        if (c < a.n) st4<DT>(o + (int64_t)c * Elt<DT>::B, y);
+      }
     }
+    if (!GROUPED || !tile.more) return;
+    __syncthreads();  // (the next tile's loads go where this one's sums were joined)
   }
 }
 
@@ -380,121 +395,127 @@ __global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_
 // with x in registers, the next ones' weights on their way and a join a step (78); x in LDS and wavefronts that read their channels on their
 // own, 2 to 8 blocks ahead and with nothing to join (69 - 75).
 template <int DT, int TT, int NW, int WAVES, int P, bool GROUPED>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void k_few(ProductArgs a) {
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void k_few(ProductArgs args) {
   constexpr int NT = TT / 16;
   __shared__ f32x4 part[WAVES][NW * NT][64];
-  const Tile tile = tile_of<TT, 16 * NW, GROUPED>(a);
-  if (!tile.any) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
-  const int kb = (a.k + kBlock - 1) / kBlock;
-  const uint8_t *px[NT], *pw[NW];
-  const float* sx[NT];
+  for (uint32_t block = blockIdx.x;; block += gridDim.x) {
+    uint32_t thread = threadIdx.x;
+    const ProductArgs a = args_of<GROUPED>(args, thread);
+    const Tile tile = tile_of<TT, 16 * NW, GROUPED>(a, block, thread);
+    if (!tile.any) return;
+    const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6), col = lane & 15, quad = lane >> 4;
+    const int kb = (a.k + kBlock - 1) / kBlock;
+    const uint8_t *px[NT], *pw[NW];
+    const float* sx[NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int32_t at = tile.first + t * 16 + col, r = x_row(a, at < tile.last ? at : tile.last - 1);
-    px[t] = a.x + (int64_t)(r < 0 ? 0 : r) * a.x_s + quad * 16;
-    sx[t] = a.xs + (r < 0 ? 0 : r);
-  }
-  const uint8_t* w0 = a.w + (int64_t)tile.expert * a.n * a.k;
+    for (int t = 0; t < NT; ++t) {
+      const int32_t at = tile.first + t * 16 + col, r = x_row(a, at < tile.last ? at : tile.last - 1);
+      px[t] = a.x + (int64_t)(r < 0 ? 0 : r) * a.x_s + quad * 16;
+      sx[t] = a.xs + (r < 0 ? 0 : r);
+    }
+    const uint8_t* w0 = a.w + (int64_t)tile.expert * a.n * a.k;
 #pragma unroll
-  for (int m = 0; m < NW; ++m) {
-    const int c = tile.channel + m * 16 + col;
-    pw[m] = w0 + (int64_t)(c < a.n ? c : a.n - 1) * a.k + quad * 16;
-  }
-  const int nb = (a.n + kBlock - 1) / kBlock;
-  typedef const __attribute__((address_space(4))) float* scalar_floats;
-  const scalar_floats sw = (scalar_floats)(uintptr_t)(a.ws + ((int64_t)tile.expert * nb + tile.channel / kBlock) * kb);
+    for (int m = 0; m < NW; ++m) {
+      const int c = tile.channel + m * 16 + col;
+      pw[m] = w0 + (int64_t)(c < a.n ? c : a.n - 1) * a.k + quad * 16;
+    }
+    const int nb = (a.n + kBlock - 1) / kBlock;
+    typedef const __attribute__((address_space(4))) float* scalar_floats;
+    const scalar_floats sw = (scalar_floats)(uintptr_t)(a.ws + ((int64_t)tile.expert * nb + tile.channel / kBlock) * kb);
 
-  struct Block {
-    i32x8 w[NW], x[NT];
-    float fx[NT], fw;  // multiplied where they are used: a product here would wait for all of the block's loads
-  };
-  const auto load = [&](int b, Block& o) {
-    // pieces behind the last code, and blocks behind the last one: the first piece of the row in their place, and x's codes zeroed
-    const int64_t lo = b * kBlock + quad * 16 < a.k ? b * kBlock : -quad * 16, hi = b * kBlock + 64 + quad * 16 < a.k ? b * kBlock + 64 : -quad * 16;
-    const auto both = [&](const uint8_t* p) {
-      return __builtin_shufflevector(*reinterpret_cast<const i32x4*>(p + lo), *reinterpret_cast<const i32x4*>(p + hi), 0, 1, 2, 3, 4, 5, 6, 7);
+    struct Block {
+      i32x8 w[NW], x[NT];
+      float fx[NT], fw;  // multiplied where they are used: a product here would wait for all of the block's loads
     };
+    const auto load = [&](int b, Block& o) {
+      // pieces behind the last code, and blocks behind the last one: the first piece of the row in their place, and x's codes zeroed
+      const int64_t lo = b * kBlock + quad * 16 < a.k ? b * kBlock : -quad * 16, hi = b * kBlock + 64 + quad * 16 < a.k ? b * kBlock + 64 : -quad * 16;
+      const auto both = [&](const uint8_t* p) {
+        return __builtin_shufflevector(*reinterpret_cast<const i32x4*>(p + lo), *reinterpret_cast<const i32x4*>(p + hi), 0, 1, 2, 3, 4, 5, 6, 7);
+      };
 #pragma unroll
-    for (int m = 0; m < NW; ++m) o.w[m] = both(pw[m]);
-    const int at = b < kb ? b : kb - 1;
-    o.fw = sw[at];
+      for (int m = 0; m < NW; ++m) o.w[m] = both(pw[m]);
+      const int at = b < kb ? b : kb - 1;
+      o.fw = sw[at];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      o.x[t] = both(px[t]);
-      o.fx[t] = sx[t][(int64_t)at * a.xs_s];
-    }
-  };
-  f32x4 acc[NW][NT] = {};
-  Block ring[P];
-  const auto use = [&](Block& o) {
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const float f = o.fx[t] * o.fw;
-#pragma unroll
-      for (int m = 0; m < NW; ++m) {
-        const f32x4 d = Unit<DT>::dot(Unit<DT>::make(o.w[m]), Unit<DT>::make(o.x[t]));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[m][t][e] = __builtin_fmaf(f, d[e], acc[m][t][e]);
+      for (int t = 0; t < NT; ++t) {
+        o.x[t] = both(px[t]);
+        o.fx[t] = sx[t][(int64_t)at * a.xs_s];
       }
-    }
-  };
-  const auto use_last = [&](int b, Block& o) {  // with the codes behind k zeroed
+    };
+    f32x4 acc[NW][NT] = {};
+    Block ring[P];
+    const auto use = [&](Block& o) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const bool there = b * kBlock + (e < 4 ? 0 : 64) + quad * 16 < a.k;
+      for (int t = 0; t < NT; ++t) {
+        const float f = o.fx[t] * o.fw;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) o.x[t][e] = there ? o.x[t][e] : 0;
+        for (int m = 0; m < NW; ++m) {
+          const f32x4 d = Unit<DT>::dot(Unit<DT>::make(o.w[m]), Unit<DT>::make(o.x[t]));
 #pragma unroll
-      for (int m = 0; m < NW; ++m) o.w[m][e] = there ? o.w[m][e] : 0;
-    }
-    use(o);
-  };
-  int b = wave;
-  if (b + (2 * P - 1) * WAVES < kb) {
-    // no branch in here, and none ahead of it that not all loads are behind: the waits would be for all loads under way
-#pragma unroll
-    for (int p = 0; p < P; ++p) load(b + p * WAVES, ring[p]);
-    do {
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        use(ring[p]);
-        __builtin_amdgcn_sched_barrier(0);  // (else all uses would be ahead of all loads)
-        load(b + (P + p) * WAVES, ring[p]);
-        __builtin_amdgcn_sched_barrier(0);
+          for (int e = 0; e < 4; ++e) acc[m][t][e] = __builtin_fmaf(f, d[e], acc[m][t][e]);
+        }
       }
-      b += P * WAVES;
-    } while (b + (2 * P - 1) * WAVES < kb);
-  } else {
+    };
+    const auto use_last = [&](int b, Block& o) {  // with the codes behind k zeroed
 #pragma unroll
-    for (int p = 0; p < P; ++p)
-      if (p == 0 || b + p * WAVES < kb) load(b + p * WAVES, ring[p]);
-  }
+      for (int e = 0; e < 8; ++e) {
+        const bool there = b * kBlock + (e < 4 ? 0 : 64) + quad * 16 < a.k;
 #pragma unroll
-  for (int p = 0; p < 2 * P - 1; ++p) {
-    const int at = b + p * WAVES;
-    if (at < kb) use_last(at, ring[p % P]);
-    if (p < P - 1 && at + P * WAVES < kb) load(at + P * WAVES, ring[p]);
-  }
+        for (int t = 0; t < NT; ++t) o.x[t][e] = there ? o.x[t][e] : 0;
 #pragma unroll
-  for (int m = 0; m < NW; ++m)
+        for (int m = 0; m < NW; ++m) o.w[m][e] = there ? o.w[m][e] : 0;
+      }
+      use(o);
+    };
+    int b = wave;
+    if (b + (2 * P - 1) * WAVES < kb) {
+      // no branch in here, and none ahead of it that not all loads are behind: the waits would be for all loads under way
 #pragma unroll
-    for (int t = 0; t < NT; ++t) part[wave][m * NT + t][lane] = acc[m][t];
-  __syncthreads();
-  for (int i = wave; i < NW * NT; i += WAVES) {
-    const int m = i / NT, t = i % NT;
-    const int32_t r = tile.first + t * 16 + col;
-    const int c = tile.channel + m * 16 + quad * 4;
-    f32x4 y = part[0][i][lane];
+      for (int p = 0; p < P; ++p) load(b + p * WAVES, ring[p]);
+      do {
 #pragma unroll
-    for (int v = 1; v < WAVES; ++v) {
-      const f32x4 o = part[v][i][lane];
+        for (int p = 0; p < P; ++p) {
+          use(ring[p]);
+          __builtin_amdgcn_sched_barrier(0);  // (else all uses would be ahead of all loads)
+          load(b + (P + p) * WAVES, ring[p]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        b += P * WAVES;
+      } while (b + (2 * P - 1) * WAVES < kb);
+    } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] += o[e];
+      for (int p = 0; p < P; ++p)
+        if (p == 0 || b + p * WAVES < kb) load(b + p * WAVES, ring[p]);
     }
-    if (r >= tile.last || c >= a.n) continue;
-    if (x_row(a, r) < 0) y = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
-    st4<DT>(a.out + (int64_t)r * a.out_s + (int64_t)c * Elt<DT>::B, y);
+#pragma unroll
+    for (int p = 0; p < 2 * P - 1; ++p) {
+      const int at = b + p * WAVES;
+      if (at < kb) use_last(at, ring[p % P]);
+      if (p < P - 1 && at + P * WAVES < kb) load(at + P * WAVES, ring[p]);
+    }
+#pragma unroll
+    for (int m = 0; m < NW; ++m)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) part[wave][m * NT + t][lane] = acc[m][t];
+    __syncthreads();
+    for (int i = wave; i < NW * NT; i += WAVES) {
+      const int m = i / NT, t = i % NT;
+      const int32_t r = tile.first + t * 16 + col;
+      const int c = tile.channel + m * 16 + quad * 4;
+      f32x4 y = part[0][i][lane];
+#pragma unroll
+      for (int v = 1; v < WAVES; ++v) {
+        const f32x4 o = part[v][i][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] += o[e];
+      }
+      if (r >= tile.last || c >= a.n) continue;
+      if (x_row(a, r) < 0) y = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+      st4<DT>(a.out + (int64_t)r * a.out_s + (int64_t)c * Elt<DT>::B, y);
+    }
+    if (!GROUPED || !tile.more) return;
+    __syncthreads();  // (the next tile's sums go where this one's were)
   }
 }
 
