@@ -461,15 +461,17 @@ __device__ __forceinline__ int dpp_sum(int v) {
 __device__ __forceinline__ int row_sum(int v) { return dpp_sum<0x121>(dpp_sum<0x122>(dpp_sum<0x124>(dpp_sum<0x128>(v)))); }
 __device__ __forceinline__ int row_max(int v) { return dpp_max<0x121>(dpp_max<0x122>(dpp_max<0x124>(dpp_max<0x128>(v)))); }
 
-template <int DT>
-__device__ __forceinline__ void ld4(const uint8_t* p, float* f) {
-  if constexpr (DT == PLORA_F32) {
-    *reinterpret_cast<f32x4*>(f) = *reinterpret_cast<const f32x4*>(p);
+// N = 4 or 8 consecutive logits from any element on.  (The compiler is told of no more alignment than there is, and reads them with one instruction all the
+// same: the GPU takes any address.)
+template <int DT, int N>
+__device__ __forceinline__ void ld_any(const uint8_t* p, float* f) {
+  alignas(16) uint8_t q[N * Elt<DT>::B];
+  __builtin_memcpy(q, p, sizeof(q));
+  if constexpr (N == 8) {
+    ld8<DT>(q, f);
   } else {
-    const uint2 u = *reinterpret_cast<const uint2*>(p);
-    const uint8_t* q = reinterpret_cast<const uint8_t*>(&u);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = ld1<DT>(q, i);
+    for (int i = 0; i < N; ++i) f[i] = ld1<DT>(q, i);
   }
 }
 
@@ -496,8 +498,7 @@ __global__ __launch_bounds__(THREADS) void k_route_choose(RouteArgs a) {
     for (int i = 0; i < V; i += G) {
       const uint8_t* p = a.logits + (t * a.stride + expert_of(i)) * Elt<DT>::B;
       if (live && expert_of(i) + G <= a.n_experts) {
-        if constexpr (G == 8) ld8<DT>(p, v + i);
-        else ld4<DT>(p, v + i);
+        ld_any<DT, G>(p, v + i);
       } else {
 #pragma unroll
         for (int j = 0; j < G; ++j) v[i + j] = live && expert_of(i + j) < a.n_experts ? ld1<DT>(p, j) : -INFINITY;
