@@ -964,6 +964,7 @@ def plora_route(dtype, n_tokens, n_experts, top_k, logits, renormalise, scale, e
 _ELEMENTS = (PLORA_F16, PLORA_BF16, PLORA_F32)
 _EIGHT = ("torch.float8_e4m3fn", "torch.uint8")
 _NO_ROWS = (None, None, 0, 0)
+_MOST = 0x7fffffff  # the library's counts have 32 bits; ctypes would take larger ones modulo 2^32
 
 
 def _place_of(call, t, n_rows, width, dtype, device):
@@ -984,7 +985,10 @@ def _matrix_of(call, t, n_rows, width, dtype, device):
 def _two(call, t):
     if t.dim() != 2:
         raise PloraError(call, PLORA_ERR_INVAL)
-    return t.shape
+    a, b = t.shape
+    if a > _MOST or b > _MOST:
+        raise PloraError(call, PLORA_ERR_LIMIT)
+    return a, b
 
 
 # The classes below take torch tensors as those above do: all of the GPU that is torch's current one at the call; stream None is the null stream.
@@ -1028,6 +1032,8 @@ class Fp8Weights:
             raise PloraError(call, PLORA_ERR_INVAL)
         n, k = codes.shape[-2:]
         experts = codes.shape[0] if codes.dim() == 3 else 1
+        if max(codes.shape) > _MOST:
+            raise PloraError(call, PLORA_ERR_LIMIT)
         self.device = codes.get_device()
         if self.device < 0 or scales.get_device() != self.device or str(codes.dtype) not in _EIGHT or str(scales.dtype) != "torch.float32" or \
                 scales.shape != (*codes.shape[:-2], -(-n // 128), -(-k // 128)) or not codes.is_contiguous() or not scales.is_contiguous():
@@ -1088,6 +1094,8 @@ class Routing:
             raise PloraError(call, PLORA_ERR_INVAL)
         self.experts, self.weights, self.offsets, self.rows, self.places, self.workspace = experts, weights, offsets, rows, places, workspace
         self.n, self.k, self.n_experts = n, k, offsets.numel() - 1
+        if self.n_experts > _MOST:
+            raise PloraError(call, PLORA_ERR_LIMIT)
         size = 0 if workspace is None else workspace.nbytes
         self.at = (_ints_of(call, experts, n * k, dev), weights.data_ptr(), _ints_of(call, offsets, 2, dev), _ints_of(call, rows, n * k, dev),
                    _ints_of(call, places, n * k, dev), workspace.data_ptr() if size else None, size)
