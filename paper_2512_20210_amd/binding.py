@@ -1164,6 +1164,8 @@ class BlockNorm:
                 (out8 is not None and (out8.device != device or out8.n != n or out8.k != dim)):
             raise PloraError(call, PLORA_ERR_INVAL)
         if gate is not None and gate.dim() == 1:
+            if gate.shape[0] != dim:
+                raise PloraError(call, PLORA_ERR_INVAL)
             gate = gate.expand(n, dim)
         b, bs = _place_of(call, block, rows, dim, dtype, device)
         g, gs = (None, 0) if gate is None else _place_of(call, gate, n, dim, dtype, device)

@@ -57,3 +57,13 @@ def test_counts_past_32_bits(monkeypatch, call):
 def test_the_largest_counts_are_taken():
     """(Nothing is launched: these only hold what a call is given.)"""
     assert rows((1 << 31) - 1, 16).n == (1 << 31) - 1 and weights(8, 1 << 20).k == 1 << 20 and routing((1 << 31) - 1, 1, 8).n == (1 << 31) - 1
+
+
+@pytest.mark.parametrize("width", [0, 1, 63, 128])
+def test_a_gate_of_another_width(monkeypatch, width):
+    monkeypatch.setattr(P.binding, "_device", lambda: 0)
+    f = lambda *z: Shaped(torch.bfloat16, *z)  # noqa: E731
+    gate = f(width)
+    gate.expand = lambda *z: gate.t.expand(*z)
+    with pytest.raises(P.PloraError, match="INVAL"):
+        P.BlockNorm().run(f(3, 64), out=f(3, 64), gate=gate)
