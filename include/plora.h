@@ -567,6 +567,15 @@ int plora_fp8_matmul(const plora_fp8_rows* x, const plora_fp8_weights* w, int32_
 int plora_fp8_grouped(const plora_fp8_rows* x, int32_t n_x_rows, const plora_fp8_weights* w, const int32_t* offsets, const int32_t* rows,
                       int32_t dtype, int32_t n_rows, const plora_matrix* out, plora_stream stream);
 
+/* Which of their kernels the two calls above choose (for tests and profiles; host only, no pointer but the records' own is followed): a workgroup's rows and channels,
+ * and the parts that K is split in among its wavefronts.  16 rows: operands go from memory to registers; more: through LDS.  grouped, gathered: 0 or 1, whether the call is
+ * plora_fp8_grouped, and with `rows`.  The choice goes by sizes, the element type and x's code_stride. */
+typedef struct {
+  int32_t rows, channels, parts;
+} plora_fp8_tile;
+int plora_fp8_tile_of(const plora_fp8_rows* x, int32_t n_x_rows, const plora_fp8_weights* w, int32_t dtype, int32_t n_rows, int32_t grouped, int32_t gathered,
+                      plora_fp8_tile* tile);
+
 /* Tokens to experts.  logits: n_tokens rows of n_experts (1 .. 1024) values; of each the top_k (1 .. 32, at most n_experts) largest are chosen, largest first,
  * ties to the lowest index.  A logit of -inf or NaN is never chosen (padding: a row of -inf), and where fewer than top_k are left
  * the rest have expert -1, weight 0, place -1.  In 32 bits:

@@ -29,7 +29,7 @@ __all__ = ["PLORA_OK", "PLORA_ERR_INVAL", "PLORA_ERR_NOMEM", "PLORA_ERR_EXISTS",
            "plora_rotary_table", "plora_rotate", "plora_kv_page_bytes", "plora_kv_append", "plora_kv_read", "plora_kv_attend",
            "RotaryConfig", "RotaryStruct", "RowsStruct", "KvCacheStruct", "KvBatchStruct", "Rotary", "KvBatch", "PagedKvCache",
            "PLORA_ACT_NONE", "PLORA_ACT_SILU", "PLORA_ACT_GELU",
-           "plora_norm", "plora_fp8_quantise", "plora_fp8_quantise_weights", "plora_fp8_matmul", "plora_fp8_grouped", "plora_route",
+           "plora_norm", "plora_fp8_quantise", "plora_fp8_quantise_weights", "plora_fp8_matmul", "plora_fp8_grouped", "plora_fp8_tile_of", "plora_route",
            "plora_route_workspace_bytes", "MatrixStruct", "Fp8RowsStruct", "Fp8WeightsStruct", "NormWeightsStruct", "BlockNormStruct",
            "Fp8Rows", "Fp8Weights", "Routing", "NormWeights", "BlockNorm"]
 
@@ -921,6 +921,7 @@ lib.plora_fp8_quantise.argtypes = [_i32, _i32, _i32, _matrix_p, _i32, _fp8_rows_
 lib.plora_fp8_quantise_weights.argtypes = [_i32, _matrix_p, _fp8_weights_p, _vp]
 lib.plora_fp8_matmul.argtypes = [_fp8_rows_p, _fp8_weights_p, _i32, _i32, _matrix_p, _vp]
 lib.plora_fp8_grouped.argtypes = [_fp8_rows_p, _i32, _fp8_weights_p, _vp, _vp, _i32, _i32, _matrix_p, _vp]
+lib.plora_fp8_tile_of.argtypes = [_fp8_rows_p, _i32, _fp8_weights_p, _i32, _i32, _i32, _i32, _vp]
 lib.plora_route.argtypes = [_i32, _i32, _i32, _i32, _matrix_p, _i32, _f32, _vp, _vp, _vp, _vp, _vp, _vp, _u64, _vp]
 lib.plora_route_workspace_bytes.argtypes = [_i32, _i32]
 lib.plora_route_workspace_bytes.restype = _u64
@@ -948,6 +949,13 @@ def plora_fp8_matmul(x, w, dtype, n_rows, out, stream=None):
 
 def plora_fp8_grouped(x, n_x_rows, w, offsets_ptr, rows_ptr, dtype, n_rows, out, stream=None):
     return lib.plora_fp8_grouped(x, n_x_rows, w, offsets_ptr, rows_ptr, dtype, n_rows, out, stream)
+
+
+def plora_fp8_tile_of(x, n_x_rows, w, dtype, n_rows, grouped=False, gathered=False):
+    """-> (status, (rows, channels, parts)) of the kernel that the product of these sizes runs on; x: Fp8RowsStruct, w: Fp8WeightsStruct."""
+    tile = (_i32 * 3)()
+    rc = lib.plora_fp8_tile_of(x, n_x_rows, w, dtype, n_rows, int(grouped), int(gathered), tile)
+    return rc, tuple(tile)
 
 
 def plora_route_workspace_bytes(n_tokens, n_experts):

@@ -578,35 +578,39 @@ int best_of(const Kind* kinds, const ProductArgs& a, bool grouped) {
 }
 
 // k_few for up to 16 rows (experts: up to 8 on average), else the tiles that the fit has as the fastest.  k_product's loads name x's
-// codes by 31 bits; where a tile's rows lie further apart k_few has them all.
+// codes by 31 bits; where a tile's rows lie further apart k_few has them all.  The result is an index of kFew or, behind them, of kTiles.
+// kFew's last two differ in the wavefronts that share K: where 4 had less than 3 blocks each there are 2 (256 experts of 4096 x 512, 512 rows: 134 -> 96 us; 128 of
+// 2048 x 768: 45.3 -> 41.4).
+constexpr Kind kFew[] = {{16, 16, 8, 2, 1.15f, 0.591f, 1.114f}, {16, 32, 8, 2, 0.72f, 1.147f, 1.67f}, {16, 64, 4, 4, 0.f, 1.172f, 1.391f}, {16, 64, 2, 4, 0.f, 0.f, 0.f}};
+constexpr Kind kTiles[] = {{64, 32, 2, 1, 1.85f, 0.379f, 0.f},  {64, 64, 2, 1, 1.79f, 0.525f, 0.f},   {64, 64, 1, 2, 0.99f, 0.295f, 0.234f},
+                           {64, 128, 1, 2, 2.f, 0.48f, 0.36f},  {128, 64, 1, 1, 2.07f, 0.421f, 0.f},  {128, 128, 1, 1, 2.79f, 0.593f, 0.f},
+                           {128, 256, 1, 1, 3.93f, 0.896f, 0.f}, {256, 128, 1, 1, 4.21f, 0.87f, 0.f}, {256, 256, 1, 1, 4.93f, 1.612f, 0.f}};
+int chosen(const ProductArgs& a, bool grouped, bool gathered, int dtype) {
+  const bool far = gathered ? (__int128)a.n_x_rows * a.x_s > kReach - 256 : 256 * (__int128)a.x_s > kReach - 256;
+  if (far || (grouped ? (int64_t)a.n_rows <= 8 * (int64_t)a.n_experts : a.n_rows <= 16)) {
+    const int few = best_of<3>(kFew, a, grouped);
+    return few == 2 && a.k <= 11 * kBlock ? 3 : few;
+  }
+  return 4 + (dtype == PLORA_F32 ? best_of<8>(kTiles, a, grouped) : best_of<9>(kTiles, a, grouped));  // (fp32's operands of the largest tile do not fit the registers)
+}
+
 template <int DT, bool GROUPED>
 int product(const ProductArgs& a, plora_stream stream) {
-  const bool far = a.rows ? (__int128)a.n_x_rows * a.x_s > kReach - 256 : 256 * (__int128)a.x_s > kReach - 256;
-  if (far || (GROUPED ? (int64_t)a.n_rows <= 8 * (int64_t)a.n_experts : a.n_rows <= 16)) {
-    static constexpr Kind kFew[] = {{16, 16, 8, 2, 1.15f, 0.591f, 1.114f}, {16, 32, 8, 2, 0.72f, 1.147f, 1.67f}, {16, 64, 4, 4, 0.f, 1.172f, 1.391f}};
-    switch (best_of<3>(kFew, a, GROUPED)) {
-      case 0: return few<DT, GROUPED, 1, 8, 2>(a, stream);
-      case 1: return few<DT, GROUPED, 2, 8, 2>(a, stream);
-      default:  // less than 3 blocks for each of 4 wavefronts: two of them (256 experts of 4096 x 512, 512 rows: 134 -> 96 us; 128 of 2048 x 768: 45.3 -> 41.4)
-        if (a.k <= 11 * kBlock) return few<DT, GROUPED, 4, 2, 2>(a, stream);
-        return few<DT, GROUPED, 4, 4, 2>(a, stream);
-    }
-  }
-  static constexpr Kind kTiles[] = {{64, 32, 2, 1, 1.85f, 0.379f, 0.f},  {64, 64, 2, 1, 1.79f, 0.525f, 0.f},   {64, 64, 1, 2, 0.99f, 0.295f, 0.234f},
-                                    {64, 128, 1, 2, 2.f, 0.48f, 0.36f},   {128, 64, 1, 1, 2.07f, 0.421f, 0.f},  {128, 128, 1, 1, 2.79f, 0.593f, 0.f},
-                                    {128, 256, 1, 1, 3.93f, 0.896f, 0.f}, {256, 128, 1, 1, 4.21f, 0.87f, 0.f},  {256, 256, 1, 1, 4.93f, 1.612f, 0.f}};
-  constexpr int kOf = DT == PLORA_F32 ? 8 : 9;  // (fp32's operands of the largest tile do not fit the registers)
-  switch (best_of<kOf>(kTiles, a, GROUPED)) {
-    case 0: return tiled<DT, GROUPED, 64, 32, 4, 1, 2, 4>(a, stream);
-    case 1: return tiled<DT, GROUPED, 64, 64, 2, 2, 2, 3>(a, stream);
-    case 2: return tiled<DT, GROUPED, 64, 64, 2, 2, 1, 4>(a, stream);
-    case 3: return tiled<DT, GROUPED, 64, 128, 2, 2, 1, 3>(a, stream);
-    case 4: return tiled<DT, GROUPED, 128, 64, 4, 2, 1, 4>(a, stream);
-    case 5: return tiled<DT, GROUPED, 128, 128, 4, 2, 1, 4>(a, stream);
-    case 6: return tiled<DT, GROUPED, 128, 256, 2, 4, 1, 3>(a, stream);
-    case 7: return tiled<DT, GROUPED, 256, 128, 4, 2, 1, 3>(a, stream);
+  switch (chosen(a, GROUPED, a.rows != nullptr, DT)) {
+    case 0: return few<DT, GROUPED, 1, 8, 2>(a, stream);
+    case 1: return few<DT, GROUPED, 2, 8, 2>(a, stream);
+    case 2: return few<DT, GROUPED, 4, 4, 2>(a, stream);
+    case 3: return few<DT, GROUPED, 4, 2, 2>(a, stream);
+    case 4: return tiled<DT, GROUPED, 64, 32, 4, 1, 2, 4>(a, stream);
+    case 5: return tiled<DT, GROUPED, 64, 64, 2, 2, 2, 3>(a, stream);
+    case 6: return tiled<DT, GROUPED, 64, 64, 2, 2, 1, 4>(a, stream);
+    case 7: return tiled<DT, GROUPED, 64, 128, 2, 2, 1, 3>(a, stream);
+    case 8: return tiled<DT, GROUPED, 128, 64, 4, 2, 1, 4>(a, stream);
+    case 9: return tiled<DT, GROUPED, 128, 128, 4, 2, 1, 4>(a, stream);
+    case 10: return tiled<DT, GROUPED, 128, 256, 2, 4, 1, 3>(a, stream);
+    case 11: return tiled<DT, GROUPED, 256, 128, 4, 2, 1, 3>(a, stream);
     default:
-      if constexpr (kOf == 9) return tiled<DT, GROUPED, 256, 256, 4, 2, 1, 3, true>(a, stream);
+      if constexpr (DT != PLORA_F32) return tiled<DT, GROUPED, 256, 256, 4, 2, 1, 3, true>(a, stream);
       else return PLORA_ERR_INVAL;
   }
 }
@@ -650,4 +654,22 @@ extern "C" int plora_fp8_grouped(const plora_fp8_rows* x, int32_t n_x_rows, cons
   return dtype == PLORA_BF16  ? product<PLORA_BF16, true>(a, stream)
          : dtype == PLORA_F16 ? product<PLORA_F16, true>(a, stream)
                               : product<PLORA_F32, true>(a, stream);
+}
+
+extern "C" int plora_fp8_tile_of(const plora_fp8_rows* x, int32_t n_x_rows, const plora_fp8_weights* w, int32_t dtype, int32_t n_rows, int32_t grouped,
+                                 int32_t gathered, plora_fp8_tile* tile) {
+  if (!x || !good_sizes(w) || !good_dtype(dtype) || n_rows < 1 || n_x_rows < 1 || x->code_stride < 0 || x->code_stride > kMostStride || !tile ||
+      (!grouped && (gathered || w->n_experts != 1)))
+    return PLORA_ERR_INVAL;
+  ProductArgs a = {};
+  a.x_s = x->code_stride;
+  a.n_rows = n_rows;
+  a.n_x_rows = n_x_rows;
+  a.n = w->n;
+  a.k = w->k;
+  a.n_experts = w->n_experts;
+  const int i = chosen(a, grouped != 0, gathered != 0, dtype);
+  const Kind& kind = i < 4 ? kFew[i] : kTiles[i - 4];
+  *tile = plora_fp8_tile{kind.tt, kind.tn, kind.kg};
+  return PLORA_OK;
 }
