@@ -103,7 +103,7 @@ struct NormArgs {
 // A row has TPR threads, each with V groups of 8 channels (group i of thread j: channels 8 * (j + TPR * i)), held in registers from the
 // first load to the last store: every input is read once.  PLACES: a token's rows are gathered; FULL: with a gate or a norm ahead of it.  (Kernels of
 // their own for the registers of calls without them: 4096 channels take 58 in place of 103.)  Memory bounds it: 5093 rows of 5120 with all parts 48 us
-// for 236 MB, 2049 rows of 4096 that gather 4 rows each 28 us for 118 MB (four rows in flight and 140 registers: 30).
+// for 236 MB, 2049 rows of 4096 that gather 4 rows each 27.5 us for 118 MB (four rows in flight and 140 registers: 30).
 template <int DT, int TPR, int V, bool PLACES, bool FULL>
 __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
   constexpr int B = Elt<DT>::B, ROWS = kThreads / TPR;
@@ -296,8 +296,8 @@ struct QuantiseArgs {
   int32_t n_rows, k;
 };
 
-// 16 threads have a block of a row, a workgroup 16 rows, whose scales are one line.  Memory bounds it: 5093 rows of 4096 12.1 us for 63 MB
-// (5.2 TB/s; with four blocks a thread 14.4).
+// 16 threads have a block of a row, a workgroup 16 rows, whose scales are one line.  Memory bounds it: 5093 rows of 4096 11.9 us for 63 MB
+// (5.3 TB/s; with four blocks a thread 14.4).
 template <int DT, int ACT>
 __global__ __launch_bounds__(kThreads) void k_quantise(QuantiseArgs a) {
   constexpr int B = Elt<DT>::B;

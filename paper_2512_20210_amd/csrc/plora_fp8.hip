@@ -188,7 +188,7 @@ __device__ __forceinline__ void st4(uint8_t* p, f32x4 f) {
 // (973), 32 x 32 x 64 instructions (registers spill: 2032), 4 wavefronts of 128 x 128 (1196), lines asked for 4 stages ahead (1040), wave
 // priorities (952).
 // Smaller tiles are bound by how fast a CU gets operands that are not in its L2: with no products and no LDS reads at all, 512 x 4096 x 4096 takes
-// 17.7 us of 18.3 (14.2 from L2, which alone feeds a CU with 140 - 150 GB/s; from memory it gets 40 - 60).  Two blocks a barrier, five or six stages, all
+// 17.7 us of 18.5 (14.2 from L2, which alone feeds a CU with 140 - 150 GB/s; from memory it gets 40 - 60).  Two blocks a barrier, five or six stages, all
 // operands of a stage in registers a stage ahead, and tiles that begin at different blocks change nothing or cost up to 10 %; two sets of
 // wavefronts where there are few tiles.  Scales come through LDS as well: a scalar load in flight makes each wait for an LDS read wait for it
 // too (1024 x 1024 x 4096: 12.5 -> 11.1 us; 2048 x 5120 x 13824: 173 -> 167).
@@ -391,9 +391,10 @@ __global__ __launch_bounds__(64 * WT * WN * KG) __attribute__((amdgpu_waves_per_
 // Few rows: a workgroup has TT rows x 16 NW channels, and its WAVES wavefronts the blocks of 128 values in turn; operands go from memory to registers,
 // P of a wavefront's blocks ahead, with no barrier until the wavefronts' sums are joined in LDS (in their order: the sums do not depend
 // on which is done first).
-// Memory bounds it: 64 experts of 2816 x 2048 with 6 rows each read 5.4 TB/s (67 us). Not kept: a workgroup with 128 channels, which goes through them
+// Memory bounds it: 64 experts of 2816 x 2048 with 6 rows each read 5.25 TB/s (68.7 us). Not kept: a workgroup with 128 channels, which goes through them
 // with x in registers, the next ones' weights on their way and a join a step (78); x in LDS and wavefronts that read their channels on their
-// own, 2 to 8 blocks ahead and with nothing to join (69 - 75).
+// own, 2 to 8 blocks ahead and with nothing to join (69 - 75).  Where n is small few workgroups read the weights: one row of 1024 x 4096 takes 5.1 us on 64 CUs, of
+// 2048 x 11008 9.6 on 128.
 template <int DT, int TT, int NW, int WAVES, int P, bool GROUPED>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void k_few(ProductArgs args) {
   constexpr int NT = TT / 16;
@@ -521,10 +522,13 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 
 // ---- host side ----------------------------------------------------------------------------------------
 
-// A kernel's tile, and what it takes by a fit to calls of 1 .. 4096 rows times weights of 520 x 1040 .. 13824 x 5120 (and 2 .. 256 experts): for each round of
-// a CU `fixed` and for every step (KG blocks of 128 values) `step`, with `more` for each further workgroup that runs on the CU beside it, of
-// `at_once`; all in us.  Beside that the weights are read, with 5.3 TB/s where workgroups overlap on a CU and 4.4 where not; the two as a
+// A kernel's tile, and its cost in the rule.  The figures come from a fit (in us) to calls of 1 .. 4096 rows times weights of 520 x 1040 .. 13824 x 5120 that come from
+// memory (and 2 .. 256 experts): for each round of a CU `fixed` and for every step (KG blocks of 128 values) `step`, with `more` for each further workgroup that runs on the
+// CU beside it, of `at_once`.  Beside that the weights are read, with 5.3 TB/s where workgroups overlap on a CU and 4.4 where not; the two as a
 // root of squares (16 experts of 4096 x 13824, 512 rows of uneven groups: 253 -> 203 us; 8 of 7168 x 4096, 800 rows: 115 -> 78; 256 of 4096 x 512, 4096 rows: 256 -> 164).
+// The sum compares kernels for one call and is no forecast of its time, as the steps were fitted ahead of that root and have some of the reading in them: 256 rows of 13824 x 5120 34.0
+// (measured 35.6, and 26.4 with weights that are in the last-level cache), one row 20.8 (16.3), 10186 rows of 8 experts of 7168 x 4096 290.6 (326).  Of experts it
+// has the average number of rows alone.
 struct Kind {
   int tt, tn, kg, at_once;
   float fixed, step, more;
@@ -579,8 +583,8 @@ int best_of(const Kind* kinds, const ProductArgs& a, bool grouped) {
 
 // k_few for up to 16 rows (experts: up to 8 on average), else the tiles that the fit has as the fastest.  k_product's loads name x's
 // codes by 31 bits; where a tile's rows lie further apart k_few has them all.  The result is an index of kFew or, behind them, of kTiles.
-// kFew's last two differ in the wavefronts that share K: where 4 had less than 3 blocks each there are 2 (256 experts of 4096 x 512, 512 rows: 134 -> 96 us; 128 of
-// 2048 x 768: 45.3 -> 41.4).
+// kFew's last two differ in the wavefronts that share K: where 4 had less than 3 blocks each there are 2 (256 experts of 4096 x 512, 512 rows: 120 -> 89 us; 128 of
+// 2048 x 768: 45.1 -> 42.0).
 constexpr Kind kFew[] = {{16, 16, 8, 2, 1.15f, 0.591f, 1.114f}, {16, 32, 8, 2, 0.72f, 1.147f, 1.67f}, {16, 64, 4, 4, 0.f, 1.172f, 1.391f}, {16, 64, 2, 4, 0.f, 0.f, 0.f}};
 constexpr Kind kTiles[] = {{64, 32, 2, 1, 1.85f, 0.379f, 0.f},  {64, 64, 2, 1, 1.79f, 0.525f, 0.f},   {64, 64, 1, 2, 0.99f, 0.295f, 0.234f},
                            {64, 128, 1, 2, 2.f, 0.48f, 0.36f},  {128, 64, 1, 1, 2.07f, 0.421f, 0.f},  {128, 128, 1, 1, 2.79f, 0.593f, 0.f},
