@@ -97,6 +97,8 @@ class Case:
 
     def evict(self, i):
         self.opool.evict(i)
+        import paper_2512_20210_amd as P
+        assert P.plora_sync_adapter(self.gpool.h, i) == P.PLORA_OK  # (while its own copy runs an adapter is BUSY)
         self.gpool.evict(i)
 
     def run(self, t2a, slots=None, seed=0, y0_zero=False, check=True, x_std=1.0, share_x=(), y0_fill=None, xs=None):
